@@ -1,0 +1,584 @@
+"""Performance cases of the operators around the FP4 cache: what a serving
+engine calls between its scheduler and the attention output.
+
+A case is a dict of plain values; `kind` is
+
+  plan    block tables and slot maps of a ragged batch from its lengths
+  rows    per-head norms of queries and keys and the position rotation, rows in and out
+  write   the same pass with the prepared FP8 query and K and V into the FP4
+          cache, then the written tokens read back as rows
+  read    stored tokens read back as rows
+  extend  attention of several new queries per sequence over the FP4 cache,
+          causal, with or without a sliding window and first tokens that stay visible
+  window  the same windowed attention for one query per sequence
+
+Lengths follow from "lens" alone (equal where "spread" is 0, else lognormal
+around the median, clipped to [low, high]); a seed draws their order, the
+pages, the codes and the rows.  Caches hold codes of Gaussian data: E2M1 codes
+with the level frequencies of N(0, 1) under a scale of 2.9 levels per sigma
+and scale bytes around 2^-1.5, in the library's tile layout, at pages that are
+a random permutation of the pool.
+
+`own` false: plain torch in 32 bits (the rotated query in 64, since its FP8
+rounding has borders); true: the library's calls.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE = 16
+C = 0.156
+EPS = 1e-6
+DTYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16, "float16": torch.float16}
+DEVICE = "cuda" if torch.cuda.is_available() else "cpu"
+
+
+def _attend(name, kind, batch, q_heads, kv_heads, context, head_dim=128, spread=0.0, low=1, high=131072, lens=0,
+            bound=0, new=1, new_spread=0.0, window=0, sinks=0, dtype="bfloat16", rotate_v=True):
+    return dict(name=name, kind=kind, batch=batch, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim,
+                context=context, spread=spread, low=low, high=high, lens=lens, bound=bound, new=new,
+                new_spread=new_spread, window=window, sinks=sinks, dtype=dtype, rotate_v=rotate_v)
+
+
+def _rows(name, kind, tokens, q_heads, kv_heads, head_dim=128, rot=128, interleaved=False, norm=True,
+          dtype="bfloat16", fused=True, rotate_v=True, fp8=True):
+    return dict(name=name, kind=kind, tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, rot=rot,
+                interleaved=interleaved, norm=norm, dtype=dtype, fused=fused, rotate_v=rotate_v, fp8=fp8)
+
+
+def listed():
+    return [
+        # every decode step of a batch of 64: one new token each, a page now and then; all launch latency
+        dict(name="plan-step-b64", kind="plan", batch=64, context=8192, new=1, spread=0.9, lens=1, width=2048,
+             capacity=64),
+        # a scheduler's mixed step: prompt chunks and single tokens of 300 sequences, padded to its token budget
+        dict(name="plan-mixed-b300", kind="plan", batch=300, context=3000, new=40, spread=1.4, lens=2, width=1024,
+             capacity=32768),
+        # the decode step of a batch of 32, Qwen3-235B-like heads: QK norm, rotation, FP8 query, cache write
+        _rows("write-step-32", "write", 32, 64, 4),
+        # a prompt's rows of one layer at once, out of the fused QKV buffer
+        _rows("write-prompt-16381", "write", 16381, 64, 8),
+        # a layer without QK norm and head size 64, adjacent pairs rotated, rows for a cache of another format
+        _rows("rows-head64-8191", "rows", 8191, 64, 8, head_dim=64, rot=64, interleaved=True, norm=False,
+              dtype="float16", fused=False, fp8=False),
+        # a cached prefix of one layer handed on as rows
+        _rows("read-65530", "read", 65530, 8, 8),
+        # a first prompt of 8192 tokens: compute bound
+        _attend("extend-prompt-8192", "extend", 1, 64, 4, 8192, new=8192),
+        # chunked prefill and decode in one step: ragged chunks behind contexts of up to 32k tokens
+        _attend("extend-mixed-b12", "extend", 12, 48, 8, 9000, spread=0.9, low=40, high=32768, lens=4, new=300,
+                new_spread=1.5),
+        # verification of 5 drafted tokens per sequence: few rows over long contexts
+        _attend("extend-draft-b16", "extend", 16, 64, 8, 16000, spread=0.3, low=1000, high=32768, lens=5, new=5),
+        # a windowed head-size-64 layer in prefill, first tokens kept visible
+        _attend("extend-window-4099", "extend", 2, 64, 8, 6000, head_dim=64, spread=0.2, lens=6, new=4099, window=1024,
+                sinks=4),
+        # a windowed layer's decode step of a large batch with long contexts
+        _attend("window-b64-w4096", "window", 64, 64, 8, 30000, spread=0.7, low=300, high=131072, lens=7, window=4096,
+                sinks=4),
+        # a narrow window for a few users, one GPU's share of a head-size-64 layer: latency
+        _attend("window-b8-w128", "window", 8, 8, 1, 5000, head_dim=64, spread=0.5, low=20, lens=8, window=128,
+                sinks=1),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["plan", "rows", "write", "write", "read", "extend", "extend", "extend", "window", "window"])
+    d = rng.choice([64, 128, 128, 128, 256])
+    hkv = rng.choice([1, 2, 3, 4, 8])
+    g = rng.choice([1, 4, 5, 6, 8, 8, 12, 16])
+    if kind == "plan":
+        batch = _log(rng, 1, 1000)
+        new = rng.choice([1, 1, _log(rng, 1, max(2, 30000 // batch))])
+        return dict(kind="plan", batch=batch, context=_log(rng, 1, 16000), new=new, spread=rng.choice([0.0, 0.5, 1.0]),
+                    lens=rng.randrange(1 << 16), width=2048, capacity=_log(rng, max(1, batch * new // 2), 4 * batch * new))
+    if kind in ("rows", "write", "read"):
+        tokens = _log(rng, 1, 16000 if kind == "write" else 30000)
+        case = _rows("", kind, tokens, hkv * g, hkv, d, rot=rng.choice([d, d, 64, 32, 0]),
+                     interleaved=rng.random() < 0.3, norm=rng.random() < 0.7,
+                     dtype=rng.choice(["bfloat16", "bfloat16", "float16", "float32"]),
+                     fused=rng.random() < 0.6, fp8=kind == "write" and rng.random() < 0.7)
+    elif kind == "extend":
+        batch = _log(rng, 1, 24)
+        ctx = _log(rng, 16, 30000)
+        # query-key pairs no more than the largest listed case's
+        new = _log(rng, 1, max(2, min(ctx, int(1.5e11 / (hkv * g * d * batch * ctx)))))
+        case = _attend("", "extend", batch, hkv * g, hkv, max(ctx, new), d, spread=rng.choice([0.0, 0.3, 0.8]),
+                       high=32768, lens=rng.randrange(1 << 16), new=new, new_spread=rng.choice([0.0, 0.7]),
+                       window=rng.choice([0, 0, _log(rng, 16, 8192)]), sinks=rng.choice([0, 1, 4, 64]),
+                       dtype=rng.choice(["bfloat16", "bfloat16", "float16", "float32"]), rotate_v=rng.random() < 0.8)
+    else:
+        window = _log(rng, 16, 8192)
+        case = _attend("", "window", _log(rng, 1, 64), hkv * g, hkv, _log(rng, 16, 60000), d,
+                       spread=rng.choice([0.0, 0.3, 0.8]), high=131072, lens=rng.randrange(1 << 16),
+                       bound=rng.choice([0, 131072]), window=window, sinks=rng.choice([0, 1, 4, 64, 200]),
+                       dtype=rng.choice(["bfloat16", "bfloat16", "float16", "float32"]), rotate_v=rng.random() < 0.8)
+    del case["name"]
+    return case
+
+
+def _lengths(case):
+    """(cached tokens, new tokens) of every sequence of a plan; (context, queries) of an attention."""
+    r = random.Random(case["lens"])
+
+    def one(median, spread, lo, hi):
+        return min(max(int(median * math.exp(spread * r.gauss(0, 1))), lo), hi) if spread else median
+
+    if case["kind"] == "plan":
+        return [(one(case["context"], case["spread"], 0, 16 * case["width"] // 2),
+                 one(case["new"], case["spread"] if case["new"] > 1 else 0.0, 0, 8 * case["width"]))
+                for _ in range(case["batch"])]
+    out = []
+    for _ in range(case["batch"]):
+        ctx = one(case["context"], case["spread"], case["low"], case["high"])
+        out.append((ctx, min(ctx, one(case["new"], case["new_spread"], 1, 1 << 20))))
+    return out
+
+
+# --------------------------------------------------------------------------
+# Inputs
+
+
+def _gen(seed):
+    return torch.Generator(device=DEVICE).manual_seed(seed)
+
+
+def _pools(case, num_pages, seed):
+    """Codes and scales of `num_pages` pages of Gaussian data."""
+    gen, h, d = _gen(seed), case["kv_heads"], case["head_dim"]
+    # level frequencies: 2^15 quantiles of |N(0, 1)| at 2.9 levels per sigma, both nibbles of a byte from 8 bits of
+    # them, independent
+    x = np.sqrt(2) * _erfinv((np.arange(128) + 0.5) / 128) * 2.9
+    mag = np.searchsorted([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], x).astype(np.int64)
+    nib = np.concatenate([mag, mag + 8])
+    byte = torch.as_tensor((nib[:, None] + 16 * nib[None, :]).reshape(-1).astype(np.uint8), device=DEVICE)
+    codes = torch.empty(num_pages * h * 16 * d, dtype=torch.uint8, device=DEVICE)
+    for lo in range(0, codes.numel(), 1 << 27):
+        n = min(1 << 27, codes.numel() - lo)
+        codes[lo:lo + n] = byte[torch.randint(0, 1 << 16, (n,), generator=gen, device=DEVICE, dtype=torch.int32).long()]
+    scales = torch.randint(124, 127, (num_pages * h * d,), generator=gen, device=DEVICE, dtype=torch.uint8)
+    return codes, scales
+
+
+def _erfinv(y):
+    return torch.erfinv(torch.as_tensor(y, dtype=torch.float64)).numpy()
+
+
+def _prepare_plan(case, seed):
+    rng = np.random.default_rng(seed)
+    pairs = np.array(_lengths(case), dtype=np.int64)[rng.permutation(case["batch"])]
+    held = -(-pairs[:, 0] // PAGE)
+    need = int((-(-(pairs.sum(1)) // PAGE) - held).sum())
+    perm = rng.permutation(int(held.sum()) + need + 9)
+    table = np.zeros((case["batch"], case["width"]), dtype=np.int32)
+    at = 0
+    for b, n in enumerate(held):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    t = lambda x: torch.as_tensor(np.ascontiguousarray(x.astype(np.int32)), device=DEVICE)  # noqa: E731
+    state = dict(cached=t(pairs[:, 0]), new=t(pairs[:, 1]), free=t(perm[at:]), table=t(table))
+    if own:
+        from paper_2606_20474_amd import uq
+        state["plan"] = uq.TokenPlan.alloc(case["batch"], case["capacity"], DEVICE)
+    return state
+
+
+def _table(case, lens, rng):
+    """Page table of a batch, its pages a permutation of the pool; spare pages at the end."""
+    pages = [-(-n // PAGE) for n in lens]
+    num_pages = sum(pages) + 3
+    perm = rng.permutation(num_pages)
+    bound = max(case.get("bound", 0), max(lens))
+    table = np.zeros((len(lens), -(-bound // PAGE)), dtype=np.int32)
+    at = 0
+    for b, n in enumerate(pages):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    return table, num_pages, bound
+
+
+def _desc(case, num_pages):
+    from paper_2606_20474_amd import uq
+    return uq.CacheDesc(num_kv_heads=case["kv_heads"], num_pages=num_pages, c=C, rotate_v=case["rotate_v"],
+                        head_dim=case["head_dim"])
+
+
+def _prepare_rows(case, seed):
+    rng, gen = np.random.default_rng(seed), _gen(seed)
+    t, hq, hkv, d, dt = case["tokens"], case["q_heads"], case["kv_heads"], case["head_dim"], DTYPES[case["dtype"]]
+    num_seqs = min(8, t)
+    per = -(-t // num_seqs)
+    table, num_pages, _ = _table(case, [per] * num_seqs, rng)
+    seq, pos = np.arange(t) // per, np.arange(t) % per
+    slots = table[seq, pos // PAGE].astype(np.int64) * PAGE + pos % PAGE
+    state = dict(slots=torch.as_tensor(slots, device=DEVICE), num_pages=num_pages)
+    if case["kind"] == "read":
+        state["pools"] = _pools(case, num_pages, seed)
+        if own:
+            state["desc"] = _desc(case, num_pages)
+            state["out"] = [torch.empty((t, hkv, d), dtype=dt, device=DEVICE) for _ in range(2)]
+        return state
+    gain = np.ones((hq + 2 * hkv, d), dtype=np.float32)   # four outlier channels per KV head, as keys and values have
+    for h in range(hq, hq + 2 * hkv):
+        gain[h, rng.permutation(d)[:4]] = 20.0
+    buf = torch.randn((t, hq + 2 * hkv, d), generator=gen, device=DEVICE, dtype=torch.float32)
+    buf = buf.mul_(torch.as_tensor(gain, device=DEVICE)).to(dt)
+    rows = buf[:, :hq], buf[:, hq:hq + hkv], buf[:, hq + hkv:]
+    state["q"], state["k"], state["v"] = rows if case["fused"] else [x.contiguous() for x in rows]
+    state["w"] = [torch.rand(d, generator=gen, device=DEVICE) + 0.5 for _ in range(2)] if case["norm"] else [None, None]
+    # a later chunk of a long conversation: positions from 20000 on
+    state["pos"] = torch.as_tensor((pos + 20000).astype(np.int32), device=DEVICE)
+    if case["rot"]:
+        angle = torch.outer(torch.arange(20000 + per, dtype=torch.float64),
+                            10000.0 ** (-torch.arange(0, case["rot"], 2, dtype=torch.float64) / case["rot"]))
+        state["table"] = torch.cat([angle.cos(), angle.sin()], 1).float().to(DEVICE)
+    else:
+        state["table"] = None
+    if own:
+        from paper_2606_20474_amd import uq
+        state["spec"] = uq.NormRope(positions=state["pos"], cos_sin=state["table"], q_weight=state["w"][0],
+                                    k_weight=state["w"][1], eps=EPS, interleaved=case["interleaved"])
+        state["q_out"] = torch.empty((t, hq, d), dtype=torch.uint8 if case["fp8"] else dt, device=DEVICE)
+        state["out"] = [torch.empty((t, hkv, d), dtype=torch.bfloat16 if case["kind"] == "write" else dt, device=DEVICE)
+                        for _ in range(2)]
+        if case["kind"] == "write":
+            state["desc"] = _desc(case, num_pages)
+            state["pools"] = state["desc"].alloc_pools(DEVICE, fill=0)
+    return state
+
+
+def _prepare_attend(case, seed):
+    rng, gen = np.random.default_rng(seed), _gen(seed)
+    pairs = np.array(_lengths(case), dtype=np.int64)[rng.permutation(case["batch"])]
+    lens, new = pairs[:, 0], pairs[:, 1] if case["kind"] == "extend" else np.ones(case["batch"], dtype=np.int64)
+    table, num_pages, bound = _table(case, [int(n) for n in lens], rng)
+    hq, d, dt = case["q_heads"], case["head_dim"], DTYPES[case["dtype"]]
+    state = dict(pools=_pools(case, num_pages, seed), table=torch.as_tensor(table, device=DEVICE),
+                 lens=torch.as_tensor(lens.astype(np.int32), device=DEVICE), bound=bound,
+                 cu=torch.as_tensor(np.concatenate([[0], np.cumsum(new)]).astype(np.int32), device=DEVICE),
+                 pairs=[(int(n), int(m)) for n, m in zip(lens, new)],
+                 q=torch.randn((int(new.sum()), hq, d), generator=gen, device=DEVICE, dtype=torch.float32).to(dt))
+    if own:
+        from paper_2606_20474_amd import uq
+        desc = state["desc"] = _desc(case, num_pages)
+        state["out"] = torch.empty(state["q"].shape, dtype=torch.bfloat16, device=DEVICE)
+        if case["kind"] == "extend":
+            n = uq.extend_workspace_bytes(desc, state["q"].shape[0], case["batch"], hq, bound, case["window"], case["sinks"])
+        else:
+            n = uq.decode_window_workspace_bytes(desc, case["batch"], hq, bound, case["window"], case["sinks"])
+        state["workspace"] = torch.empty(n, dtype=torch.uint8, device=DEVICE)
+    return state
+
+
+def prepare(case, seed):
+    make = {"plan": _prepare_plan, "rows": _prepare_rows, "write": _prepare_rows, "read": _prepare_rows,
+            "extend": _prepare_attend, "window": _prepare_attend}[case["kind"]]
+    return dict(make(case, seed), case=case)
+
+
+# --------------------------------------------------------------------------
+# The plain forms
+
+
+def _hadamard(d, dtype):
+    h = torch.ones((1, 1), dtype=torch.float64)
+    while h.shape[0] < d:
+        h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+    return (h / math.sqrt(d)).to(DEVICE, dtype)
+
+
+def _fp8_query(q, d):
+    """e4m3(R q), the rotation in 64 bits: the rounding has borders."""
+    return (q.double() @ _hadamard(d, torch.float64)).clamp(-448, 448).float().to(torch.float8_e4m3fn)
+
+
+def _stored(case, pools, page, off):
+    """K and V in 32 bits, as stored, of the tokens at (page, off): [..., Hkv, d] each."""
+    h, d = case["kv_heads"], case["head_dim"]
+    codes, scales = pools
+    level = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6], device=DEVICE)
+    pair = torch.stack([level.repeat(16), level.repeat_interleave(16)], 1)         # a byte's two values
+    k = codes.view(-1, h, 2, d // 32, PAGE, 16)[page, :, 0, :, off]                # [..., Hkv, d/32, 16]
+    v = codes.view(-1, h, 2, 4, d // 8, 4, 4)[page, :, 1, off // 4, :, off % 4]    # [..., Hkv, d/8, 4]
+    s = scales.view(-1, h, 2, d // 32, PAGE)[page, :, :, :, off]                   # [..., Hkv, 2, d/32]
+    s = torch.exp2(s.float() - 127)[..., None]
+    return ((pair[k.int()].flatten(-2) * s[..., 0, :, :]).flatten(-2),
+            (pair[v.int()].reshape(*v.shape[:-2], d // 32, 32) * s[..., 1, :, :]).flatten(-2))
+
+
+def _plan_plain(s):
+    case = s["case"]
+    cap, width = case["capacity"], case["width"]
+    h, n = s["cached"].clamp(min=0).long(), s["new"].clamp(min=0).long()
+    end = n.cumsum(0)
+    held, total = (h + 15) // 16, (h + n + 15) // 16
+    fits = (total <= width) & (end <= cap)
+    need = torch.where(fits, total - held, 0)
+    first = need.cumsum(0) - need
+    ok = fits & (first + need <= s["free"].numel())
+    got = torch.where(ok, need, 0)
+    column = torch.arange(width, device=DEVICE)
+    fresh = (column >= held[:, None]) & (column < (held + got)[:, None])
+    entry = (first[:, None] + column - held[:, None]).clamp(0, s["free"].numel() - 1)
+    table = torch.where(fresh, s["free"][entry], s["table"])
+    t = torch.arange(cap, device=DEVICE)
+    real = t < end[-1]
+    seq = torch.searchsorted(end, t, right=True).clamp(max=case["batch"] - 1)
+    pos = torch.where(real, h[seq] + t - (end - n)[seq], 0)
+    page = table[seq, (pos // 16).clamp(max=width - 1)].long()
+    slots = torch.where(real & ok[seq], page * 16 + pos % 16, -1)
+    cu = torch.cat([torch.zeros_like(end[:1]), end]).clamp(max=cap)
+    return dict(table=table, context=torch.where(ok, h + n, 0).int(), cu=cu.int(),
+                seq=torch.where(real, seq, -1).int(), pos=pos.int(), slots=slots,
+                result=torch.stack([cu[-1], got.sum(), (~ok).sum()]).int())
+
+
+def _norm_rope(s, x, w):
+    """Rows [T, H, d] normalised per head and rotated, in 32 bits."""
+    case, x = s["case"], x.float()
+    if w is not None:
+        x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * w
+    r = case["rot"]
+    if not r:
+        return x
+    cs = s["table"][s["pos"].long()][:, None]
+    c, sn = cs[..., :r // 2], cs[..., r // 2:]
+    y = x.clone()
+    a, b = (x[..., 0:r:2], x[..., 1:r:2]) if case["interleaved"] else (x[..., :r // 2], x[..., r // 2:r])
+    if case["interleaved"]:
+        y[..., 0:r:2], y[..., 1:r:2] = a * c - b * sn, b * c + a * sn
+    else:
+        y[..., :r // 2], y[..., r // 2:r] = a * c - b * sn, b * c + a * sn
+    return y
+
+
+def _round_trip(x, rotate):
+    """fp32 rows -> the rows that their FP4 codes and scales stand for."""
+    d = x.shape[-1]
+    r = _hadamard(d, torch.float32)
+    g = (x @ r if rotate else x).unflatten(-1, (-1, 32))
+    # 2^round(log2(C max)): the significand against sqrt(2)
+    m, e = torch.frexp(g.abs().amax(-1, keepdim=True) * C)
+    scale = torch.exp2((e - 1 + (2 * m >= math.sqrt(2)).int()).float().clamp(-127, 127))
+    y = (g / scale).abs()
+    level = sum(step * (y > at).float() for at, step in ((.25, .5), (1.25, .5), (2.5, 1.), (5., 2.)))
+    level = level + sum(step * (y >= at).float() for at, step in ((.75, .5), (1.75, .5), (3.5, 1.)))
+    g = (torch.copysign(level, g) * scale).flatten(-2)
+    return g @ r if rotate else g
+
+
+def _rows_plain(s):
+    case = s["case"]
+    d, dt = case["head_dim"], DTYPES[case["dtype"]]
+    if case["kind"] == "read":
+        k, v = _stored(case, s["pools"], s["slots"] // PAGE, s["slots"] % PAGE)
+        r = _hadamard(d, torch.float32)
+        return [(k @ r).to(dt), (v @ r if case["rotate_v"] else v).to(dt)]
+    q, k = _norm_rope(s, s["q"], s["w"][0]), _norm_rope(s, s["k"], s["w"][1])
+    if case["kind"] == "rows":
+        return [q.to(dt), k.to(dt)]
+    return [_fp8_query(q, d) if case["fp8"] else q.to(dt), _round_trip(k, True).bfloat16(),
+            _round_trip(s["v"].float(), case["rotate_v"]).bfloat16()]
+
+
+def _attend_plain(s):
+    case = s["case"]
+    hkv, d, w, sinks = case["kv_heads"], case["head_dim"], case["window"], case["sinks"]
+    q8 = _fp8_query(s["q"], d).float()
+    out = torch.empty(s["q"].shape, dtype=torch.float32, device=DEVICE)
+    at = 0
+    for b, (n, m) in enumerate(s["pairs"]):
+        p = torch.arange(n - m, n, device=DEVICE)[:, None]
+        t = torch.arange(n, device=DEVICE)
+        if w:   # only the tokens that some query sees
+            t = t[(t < sinks) | (t > n - m - w)]
+        seen = t <= p
+        if w:
+            seen = seen & ((t > p - w) | (t < sinks))
+        k, v = _stored(case, s["pools"], s["table"][b].long()[t // PAGE], t % PAGE)    # [n, Hkv, d]
+        for h in range(hkv):
+            qh = q8[at:at + m].unflatten(1, (hkv, -1))[:, h].transpose(0, 1)            # [G, m, d]
+            sc = (qh @ k[:, h].t()) * d ** -0.5
+            sc = sc.masked_fill(~seen, -math.inf)
+            e = torch.exp(sc - sc.amax(-1, keepdim=True))
+            o = (e @ v[:, h]) / e.sum(-1, keepdim=True)
+            out[at:at + m].unflatten(1, (hkv, -1))[:, h] = o.transpose(0, 1)
+        at += m
+    return (out @ _hadamard(d, torch.float32) if case["rotate_v"] else out).bfloat16()
+
+
+def _run_own(s):
+    from paper_2606_20474_amd import uq
+    case = s["case"]
+    kind = case["kind"]
+    if kind == "plan":
+        p = uq.plan_tokens(s["cached"], s["new"], s["free"], s["table"], s["plan"])
+        return dict(table=s["table"], context=p.context_lens, cu=p.cu_seqlens, seq=p.seq_ids, pos=p.positions,
+                    slots=p.slots, result=p.result)
+    if kind == "read":
+        return list(uq.read_kv(s["desc"], s["slots"], *s["pools"], k_out=s["out"][0], v_out=s["out"][1]))
+    if kind == "rows":
+        return list(uq.norm_rope(s["spec"], s["q"], s["k"], q_out=s["q_out"], k_out=s["out"][0]))
+    if kind == "write":
+        q = uq.norm_rope_write(s["desc"], s["spec"], s["q"], s["k"], s["v"], s["slots"], *s["pools"], q_out=s["q_out"])
+        k, v = uq.read_kv(s["desc"], s["slots"], *s["pools"], k_out=s["out"][0], v_out=s["out"][1])
+        return [q.view(torch.float8_e4m3fn) if case["fp8"] else q, k, v]
+    if kind == "extend":
+        return uq.extend_attention(s["desc"], s["q"], s["cu"], *s["pools"], s["table"], s["lens"], s["bound"],
+                                   window=case["window"], sinks=case["sinks"], workspace=s["workspace"], out=s["out"])
+    return uq.decode_window(s["desc"], s["q"], *s["pools"], s["table"], s["lens"], s["bound"], case["window"],
+                            sinks=case["sinks"], workspace=s["workspace"], out=s["out"])
+
+
+def run(s):
+    if own:
+        return _run_own(s)
+    kind = s["case"]["kind"]
+    return _plan_plain(s) if kind == "plan" else _attend_plain(s) if kind in ("extend", "window") else _rows_plain(s)
+
+
+# --------------------------------------------------------------------------
+# Work, and the results in 64 bits
+
+
+def _seen(n, m, w, sinks):
+    """(distinct tokens that m queries at the end of n tokens see, query-token pairs)."""
+    if not w:
+        return n, m * (n - m) + m * (m + 1) // 2
+    low = max(0, n - m - w + 1)
+    p = np.arange(n - m, n)
+    kept = np.minimum(sinks, np.maximum(p + 1 - w, 0))
+    return n - low + min(sinks, low), int((np.minimum(p + 1, w) + kept).sum())
+
+
+def work(case):
+    if case["kind"] == "plan":
+        pairs = _lengths(case)
+        pages = sum(-(-(h + n) // PAGE) - -(-h // PAGE) for h, n in pairs)
+        return {"bytes": case["batch"] * 16 + 16 * case["capacity"] + 8 * pages, "flops": 0}
+    d, hkv, hq = case["head_dim"], case["kv_heads"], case["q_heads"]
+    item = 4 if case["dtype"] == "float32" else 2
+    stored = hkv * 17 * d // 16
+    if case["kind"] == "read":
+        return {"bytes": case["tokens"] * (stored + 2 * hkv * d * item + 8), "flops": 0}
+    if case["kind"] in ("rows", "write"):
+        t, q_item = case["tokens"], 1 if case["fp8"] else item
+        ops = (4 if case["norm"] else 0) + (3 if case["rot"] else 0)
+        n = t * (hq + hkv) * d * item + t * hq * d * q_item + 4 * t
+        if case["kind"] == "rows":
+            return {"bytes": n + t * hkv * d * item, "flops": t * (hq + hkv) * d * ops}
+        return {"bytes": n + t * hkv * d * item + 16 * t + 2 * t * stored + t * 2 * hkv * d * 2,
+                "flops": t * (hq + hkv) * d * ops + t * (hq + 4 * hkv) * d * int(math.log2(d))}
+    seen = [_seen(n, m if case["kind"] == "extend" else 1, case["window"], case["sinks"]) for n, m in _lengths(case)]
+    rows = sum(m if case["kind"] == "extend" else 1 for _, m in _lengths(case)) * hq * d
+    return {"bytes": sum(n for n, _ in seen) * stored + rows * (item + 2), "flops": 4 * d * hq * sum(n for _, n in seen)}
+
+
+def _walsh(x):
+    """R x of the last dimension in 64 bits, by pairs."""
+    d, shape, h = x.shape[-1], x.shape, 1
+    x = x.double()
+    while h < d:
+        y = x.reshape(-1, d // (2 * h), 2, h)
+        x = torch.stack([y[:, :, 0] + y[:, :, 1], y[:, :, 0] - y[:, :, 1]], 2)
+        h *= 2
+    return x.reshape(shape) / math.sqrt(d)
+
+
+def _grid_round(x, mantissa, emin, top):
+    """Nearest value (ties to even) with `mantissa` fraction bits, least exponent emin, largest magnitude top."""
+    e = torch.floor(torch.log2(x.abs().clamp(min=2.0 ** (emin - mantissa - 1))))
+    e = torch.where(torch.exp2(e) > x.abs(), e - 1, e)      # log2 may round up to the next whole number
+    step = torch.exp2(e.clamp(min=emin) - mantissa)
+    return (torch.round(x / step) * step).clamp(-top, top)
+
+
+def _tile_values(case, codes, scales, pages):
+    """K and V in 64 bits, as stored, of whole pages: [tokens, Hkv, d]."""
+    h, d = case["kv_heads"], case["head_dim"]
+    c = codes.view(-1, h, 2, 8 * d)[pages].long()
+    nib = torch.stack([c & 15, c >> 4], -1).flatten(-2)                            # [pages, Hkv, 2, 16 d]
+    e, m = nib >> 1 & 3, (nib & 1).double()
+    val = torch.where(e == 0, m / 2, (1 + m / 2) * torch.exp2((e - 1).double())) * (1 - 2 * (nib >> 3)).double()
+    sc = torch.exp2(scales.view(-1, h, 2, d // 32, PAGE)[pages].double() - 127)     # [pages, Hkv, 2, d/32, 16]
+    n = len(pages)
+    k = val[:, :, 0].reshape(n, h, d // 32, PAGE, 32) * sc[:, :, 0, :, :, None]
+    v = val[:, :, 1].reshape(n, h, 4, d // 8, 4, 8).permute(0, 1, 2, 4, 3, 5).reshape(n, h, PAGE, d // 32, 32)
+    v = v * sc[:, :, 1].transpose(-1, -2)[..., None]
+    return (k.permute(0, 3, 1, 2, 4).reshape(n * PAGE, h, d), v.permute(0, 2, 1, 3, 4).reshape(n * PAGE, h, d))
+
+
+def _exact_rows(case, seed):
+    s = _prepare_rows(case, seed)
+    d, t = case["head_dim"], case["tokens"]
+    if case["kind"] == "read":
+        k, v = [], []
+        pages, inverse = torch.unique(s["slots"] // PAGE, return_inverse=True)
+        at = inverse * PAGE + s["slots"] % PAGE
+        k, v = _tile_values(case, *s["pools"], pages)
+        return [_walsh(k[at]), _walsh(v[at]) if case["rotate_v"] else v[at]]
+
+    def head(x, w):
+        x = x.double()
+        if w is not None:
+            x = x / torch.sqrt((x * x).sum(-1, keepdim=True) / d + EPS) * w.double()
+        r = case["rot"] // 2
+        if r:
+            z = torch.view_as_complex(x[..., :2 * r].reshape(*x.shape[:-1], r, 2) if case["interleaved"] else
+                                      torch.stack([x[..., :r], x[..., r:2 * r]], -1))
+            cs = s["table"].double()[s["pos"].long()]
+            z = torch.view_as_real(z * torch.complex(cs[:, :r], cs[:, r:])[:, None])
+            z = z.flatten(-2) if case["interleaved"] else z.transpose(-1, -2).flatten(-2)
+            x = torch.cat([z, x[..., 2 * r:]], -1)
+        return x
+
+    def code(x, rotate):
+        x = _walsh(x) if rotate else x.double()
+        g = x.reshape(t, -1, d // 32, 32)
+        top = g.abs().max(-1, keepdim=True).values * float(np.float32(C))
+        e = torch.floor(torch.log2(top.clamp(min=2.0 ** -140)) + 0.5).clamp(-127, 127)
+        y = (_grid_round(g / torch.exp2(e), 1, 0, 6.0) * torch.exp2(e)).reshape(x.shape)
+        return _walsh(y) if rotate else y
+
+    q, k = head(s["q"], s["w"][0]), head(s["k"], s["w"][1])
+    if case["kind"] == "rows":
+        return [q, k]
+    return [_grid_round(_walsh(q), 3, -6, 448.0) if case["fp8"] else q, code(k, True), code(s["v"], case["rotate_v"])]
+
+
+def _exact_attend(case, seed):
+    s = _prepare_attend(case, seed)
+    d, hkv, w, sinks = case["head_dim"], case["kv_heads"], case["window"], case["sinks"]
+    q = _grid_round(_walsh(s["q"]), 3, -6, 448.0)
+    out, at = torch.empty(s["q"].shape, dtype=torch.float64, device=DEVICE), 0
+    for b, (n, m) in enumerate(s["pairs"]):
+        k, v = _tile_values(case, *s["pools"], s["table"][b, :-(-n // PAGE)].long())
+        for i in range(0, m, 1024):                       # query rows, so that a block's scores fit
+            p = torch.arange(n - m + i, min(n - m + i + 1024, n), device=DEVICE)
+            lo = max(0, int(p[0]) - w + 1) if w else 0    # first token that a window of these rows reaches
+            keep = torch.cat([torch.arange(min(sinks, lo)), torch.arange(lo, int(p[-1]) + 1)]).to(DEVICE)
+            hidden = keep[None] > p[:, None]
+            if w:
+                hidden |= (keep[None] <= p[:, None] - w) & (keep[None] >= sinks)
+            for h in range(hkv):
+                g = s["q"].shape[1] // hkv
+                qh = q[at + i:at + i + len(p), h * g:(h + 1) * g].reshape(-1, d)
+                sc = (qh @ k[keep, h].t().contiguous() / math.sqrt(d)).reshape(len(p), g, -1)
+                pr = torch.softmax(sc.masked_fill_(hidden[:, None], -math.inf), -1)
+                out[at + i:at + i + len(p), h * g:(h + 1) * g] = (pr.flatten(0, 1) @ v[keep, h]).reshape(len(p), g, d)
+        at += m
+    return _walsh(out) if case["rotate_v"] else out
+
+
+def exact(case, seed):
+    if case["kind"] == "plan":
+        return None   # whole numbers
+    return _exact_attend(case, seed) if case["kind"] in ("extend", "window") else _exact_rows(case, seed)
