@@ -323,7 +323,7 @@ def _plan_plain(s):
     fits = (total <= width) & (end <= cap)
     need = torch.where(fits, total - held, 0)
     first = need.cumsum(0) - need
-    ok = fits & (first + need <= s["free"].numel())
+    ok = fits & ((need == 0) | (first + need <= s["free"].numel()))
     got = torch.where(ok, need, 0)
     column = torch.arange(width, device=DEVICE)
     fresh = (column >= held[:, None]) & (column < (held + got)[:, None])
