@@ -568,6 +568,205 @@ uq_status uq_decode_attention_noalloc(const uq_cache_desc *desc, const void *q, 
                                       int32_t partition_tokens, void *out, uq_dtype out_dtype, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Around the cache: what a serving step needs before and beside decode
+ * attention.  uq_plan_tokens turns the request lengths of a step into pages,
+ * slots and positions; uq_norm_rope(_write) takes the rows of the QKV
+ * projection to prepared queries and cache entries; uq_read_kv gives stored
+ * tokens back as rows; uq_extend_attention is attention for several new
+ * queries per sequence (prompt chunks, drafted tokens), uq_decode_window for
+ * one query per sequence under a sliding window.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * uq_plan_tokens -- page assignment and slot maps of one step of a ragged
+ * batch, made on the device from its lengths.
+ *   cached_lens   : int32 [batch], tokens of each sequence that are in the
+ *                   cache already; their pages are the first
+ *                   ceil(cached / 16) entries of its page-table row.
+ *                   Negative counts as 0.
+ *   new_lens      : int32 [batch], tokens this step appends (0 allowed;
+ *                   negative counts as 0).  The step's token rows hold the
+ *                   sequences one after another.
+ *   free_pages    : int32 [num_free_pages], pages no sequence holds (may be
+ *                   NULL when num_free_pages == 0).
+ *   page_table    : int32 [batch][max_pages_per_seq], read and written: the
+ *                   entries of the new pages, taken from the front of
+ *                   free_pages in sequence order.
+ *   num_tokens    : rows the step has room for; the token arrays' length.
+ * Outputs (device):
+ *   context_lens  : int32 [batch], cached + new; 0 for a refused sequence.
+ *   cu_seqlens    : int32 [batch + 1], first token row of each sequence, then
+ *                   the number of rows in use (at most num_tokens).
+ *   seq_ids, positions : int32 [num_tokens], each row's sequence and
+ *                   position; -1 and 0 for rows behind the last sequence.
+ *   slots         : int64 [num_tokens], physical slot page * 16 + offset
+ *                   (slot_mapping of uq_quantize_kv); -1 for rows behind the
+ *                   last sequence and those of refused sequences.
+ *   result        : int32 [3]: rows in use, pages taken, sequences refused.
+ * A sequence is refused (its row of the page table stays as it was, its
+ * tokens get no slots) when cached + new does not fit its page-table row,
+ * when its token rows end beyond num_tokens, or when it needs new pages and the
+ * free ones run out: the pages it and the sequences before it need (those
+ * refused for the first two reasons apart) exceed num_free_pages.  The caller
+ * drops the first result[1] entries of free_pages.
+ * No output may overlap an input other than page_table.  batch == 0 is valid.
+ * Errors: INVALID_ARGUMENT for null pointers, negative batch, num_free_pages or
+ * num_tokens, max_pages_per_seq < 1; UNSUPPORTED for batch > 4096, num_tokens
+ * or num_free_pages >= 2^29, or max_pages_per_seq >= 2^27.
+ */
+uq_status uq_plan_tokens(int32_t batch, const int32_t *cached_lens, const int32_t *new_lens,
+                         const int32_t *free_pages, int32_t num_free_pages, int32_t *page_table,
+                         int32_t max_pages_per_seq, int64_t num_tokens, int32_t *context_lens, int32_t *cu_seqlens,
+                         int32_t *seq_ids, int32_t *positions, int64_t *slots, int32_t *result, void *stream);
+
+/* Per-head norm and position rotation of queries and keys. */
+typedef struct uq_norm_rope_desc {
+    const float *q_weight;      /* [head_dim] (device, 16-byte aligned), or NULL: queries are not normalised */
+    const float *k_weight;      /* the same for the keys */
+    float eps;                  /* finite, >= 0; added to the mean square */
+    const int32_t *positions;   /* [num_tokens] (device); NULL when rot_dim == 0 */
+    const float *cos_sin;       /* [max_position][rot_dim] (device, 16-byte aligned): rot_dim / 2 cosines, then
+                                   the sines of the same angles; NULL when rot_dim == 0 */
+    int32_t max_position;       /* rows of cos_sin, >= 1 (unless rot_dim == 0) */
+    int32_t rot_dim;            /* leading channels that are rotated: 0, 16, 32 or a multiple of 64 up to
+                                   head_dim */
+    int32_t interleaved;        /* 0: channel c pairs with c + rot_dim / 2; 1: channels 2 i and 2 i + 1 */
+} uq_norm_rope_desc;
+
+/*
+ * uq_norm_rope -- for every token and head of q and k, in fp32:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight   (with a weight, else y = x),
+ *   (a, b) <- (a cos - b sin, b cos + a sin)  for each pair of the rotated
+ *                                             channels, angle of the token's position.
+ *   q, k          : [num_tokens][heads][head_dim] of in_dtype (F32, BF16 or
+ *                   F16), 16-byte aligned; token t starts at element
+ *                   t * stride (a multiple of 16 bytes, at least heads *
+ *                   head_dim), heads and channels are contiguous.
+ *   q_out, k_out  : the rows, out_dtype F32, BF16 or F16 (rounded once to
+ *                   nearest), contiguous, 16-byte aligned.  q_out may be q and
+ *                   k_out k where q (k) is contiguous and of out_dtype;
+ *                   other overlaps are not allowed.
+ *   k and k_out may both be NULL (num_kv_heads 0): queries alone.
+ * Positions outside [0, max_position) are clamped to it.  A row of zeros
+ * needs eps > 0 (else it is 0 * inf); squares and their sum stay in fp32
+ * range.  head_dim: 64, 128 or 256.  num_tokens == 0 is a no-op.
+ * Errors: INVALID_ARGUMENT for null or misaligned pointers, negative sizes,
+ * num_q_heads < 1, a stride too small or misaligned, a bad eps or max_position;
+ * UNSUPPORTED for other head_dim, rot_dim or dtypes, or 2^31 rows or more.
+ */
+uq_status uq_norm_rope(const uq_norm_rope_desc *spec, int32_t head_dim, const void *q, int64_t q_stride,
+                       int32_t num_q_heads, const void *k, int64_t k_stride, int32_t num_kv_heads,
+                       uq_dtype in_dtype, int64_t num_tokens, void *q_out, void *k_out, uq_dtype out_dtype,
+                       void *stream);
+
+/*
+ * uq_norm_rope_write -- the same pass with the cache behind it, one launch:
+ * queries as above, or (q_out_dtype FP8_E4M3) rotated and cast as
+ * uq_prepare_query does; keys normed, rotated by position and stored with the
+ * values as uq_quantize_kv stores fp32 rows: the cache bytes are those of
+ * uq_norm_rope with F32 output followed by uq_quantize_kv (V as it is).
+ *   q             : as above, q_stride; k, v as above with kv_stride, all of
+ *                   in_dtype.
+ *   q_out         : [num_tokens][num_q_heads][head_dim] F32, BF16, F16 or
+ *                   FP8_E4M3 (bytes), 16-byte aligned.  Padding tokens get
+ *                   their queries too.
+ *   page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes,
+ *   kv_scales     : as in uq_quantize_kv.
+ * Errors: those of uq_norm_rope and uq_quantize_kv.
+ */
+uq_status uq_norm_rope_write(const uq_cache_desc *desc, const uq_norm_rope_desc *spec, const void *q,
+                             int64_t q_stride, int32_t num_q_heads, const void *k, const void *v, int64_t kv_stride,
+                             uq_dtype in_dtype, int64_t num_tokens, void *q_out, uq_dtype q_out_dtype,
+                             const int32_t *page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                             const int64_t *slot_mapping, uint8_t *kv_codes, uint8_t *kv_scales, void *stream);
+
+/*
+ * uq_read_kv -- stored tokens as rows, the inverse of uq_quantize_kv: the
+ * values the codes and scales stand for, K rotated back, V with rotate_v, in
+ * fp32, rounded once to out_dtype (F32, BF16 or F16).
+ *   slot_mapping, page_table : as in uq_quantize_kv; a token whose slot is
+ *                   skipped there leaves its rows as they were.
+ *   k_out, v_out  : [num_tokens][num_kv_heads][head_dim], contiguous, 16-byte
+ *                   aligned; either may be NULL.
+ * Errors: as uq_quantize_kv; INVALID_ARGUMENT when both outputs are NULL.
+ */
+uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const uint8_t *kv_scales,
+                     const int32_t *page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                     const int64_t *slot_mapping, int64_t num_tokens, void *k_out, void *v_out, uq_dtype out_dtype,
+                     void *stream);
+
+/*
+ * uq_extend_attention -- attention of the step's new tokens over the FP4
+ * cache, which holds them already (uq_quantize_kv or uq_norm_rope_write
+ * first).  Sequence b's queries are the rows cu_seqlens[b] .. cu_seqlens[b + 1]
+ * - 1; they are the last ones of its context: with m of them and context
+ * length n, query i stands at position n - m + i and sees the tokens t <= its
+ * position and, with a window, only t > position - window or t < sinks.
+ *   q             : [num_tokens][num_q_heads][head_dim] F32, BF16 or F16
+ *                   (rotated and cast to FP8 inside the call), or FP8_E4M3
+ *                   bytes prepared by uq_norm_rope_write or uq_prepare_query;
+ *                   token t starts at element t * q_stride (a multiple of 16
+ *                   bytes); 16-byte aligned.
+ *   cu_seqlens    : int32 [batch + 1] (device), ascending, 0 first, at most
+ *                   num_tokens (read clamped to 0 .. num_tokens).
+ *   context_lens  : int32 [batch] (device), as in uq_decode_attention;
+ *                   lengths above max_context are clamped to it.
+ *   window        : 0: every token up to the query's own is visible; else the
+ *                   last `window` of them, the query's own included.
+ *   sinks         : first tokens that stay visible; used with a window only.
+ *   workspace     : >= uq_extend_workspace_bytes(...), 16-byte aligned (may be
+ *                   NULL when that is 0); no initial contents required.  Calls
+ *                   that share one must not run concurrently.
+ *   out           : [num_tokens][num_q_heads][head_dim] F32 or BF16,
+ *                   contiguous, 16-byte aligned.  A query that sees nothing (a
+ *                   position below 0: more queries than context) gives 0.
+ *                   Rows behind cu_seqlens[batch] are left as they were.
+ * QK^T is that of uq_decode_attention (FP8 query, FP4 keys); the softmax
+ * runs in fp32; its weights enter PV rounded once to BF16 (relative error up
+ * to 2^-8 / 2 each, while uq_decode_attention carries 16 bits of them).
+ * A long context with few queries is split over blocks and joined by a second
+ * launch; the bits of a row depend on num_tokens, batch and max_context then.
+ * num_tokens == 0 or batch == 0 is a no-op.
+ * Errors: as uq_decode_attention, plus INVALID_ARGUMENT for a null
+ * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for
+ * num_tokens >= 2^26 or more blocks than a grid holds.
+ */
+size_t uq_extend_workspace_bytes(const uq_cache_desc *desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
+                                 int32_t max_context, int32_t window, int32_t sinks);
+uq_status uq_extend_attention(const uq_cache_desc *desc, const void *q, uq_dtype q_dtype, int64_t q_stride,
+                              int64_t num_tokens, const int32_t *cu_seqlens, int32_t batch, int32_t num_q_heads,
+                              const uint8_t *kv_codes, const uint8_t *kv_scales, const int32_t *page_table,
+                              int32_t max_pages_per_seq, const int32_t *context_lens, int32_t max_context,
+                              int32_t window, int32_t sinks, float softmax_scale, void *workspace,
+                              size_t workspace_bytes, void *out, uq_dtype out_dtype, void *stream);
+
+/*
+ * uq_decode_window -- uq_decode_attention (k_new == v_new == NULL) or
+ * uq_decode_step (both given) where the query sees only the last `window`
+ * tokens of its context (its own included) and the first `sinks`.  Pages
+ * without a visible token are not read: their page-table entries and contents
+ * may be anything, so an engine can hand them back.  The tokens of the pages
+ * that are read need not all have been written, as long as the visible ones
+ * were.
+ *   window        : >= 1; sinks: >= 0.
+ *   partition_tokens : as in uq_decode_attention, counted over the visible
+ *                   pages; 0 for the default.
+ *   workspace     : >= uq_decode_window_workspace_bytes(...).
+ * Every other argument, the output and the errors are those of uq_decode_step
+ * (the step: head_dim 128), plus INVALID_ARGUMENT for a bad window or sinks or only one of
+ * k_new, v_new.
+ */
+size_t uq_decode_window_workspace_bytes(const uq_cache_desc *desc, int32_t batch, int32_t num_q_heads,
+                                        int32_t max_context, int32_t window, int32_t sinks,
+                                        int32_t partition_tokens);
+uq_status uq_decode_window(const uq_cache_desc *desc, const void *q, uq_dtype q_dtype, const void *k_new,
+                           const void *v_new, uq_dtype new_dtype, int32_t batch, int32_t num_q_heads,
+                           uint8_t *kv_codes, uint8_t *kv_scales, const int32_t *page_table,
+                           int32_t max_pages_per_seq, const int32_t *context_lens, int32_t max_context,
+                           int32_t window, int32_t sinks, float softmax_scale, int32_t partition_tokens,
+                           void *workspace, size_t workspace_bytes, void *out, uq_dtype out_dtype, void *stream);
+
+/* ------------------------------------------------------------------------
  * Measurement probes (diagnostics, not part of the method; section
  * "Kernel-Level Roofline Analysis" measures against the HBM roof, and these
  * give the share of it this GPU actually delivers to the access patterns of

@@ -218,6 +218,9 @@ uq_status make_decode_params(const uq_cache_desc* desc, const void* q, uq_dtype 
     p.merge_by_head = 0;
     p.long_blocks = 0;
     p.probe_sink = nullptr;
+    p.window = 0;
+    p.sinks = 0;
+    p.context_bound = max_context;
     return UQ_OK;
 }
 
@@ -427,22 +430,24 @@ const char* uq_status_string(uq_status s) {
 
 int32_t uq_version(void) { return 100; }
 
-uq_status uq_quantize_kv(const uq_cache_desc* desc, const void* k, const void* v, uq_dtype in_dtype,
-                         int64_t num_tokens, int64_t token_stride, const int32_t* page_table, int32_t num_seqs,
-                         int32_t max_pages_per_seq, const int64_t* slot_mapping, uint8_t* kv_codes,
-                         uint8_t* kv_scales, void* stream) {
-    uq_status s = check_desc(desc);
-    if (s != UQ_OK) return s;
-    if (in_dtype != UQ_F32 && in_dtype != UQ_BF16 && in_dtype != UQ_F16) return UQ_ERR_UNSUPPORTED;
-    if (num_tokens < 0) return UQ_ERR_INVALID_ARGUMENT;
-    if (k == nullptr || v == nullptr || slot_mapping == nullptr || kv_codes == nullptr || kv_scales == nullptr)
-        return UQ_ERR_INVALID_ARGUMENT;
-    if (token_stride < int64_t(desc->num_kv_heads) * desc->head_dim) return UQ_ERR_INVALID_ARGUMENT;
-    const int64_t vec_elems = in_dtype == UQ_F32 ? 4 : 8;   // one 16-byte load
-    if (token_stride % vec_elems != 0 || !aligned16(k) || !aligned16(v)) return UQ_ERR_INVALID_ARGUMENT;
+// The checks and parameters uq_quantize_kv shares with the calls that use its
+// slots and pools.
+static uq_status check_slots(const int32_t* page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                             const int64_t* slot_mapping, const uint8_t* kv_codes, const uint8_t* kv_scales) {
+    if (slot_mapping == nullptr || kv_codes == nullptr || kv_scales == nullptr) return UQ_ERR_INVALID_ARGUMENT;
     if (!aligned16(kv_codes) || !aligned16(kv_scales)) return UQ_ERR_INVALID_ARGUMENT;
     if (page_table != nullptr && (max_pages_per_seq < 1 || num_seqs < 1)) return UQ_ERR_INVALID_ARGUMENT;
-    if (num_tokens == 0) return UQ_OK;
+    return UQ_OK;
+}
+static bool row_dtype(uq_dtype t) { return t == UQ_F32 || t == UQ_BF16 || t == UQ_F16; }
+// Rows of `heads` vectors, token t at element t * stride: 16-byte loads.
+static bool rows_ok(const void* x, int64_t stride, int64_t heads, int32_t head_dim, uq_dtype dtype) {
+    return x != nullptr && aligned16(x) && stride >= heads * head_dim && stride % (dtype == UQ_F32 ? 4 : 8) == 0;
+}
+static uq::QuantizeParams slot_params(const uq_cache_desc* desc, const void* k, const void* v, int64_t num_tokens,
+                                      int64_t token_stride, const int32_t* page_table, int32_t num_seqs,
+                                      int32_t max_pages_per_seq, const int64_t* slot_mapping, uint8_t* kv_codes,
+                                      uint8_t* kv_scales) {
     uq::QuantizeParams p;
     p.k = k;
     p.v = v;
@@ -459,7 +464,147 @@ uq_status uq_quantize_kv(const uq_cache_desc* desc, const void* k, const void* v
     p.codes = kv_codes;
     p.scales = kv_scales;
     p.head_dim = desc->head_dim;
+    return p;
+}
+
+uq_status uq_quantize_kv(const uq_cache_desc* desc, const void* k, const void* v, uq_dtype in_dtype,
+                         int64_t num_tokens, int64_t token_stride, const int32_t* page_table, int32_t num_seqs,
+                         int32_t max_pages_per_seq, const int64_t* slot_mapping, uint8_t* kv_codes,
+                         uint8_t* kv_scales, void* stream) {
+    uq_status s = check_desc(desc);
+    if (s != UQ_OK) return s;
+    if (!row_dtype(in_dtype)) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (!rows_ok(k, token_stride, desc->num_kv_heads, desc->head_dim, in_dtype) ||
+        !rows_ok(v, token_stride, desc->num_kv_heads, desc->head_dim, in_dtype))
+        return UQ_ERR_INVALID_ARGUMENT;
+    s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
+    if (s != UQ_OK || num_tokens == 0) return s;
+    const uq::QuantizeParams p = slot_params(desc, k, v, num_tokens, token_stride, page_table, num_seqs,
+                                             max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     return from_hip(uq::launch_quantize_kv(p, int(in_dtype), static_cast<hipStream_t>(stream)));
+}
+
+uq_status uq_plan_tokens(int32_t batch, const int32_t* cached_lens, const int32_t* new_lens,
+                         const int32_t* free_pages, int32_t num_free_pages, int32_t* page_table,
+                         int32_t max_pages_per_seq, int64_t num_tokens, int32_t* context_lens, int32_t* cu_seqlens,
+                         int32_t* seq_ids, int32_t* positions, int64_t* slots, int32_t* result, void* stream) {
+    if (batch < 0 || num_free_pages < 0 || num_tokens < 0 || max_pages_per_seq < 1) return UQ_ERR_INVALID_ARGUMENT;
+    if (batch > uq::kPlanTokensBatch || num_tokens >= (int64_t(1) << 29) || num_free_pages >= (1 << 29) ||
+        max_pages_per_seq >= (1 << 27))
+        return UQ_ERR_UNSUPPORTED;
+    if (batch > 0 && (cached_lens == nullptr || new_lens == nullptr || page_table == nullptr || context_lens == nullptr))
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (cu_seqlens == nullptr || result == nullptr || (num_free_pages > 0 && free_pages == nullptr))
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens > 0 && (seq_ids == nullptr || positions == nullptr || slots == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
+    const uq::PlanParams p{batch,        cached_lens,  new_lens,   free_pages, num_free_pages, page_table, max_pages_per_seq,
+                           num_tokens,   context_lens, cu_seqlens, seq_ids,    positions,      slots,      result};
+    return from_hip(uq::launch_plan_tokens(p, static_cast<hipStream_t>(stream)));
+}
+
+// The norm and rotation part of the parameter block; every argument check of
+// the spec, q and the output types.
+static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
+                                 int32_t num_q_heads, uq_dtype in_dtype, int64_t num_tokens, void* q_out,
+                                 uq_dtype out_dtype, uq::NormRopeParams& p) {
+    if (spec == nullptr || num_tokens < 0 || num_q_heads < 1 || spec->rot_dim < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return UQ_ERR_UNSUPPORTED;
+    if (!row_dtype(in_dtype)) return UQ_ERR_UNSUPPORTED;
+    const int32_t rot = spec->rot_dim;
+    if (rot > head_dim || (rot % 64 != 0 && rot != 16 && rot != 32)) return UQ_ERR_UNSUPPORTED;
+    if (!(isfinite(spec->eps) && spec->eps >= 0.0f)) return UQ_ERR_INVALID_ARGUMENT;
+    if (!aligned16(spec->q_weight) || !aligned16(spec->k_weight)) return UQ_ERR_INVALID_ARGUMENT;
+    if (rot > 0 && ((spec->positions == nullptr && num_tokens > 0) || spec->cos_sin == nullptr || !aligned16(spec->cos_sin) ||
+                    spec->max_position < 1))
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens > 0 && (!rows_ok(q, q_stride, num_q_heads, head_dim, in_dtype) || q_out == nullptr || !aligned16(q_out)))
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens >= (int64_t(1) << 31) / num_q_heads) return UQ_ERR_UNSUPPORTED;   // vectors are numbered in 32 bits
+    p.q = q;
+    p.k = nullptr;
+    p.q_stride = q_stride;
+    p.k_stride = 0;
+    p.num_q_heads = num_q_heads;
+    p.num_kv_heads = 1;
+    p.num_tokens = num_tokens;
+    p.q_weight = spec->q_weight;
+    p.k_weight = spec->k_weight;
+    p.eps = spec->eps;
+    p.positions = spec->positions;
+    p.cos_sin = spec->cos_sin;
+    p.max_position = spec->max_position;
+    p.rot = rot;
+    p.interleaved = spec->interleaved != 0;
+    p.q_out = q_out;
+    p.k_out = nullptr;
+    p.out_dtype = int32_t(out_dtype);
+    p.q_blocks = 0;
+    return UQ_OK;
+}
+
+uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
+                       int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
+                       uq_dtype in_dtype, int64_t num_tokens, void* q_out, void* k_out, uq_dtype out_dtype,
+                       void* stream) {
+    uq::NormRopeParams p;
+    uq_status s = norm_rope_setup(spec, head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, out_dtype, p);
+    if (s != UQ_OK) return s;
+    if (!row_dtype(out_dtype)) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens == 0) return num_kv_heads < 0 ? UQ_ERR_INVALID_ARGUMENT : UQ_OK;
+    if ((k == nullptr) != (k_out == nullptr) || (k == nullptr) != (num_kv_heads == 0) || num_kv_heads < 0)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (k != nullptr) {
+        if (!rows_ok(k, k_stride, num_kv_heads, head_dim, in_dtype) || !aligned16(k_out)) return UQ_ERR_INVALID_ARGUMENT;
+        if (num_tokens >= (int64_t(1) << 31) / (int64_t(num_q_heads) + num_kv_heads)) return UQ_ERR_UNSUPPORTED;
+    }
+    p.k = k;
+    p.k_stride = k_stride;
+    p.num_kv_heads = num_kv_heads;
+    p.k_out = k_out;
+    return from_hip(uq::launch_norm_rope(p, nullptr, head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));
+}
+
+uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc* spec, const void* q,
+                             int64_t q_stride, int32_t num_q_heads, const void* k, const void* v, int64_t kv_stride,
+                             uq_dtype in_dtype, int64_t num_tokens, void* q_out, uq_dtype q_out_dtype,
+                             const int32_t* page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                             const int64_t* slot_mapping, uint8_t* kv_codes, uint8_t* kv_scales, void* stream) {
+    uq_status s = check_desc(desc);
+    if (s != UQ_OK) return s;
+    uq::NormRopeParams p;
+    s = norm_rope_setup(spec, desc->head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, q_out_dtype, p);
+    if (s != UQ_OK) return s;
+    if (!row_dtype(q_out_dtype) && q_out_dtype != UQ_FP8_E4M3) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens == 0) return UQ_OK;
+    if (!rows_ok(k, kv_stride, desc->num_kv_heads, desc->head_dim, in_dtype) ||
+        !rows_ok(v, kv_stride, desc->num_kv_heads, desc->head_dim, in_dtype))
+        return UQ_ERR_INVALID_ARGUMENT;
+    s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
+    if (s != UQ_OK) return s;
+    if (num_tokens >= (int64_t(1) << 31) / (int64_t(num_q_heads) + desc->num_kv_heads) - 16) return UQ_ERR_UNSUPPORTED;
+    const uq::QuantizeParams c = slot_params(desc, k, v, num_tokens, kv_stride, page_table, num_seqs,
+                                             max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
+    return from_hip(uq::launch_norm_rope(p, &c, desc->head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));
+}
+
+uq_status uq_read_kv(const uq_cache_desc* desc, const uint8_t* kv_codes, const uint8_t* kv_scales,
+                     const int32_t* page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                     const int64_t* slot_mapping, int64_t num_tokens, void* k_out, void* v_out, uq_dtype out_dtype,
+                     void* stream) {
+    uq_status s = check_desc(desc);
+    if (s != UQ_OK) return s;
+    if (!row_dtype(out_dtype)) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens == 0) return UQ_OK;
+    if (k_out == nullptr && v_out == nullptr) return UQ_ERR_INVALID_ARGUMENT;
+    if (!aligned16(k_out) || !aligned16(v_out)) return UQ_ERR_INVALID_ARGUMENT;
+    s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
+    if (s != UQ_OK) return s;
+    const uq::QuantizeParams c = slot_params(desc, nullptr, nullptr, num_tokens, 0, page_table, num_seqs,
+                                             max_pages_per_seq, slot_mapping, const_cast<uint8_t*>(kv_codes),
+                                             const_cast<uint8_t*>(kv_scales));
+    return from_hip(uq::launch_read_kv(c, k_out, v_out, int(out_dtype), static_cast<hipStream_t>(stream)));
 }
 
 uq_status uq_prepare_query(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t rows, uint8_t* q_fp8,
@@ -550,6 +695,147 @@ uq_status uq_decode_attention(const uq_cache_desc* desc, const void* q, uq_dtype
                                max_pages_per_seq, context_lens, max_context, softmax_scale, partition_tokens, workspace,
                                workspace_bytes, out, out_dtype, p);
     if (s != UQ_OK) return s;
+    s = from_hip(uq::launch_decode_partials(p, static_cast<hipStream_t>(stream)));
+    if (s != UQ_OK) return s;
+    return from_hip(uq::launch_decode_merge(p, static_cast<hipStream_t>(stream)));
+}
+
+// How a call of uq_extend_attention is cut: the row blocks per KV head the batch
+// can have, and the blocks that share a row block's tiles.  Two blocks per CU are
+// wanted; a split has at least 4 tiles of 64 tokens of the longest walk.
+struct ExtendShape {
+    int64_t row_blocks;
+    int32_t splits;
+    size_t workspace;
+};
+static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
+                              int32_t max_context, int32_t window, int32_t sinks, ExtendShape& e) {
+    uq_status s = check_desc(desc);
+    if (s != UQ_OK) return s;
+    if (num_tokens < 0 || batch < 0 || num_q_heads < 1 || max_context < 0 || window < 0 || sinks < 0)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (num_q_heads % desc->num_kv_heads != 0) return UQ_ERR_INVALID_ARGUMENT;
+    const int32_t group = num_q_heads / desc->num_kv_heads;
+    if (group > kMaxGroup || batch > 65535 || desc->num_kv_heads > 65535) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens >= (int64_t(1) << 26)) return UQ_ERR_UNSUPPORTED;
+    const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
+    const int64_t seqs = num_tokens < batch ? num_tokens : batch;
+    e.row_blocks = rows / m + seqs;
+    int64_t blocks = (rows + m - 1) / m;   // of a batch of full sequences; at least one each
+    blocks = (blocks > seqs ? blocks : seqs) * desc->num_kv_heads;
+    int64_t walk = max_context;
+    if (window > 0) {
+        const int64_t most = int64_t(sinks) + window + 2 * 64 + m / group + 1;
+        walk = most < walk ? most : walk;
+    }
+    const int64_t tiles = (walk + 63) / 64;
+    int64_t splits = blocks > 0 ? (2 * uq::kNumCus + blocks - 1) / blocks : 1;
+    splits = splits < tiles / 4 ? splits : tiles / 4;
+    e.splits = int32_t(splits < 1 ? 1 : splits);
+    if (e.row_blocks * desc->num_kv_heads * e.splits > 0x7FFFFFFF) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens * num_q_heads > (int64_t(1) << 34)) return UQ_ERR_UNSUPPORTED;   // blocks of the join
+    e.workspace = e.splits > 1 ? size_t(e.splits) * size_t(num_tokens) * size_t(num_q_heads) *
+                                     size_t(desc->head_dim + 2) * sizeof(float)
+                               : 0;
+    return UQ_OK;
+}
+
+size_t uq_extend_workspace_bytes(const uq_cache_desc* desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
+                                 int32_t max_context, int32_t window, int32_t sinks) {
+    ExtendShape e;
+    return extend_shape(desc, num_tokens, batch, num_q_heads, max_context, window, sinks, e) == UQ_OK ? e.workspace : 0;
+}
+
+uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride,
+                              int64_t num_tokens, const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads,
+                              const uint8_t* kv_codes, const uint8_t* kv_scales, const int32_t* page_table,
+                              int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context,
+                              int32_t window, int32_t sinks, float softmax_scale, void* workspace,
+                              size_t workspace_bytes, void* out, uq_dtype out_dtype, void* stream) {
+    ExtendShape e;
+    uq_status s = extend_shape(desc, num_tokens, batch, num_q_heads, max_context, window, sinks, e);
+    if (s != UQ_OK) return s;
+    if (!row_dtype(q_dtype) && q_dtype != UQ_FP8_E4M3) return UQ_ERR_UNSUPPORTED;
+    if (out_dtype != UQ_F32 && out_dtype != UQ_BF16) return UQ_ERR_UNSUPPORTED;
+    if (!(isfinite(softmax_scale) && softmax_scale > 0.0f)) return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens == 0 || batch == 0) return UQ_OK;
+    if (q == nullptr || cu_seqlens == nullptr || kv_codes == nullptr || kv_scales == nullptr || page_table == nullptr ||
+        context_lens == nullptr || out == nullptr)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (max_pages_per_seq < 1 || int64_t(max_context) > int64_t(max_pages_per_seq) * kPageSize)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (!aligned16(q) || !aligned16(kv_codes) || !aligned16(kv_scales) || !aligned16(out) || !aligned16(workspace))
+        return UQ_ERR_INVALID_ARGUMENT;
+    const int64_t vec = q_dtype == UQ_F32 ? 4 : q_dtype == UQ_FP8_E4M3 ? 16 : 8;   // elements of 16 bytes
+    if (q_stride < int64_t(num_q_heads) * desc->head_dim || q_stride % vec != 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (e.workspace > 0 && workspace == nullptr) return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < e.workspace) return UQ_ERR_WORKSPACE_TOO_SMALL;
+    uq::ExtendParams p;
+    p.q = q;
+    p.q_dtype = int32_t(q_dtype);
+    p.q_stride = q_stride;
+    p.num_tokens = int32_t(num_tokens);
+    p.cu_seqlens = cu_seqlens;
+    p.batch = batch;
+    p.num_q_heads = num_q_heads;
+    p.num_kv_heads = desc->num_kv_heads;
+    p.group = num_q_heads / desc->num_kv_heads;
+    p.head_dim = desc->head_dim;
+    p.codes = kv_codes;
+    p.scales = kv_scales;
+    p.page_table = page_table;
+    p.max_pages_per_seq = max_pages_per_seq;
+    p.num_pages = desc->num_pages;
+    p.context_lens = context_lens;
+    p.max_context = max_context;
+    p.window = window;
+    p.sinks = window > 0 ? sinks : 0;
+    p.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
+    p.rotate_v = desc->rotate_v != 0;
+    p.row_blocks = int32_t(e.row_blocks);
+    p.splits = e.splits;
+    p.part_acc = static_cast<float*>(workspace);
+    p.part_ml = p.part_acc != nullptr ? p.part_acc + int64_t(e.splits) * num_tokens * num_q_heads * desc->head_dim : nullptr;
+    p.out = out;
+    p.out_dtype = out_dtype == UQ_F32 ? 0 : 1;
+    return from_hip(uq::launch_extend(p, static_cast<hipStream_t>(stream)));
+}
+
+// The tokens a window's walk can have at most: the sinks' pages, and the
+// window's with the rest of its first page.
+static int32_t window_bound(int32_t max_context, int32_t window, int32_t sinks) {
+    const int64_t most = (int64_t(sinks) + 15) / 16 * 16 + window + 15;
+    return int32_t(most < max_context ? most : max_context);
+}
+
+size_t uq_decode_window_workspace_bytes(const uq_cache_desc* desc, int32_t batch, int32_t num_q_heads,
+                                        int32_t max_context, int32_t window, int32_t sinks, int32_t partition_tokens) {
+    if (window < 1 || sinks < 0 || max_context < 0) return 0;
+    return uq_decode_workspace_bytes(desc, batch, num_q_heads, window_bound(max_context, window, sinks), partition_tokens);
+}
+
+uq_status uq_decode_window(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, const void* k_new,
+                           const void* v_new, uq_dtype new_dtype, int32_t batch, int32_t num_q_heads,
+                           uint8_t* kv_codes, uint8_t* kv_scales, const int32_t* page_table,
+                           int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context,
+                           int32_t window, int32_t sinks, float softmax_scale, int32_t partition_tokens,
+                           void* workspace, size_t workspace_bytes, void* out, uq_dtype out_dtype, void* stream) {
+    if (window < 1 || sinks < 0 || max_context < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (int64_t(max_context) > int64_t(max_pages_per_seq) * kPageSize) return UQ_ERR_INVALID_ARGUMENT;
+    uq::DecodeParams p;
+    uq_status s = decode_setup(desc, q, q_dtype, batch, num_q_heads, kv_codes, kv_scales, page_table,
+                               max_pages_per_seq, context_lens, window_bound(max_context, window, sinks), softmax_scale,
+                               partition_tokens, workspace, workspace_bytes, out, out_dtype, p);
+    if (s != UQ_OK) return s;
+    if (k_new != nullptr || v_new != nullptr) {
+        s = step_args(k_new, v_new, new_dtype, p);
+        if (s != UQ_OK) return s;
+    }
+    p.window = window;
+    p.sinks = sinks;
+    p.context_bound = max_context;
+    p.allow_wave_parts = 0;   // the walk's length is bounded: fixed partitions on the block grid
+    p.plan_rows = 0;
     s = from_hip(uq::launch_decode_partials(p, static_cast<hipStream_t>(stream)));
     if (s != UQ_OK) return s;
     return from_hip(uq::launch_decode_merge(p, static_cast<hipStream_t>(stream)));

@@ -247,12 +247,15 @@ template <int W, int P>
 __device__ __forceinline__ int ids_page(int wave, int chunk, int lane) {
     return P * (wave + W * (64 / P * chunk + lane / P)) + lane % P;
 }
+// Under a sliding window the pages are counted without those between the first
+// tokens and the window: from page gap_page on, the table's entry lies `shift`
+// further (both 0 otherwise).
 template <int W, int P = 2>
 __device__ __forceinline__ int32_t load_page_ids(const int32_t* __restrict__ pt_row, int first_page, int n_pages,
-                                                 int wave, int chunk, int lane) {
+                                                 int wave, int chunk, int lane, int gap_page = 0, int shift = 0) {
     const int pg = ids_page<W, P>(wave, chunk, lane);
     int32_t id = 0;
-    if (pg < n_pages) id = pt_row[first_page + pg];
+    if (pg < n_pages) id = pt_row[first_page + pg + (first_page + pg >= gap_page ? shift : 0)];
     return id;
 }
 // The same ids copied into the wave's LDS slot (lane j's id at dword j)
@@ -262,9 +265,11 @@ __device__ __forceinline__ int32_t load_page_ids(const int32_t* __restrict__ pt_
 // past the partition read its first entry (their ids are never used).
 template <int W, int P = 2>
 __device__ __forceinline__ void copy_page_ids(uint8_t* slot, const int32_t* __restrict__ pt_row, int first_page,
-                                              int n_pages, int wave, int chunk, int lane) {
-    const int pg = ids_page<W, P>(wave, chunk, lane);
-    __builtin_amdgcn_global_load_lds(pt_row + first_page + (pg < n_pages ? pg : 0), (lds_ptr_t)slot, 4, 0, 0);
+                                              int n_pages, int wave, int chunk, int lane, int gap_page = 0,
+                                              int shift = 0) {
+    int pg = ids_page<W, P>(wave, chunk, lane);
+    pg = first_page + (pg < n_pages ? pg : 0);
+    __builtin_amdgcn_global_load_lds(pt_row + pg + (pg >= gap_page ? shift : 0), (lds_ptr_t)slot, 4, 0, 0);
 }
 // This lane's id from the wave's LDS slot; the caller has waited for the copy.
 __device__ __forceinline__ int32_t read_page_ids(uint32_t slot_addr, int lane) {
@@ -1154,9 +1159,34 @@ __device__ __forceinline__ int prefix_tokens_of(const DecodeParams& p, int b, in
     return pl > 0 ? (pl & ~15) : 0;
 }
 
-template <int F, int S, bool WP, bool PROBE = false, int W = Fmt<F>::kWaves>
+// A context of `len` tokens under a sliding window, as the decode kernel walks
+// it: the pages that hold a visible token (the first `sinks` tokens and the
+// last `window`), counted without the gap between them.  Page v of the walk is
+// page v (v < gap_page) or v + shift of the sequence, and the walk's tokens
+// hide_from .. hide_to - 1 (the rest of the sinks' last page and the start of the
+// window's first) are read but hidden; where the two meet there is no
+// gap, only hidden tokens.  The walk's last token is the context's.
+struct WindowView {
+    int len;                    // tokens of the walk
+    int gap_page, shift;        // pages
+    int hide_from, hide_to;     // tokens of the walk
+};
+__device__ __forceinline__ WindowView window_view(const DecodeParams& p, int len) {
+    WindowView v;
+    const int from = len > p.window ? len - p.window : 0;   // first token of the window
+    v.gap_page = p.sinks < from ? (p.sinks + kPage - 1) / kPage : from / kPage;
+    v.shift = from / kPage - v.gap_page;
+    if (v.shift < 0) v.shift = 0;
+    v.len = len - kPage * v.shift;
+    v.hide_from = p.sinks;
+    v.hide_to = from - kPage * v.shift;
+    return v;
+}
+
+template <int F, int S, bool WP, bool PROBE = false, int W = Fmt<F>::kWaves, bool WIN = false>
 __global__ void __launch_bounds__(64 * W)
 __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>()))) decode_kernel(DecodeParams p) {
+    static_assert(!WIN || (is_fp4<F>() && !WP && !PROBE), "windows: the FP4 cache on the block grid");
     static_assert(S == 2 || S == 4, "ring slots");
     static_assert(W == 2 || W == 4 || W == 8, "waves per block");
     static_assert(!PROBE || is_fp4<F>(), "the page-gather probe follows the FP4 kernels");
@@ -1228,6 +1258,7 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
     int start, end, ctx = 0;
     bool in_place = false;               // the context is held by this block alone and finished in place
     int plan_prow = 0;                   // balanced split: the block's partial row
+    WindowView win{};                    // WIN: how the walk maps to the context
     if (plan) {
         int len;
         if (!(p.batch <= 64 ? plan_of_row<1>(p, lane, row, b, part, ctx, len, plan_prow)
@@ -1262,7 +1293,13 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
                 ctx = row_ctx;
             } else {
                 ctx = p.context_lens[b];
-                ctx = ctx < p.max_context ? ctx : p.max_context;
+                if constexpr (WIN) {
+                    ctx = ctx < p.context_bound ? ctx : p.context_bound;
+                    win = window_view(p, ctx > 0 ? ctx : 0);
+                    ctx = win.len;
+                } else {
+                    ctx = ctx < p.max_context ? ctx : p.max_context;
+                }
             }
             start = part * p.partition_tokens;
             if (cascade) {
@@ -1399,7 +1436,8 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
     float xk[8], xv[8];   // the new token's K and V (decode step, lanes 0..15 of the owning wave)
     int32_t page_new = -1;
     if (append && lane < 16) {
-        page_new = p.page_table[int64_t(b) * p.max_pages_per_seq + (pos_new >> 4)];
+        const int pg = pos_new >> 4;
+        page_new = p.page_table[int64_t(b) * p.max_pages_per_seq + pg + (WIN && pg >= win.gap_page ? win.shift : 0)];
         const int64_t elem = (int64_t(b) * p.num_kv_heads + hk) * kHeadDim + 8 * lane;
         if (p.new_dtype == 0) {
             load_x8<0>(p.k_new, elem, xk);
@@ -1450,8 +1488,9 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
     constexpr int kIdIters = 64 / kPages;   // iterations per chunk of 64 page ids
     int32_t ids = 0;
     if (n_local > 0) {
-        ids = load_page_ids<ws, kPages>(pt_row, first_page, n_pages, woff, 0, lane);
-        if (n_local > kIdIters) copy_page_ids<ws, kPages>(ids_slot, pt_row, first_page, n_pages, woff, 1, lane);
+        ids = load_page_ids<ws, kPages>(pt_row, first_page, n_pages, woff, 0, lane, win.gap_page, win.shift);
+        if (n_local > kIdIters)
+            copy_page_ids<ws, kPages>(ids_slot, pt_row, first_page, n_pages, woff, 1, lane, win.gap_page, win.shift);
     }
     // copy the pages whose ids sit at lanes kPages * i .. of `ids` into slot s
     auto issue = [&](int s, int i) {
@@ -1636,7 +1675,8 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
                 // so the wait at the top of this iteration covered it
                 ids = clamp_ids(read_page_ids(ids_addr, lane), p.num_pages);
                 if (kn + kIdIters < n_local)
-                    copy_page_ids<ws, kPages>(ids_slot, pt_row, first_page, n_pages, woff, kn / kIdIters + 1, lane);
+                    copy_page_ids<ws, kPages>(ids_slot, pt_row, first_page, n_pages, woff, kn / kIdIters + 1, lane,
+                                              win.gap_page, win.shift);
             }
             issue(slot, kn % kIdIters);
         }
@@ -1647,6 +1687,10 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
         }
 
         const int it = woff + ws * k;
+        // WIN: some token of the iteration is hidden (wave-uniform)
+        bool some_hidden = false;
+        if constexpr (WIN) some_hidden = start + kSpan * it < win.hide_to && start + kSpan * it + kSpan > win.hide_from;
+        auto hidden = [&](int tok) { return WIN && tok >= win.hide_from && tok < win.hide_to; };
         if constexpr (kTwo) {
             // A row of the product holds a token of pair A (k-blocks 0, 1) and one of
             // pair B (lanes 32..63: k-blocks 2, 3).  A token past the end may never
@@ -1657,6 +1701,12 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
 #pragma unroll
                 for (int pg = 0; pg < 2; ++pg)
                     if (lane >= 32 && start + kSpan * it + 32 + 16 * pg + (lane & 15) >= end) c.ks[pg] = 127u;
+            }
+            if (some_hidden) {
+                // hidden tokens of either pair the same
+#pragma unroll
+                for (int pg = 0; pg < 2; ++pg)
+                    if (hidden(start + kSpan * it + (lane >= 32 ? 32 : 0) + 16 * pg + (lane & 15))) c.ks[pg] = 127u;
             }
         }
 
@@ -1694,6 +1744,25 @@ __attribute__((amdgpu_waves_per_eu(occupancy<F, S, W>(), occupancy<F, S, W>())))
                         zero_token(c, 0, i);
                     }
                     if (tok0 + 16 + i >= end) {
+                        vs1 &= ~(0xFFu << (8 * i));
+                        zero_token(c, 1, i);
+                    }
+                }
+            }
+        }
+
+        if constexpr (WIN) {
+            if (some_hidden) {
+                // hidden tokens: no score, and no V (it may be anything)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (hidden(tok0 + i)) {
+                        x[i] = -__builtin_inff();
+                        vs0 &= ~(0xFFu << (8 * i));
+                        zero_token(c, 0, i);
+                    }
+                    if (hidden(tok0 + 16 + i)) {
+                        x[4 + i] = -__builtin_inff();
                         vs1 &= ~(0xFFu << (8 * i));
                         zero_token(c, 1, i);
                     }
@@ -2463,8 +2532,9 @@ __device__ __forceinline__ void merge_plan(const DecodeParams& p, bool longs, in
 
 // One launch per call: fixed partitions (PLAN false; with or without a shared
 // prefix) or the balanced split.
-template <int D, int GROUPS, bool PLAN>
+template <int D, int GROUPS, bool PLAN, bool WIN = false>
 __global__ void __launch_bounds__(256) merge_kernel(DecodeParams p) {
+    static_assert(!WIN || !PLAN, "windows have fixed partitions");
     static_assert(GROUPS == 1 || GROUPS == 4 || GROUPS == 16, "16 lanes, a wave or a block per row");
     __shared__ MergeLds<D / 16> lds[1];
     constexpr int R = 16 / GROUPS;   // query heads per block
@@ -2503,7 +2573,12 @@ __global__ void __launch_bounds__(256) merge_kernel(DecodeParams p) {
     } else {
         const int b = blockIdx.y;
         int ctx = p.context_lens[b];
-        ctx = ctx < p.max_context ? ctx : p.max_context;
+        if constexpr (WIN) {
+            ctx = ctx < p.context_bound ? ctx : p.context_bound;
+            ctx = window_view(p, ctx > 0 ? ctx : 0).len;
+        } else {
+            ctx = ctx < p.max_context ? ctx : p.max_context;
+        }
         int np = ctx > 0 ? (ctx + p.partition_tokens - 1) / p.partition_tokens : 0;
         int nq = 0;
         int64_t row0 = (int64_t(b) * p.num_q_heads + hq) * p.num_partitions;
@@ -2695,7 +2770,25 @@ hipError_t launch_gather_probe(const DecodeParams& p, uint32_t* sink, hipStream_
     return hipErrorInvalidValue;
 }
 
+template <int F>
+static hipError_t launch_window_with(const DecodeParams& p, hipStream_t stream) {
+    constexpr int W = Fmt<F>::kWaves;
+    const dim3 grid{unsigned(block_grid_blocks(p))};
+    launch_kernel(decode_kernel<F, kRingSlots, false, false, W, true>, grid, dim3(64 * W), stream, p);
+    return hipGetLastError();
+}
+static hipError_t launch_window(const DecodeParams& p, hipStream_t stream) {
+    switch (p.kv_fmt) {
+        case kFp4d64: return launch_window_with<kFp4d64>(p, stream);
+        case kFp4d64x2: return launch_window_with<kFp4d64x2>(p, stream);
+        case kFp4d64p2: return launch_window_with<kFp4d64p2>(p, stream);
+        case kFp4d256: return launch_window_with<kFp4d256>(p, stream);
+        default: return launch_window_with<kFp4>(p, stream);
+    }
+}
+
 hipError_t launch_decode_partials(const DecodeParams& p, hipStream_t stream) {
+    if (p.window > 0) return launch_window(p, stream);
     if (p.kv_fmt == kFp8) return launch_partials<kFp8>(p, stream);
     if (p.kv_fmt == kBf16) return launch_partials<kBf16>(p, stream);
     if (p.kv_fmt == kTq4) return launch_partials<kTq4>(p, stream);
@@ -2719,7 +2812,7 @@ hipError_t launch_decode_partials(const DecodeParams& p, hipStream_t stream) {
 // balanced split can have more than kLongRow rows (what the others leave of
 // plan_rows, at most its length in planner units), a block for each of those, up
 // to about one per CU, is added.
-template <int D, bool PLAN>
+template <int D, bool PLAN, bool WIN = false>
 static hipError_t launch_merge_with(DecodeParams p, hipStream_t stream) {
     const int partials = PLAN ? p.plan_rows / p.batch
                          : p.wave_parts > 1 ? (p.num_partitions + p.wave_parts - 1) / p.wave_parts : p.num_partitions;
@@ -2741,13 +2834,14 @@ static hipError_t launch_merge_with(DecodeParams p, hipStream_t stream) {
             p.long_blocks = int32_t(y * grid.x);
         }
     }
-    if (rows == 16) hipLaunchKernelGGL((merge_kernel<D, 1, PLAN>), grid, dim3(256), 0, stream, p);
-    else if (rows == 4) hipLaunchKernelGGL((merge_kernel<D, 4, PLAN>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((merge_kernel<D, 16, PLAN>), grid, dim3(256), 0, stream, p);
+    if (rows == 16) hipLaunchKernelGGL((merge_kernel<D, 1, PLAN, WIN>), grid, dim3(256), 0, stream, p);
+    else if (rows == 4) hipLaunchKernelGGL((merge_kernel<D, 4, PLAN, WIN>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((merge_kernel<D, 16, PLAN, WIN>), grid, dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 template <int D>
 static hipError_t launch_merge(const DecodeParams& p, hipStream_t stream) {
+    if (p.window > 0) return launch_merge_with<D, false, true>(p, stream);
     return p.plan_rows > 0 ? launch_merge_with<D, true>(p, stream) : launch_merge_with<D, false>(p, stream);
 }
 
@@ -2761,3 +2855,5 @@ hipError_t launch_decode_merge(const DecodeParams& p, hipStream_t stream) {
 }
 
 }  // namespace uq
+
+#include "uq_extend.hpp"

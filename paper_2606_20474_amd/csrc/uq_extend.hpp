@@ -1,0 +1,647 @@
+// uq_extend.hpp -- attention of several new queries per sequence over the FP4
+// cache (uq_extend_attention of include/uq.h), part of the uq_decode.hip
+// translation unit.
+//
+// With m queries at the end of a context of n tokens, query i at position
+// n - m + i, and G query heads per KV head, a row is a (query, head of the KV
+// head) pair, row r = query r / G, head r % G: all rows of a (sequence, KV head)
+// read the same keys and values, so a block takes M of them and walks the
+// visible context once in tiles of 64 tokens (4 pages).
+//
+//   scores    S^T = K Q^T on v_mfma_scale_f32_32x32x64_f8f6f4: FP4 keys with
+//             their scale bytes as operand A (rows = tokens), the rotated FP8
+//             queries as operand B (columns = rows of the block).  A lane then
+//             holds 16 tokens of one row, so the softmax needs no exchange
+//             between lanes but one (lanes l and l ^ 32 share a row).
+//   softmax   in the log2 domain, running maximum with a lazy rescale, sums per
+//             lane until the end.
+//   values    O^T += V^T P^T on v_mfma_f32_32x32x16_f16.  The scores leave the
+//             QK instruction in the order in which P enters as operand B (the
+//             token of a k index is free as long as V's operand uses the same
+//             order), so P stays in registers.  V is decoded once per block and
+//             tile into FP16 in LDS, transposed to operand order.
+//
+// FP16 holds a code times 2^E exactly for E in [-23, 13], and P with 11
+// significant bits; a tile with a scale outside that range (|V| from 2^16 on, or a
+// group below 2^-22) takes BF16 values and P as two BF16 terms instead, as
+// decode_kernel does.
+#pragma once
+
+#include "uq_device.hpp"
+#include "uq_internal.hpp"
+
+namespace uq {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;   // tokens per tile
+
+// Where a block's rows stand and which tiles they see.
+struct ExtendRows {
+    int b;              // sequence
+    int first, count;   // its first token row in q, number of queries
+    int row0;           // first row of the block
+    int n_ctx;          // context length
+    int sink_tiles;     // tiles of the first tokens, ahead of the others
+    int tile0;          // first of the other tiles
+    int tiles;          // all of them
+};
+
+// Tiles that rows with positions lo .. hi see.
+__device__ __forceinline__ void extend_tiles(const ExtendParams& p, int lo, int hi, ExtendRows& r) {
+    const int end = hi + 1;
+    const int last = end > 0 ? (end + kTile - 1) / kTile : 0;
+    r.sink_tiles = 0;
+    r.tile0 = 0;
+    if (p.window > 0) {
+        const int from = lo - p.window + 1;   // the first row's window, the earliest
+        r.tile0 = from > 0 ? from / kTile : 0;
+        const int sinks = p.sinks < end ? p.sinks : end;
+        r.sink_tiles = sinks > 0 ? (sinks + kTile - 1) / kTile : 0;
+        if (r.sink_tiles >= r.tile0) r.sink_tiles = r.tile0 = 0;
+    }
+    r.tiles = r.sink_tiles + (last > r.tile0 ? last - r.tile0 : 0);
+}
+
+__device__ __forceinline__ int extend_first(const ExtendParams& p, int b) {
+    const int x = p.cu_seqlens[b];
+    return x < 0 ? 0 : x < p.num_tokens ? x : p.num_tokens;
+}
+__device__ __forceinline__ int extend_context(const ExtendParams& p, int b) {
+    int n = p.context_lens[b];
+    n = n < p.max_context ? n : p.max_context;
+    return n > 0 ? n : 0;
+}
+
+// Row block `at` of the batch, M rows each, the blocks of one sequence from its
+// last rows (the longest) to its first.  False: there is none.  Wave-uniform;
+// every wave of the block finds it alone, 64 sequences at a time.
+template <int M>
+__device__ __forceinline__ bool extend_find(const ExtendParams& p, int at, ExtendRows& r) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+        const int b = b0 + lane;
+        int first = 0, count = 0;
+        if (b < p.batch) {
+            first = extend_first(p, b);
+            count = extend_first(p, b + 1) - first;
+            count = count > 0 ? count : 0;
+        }
+        const int blocks = int((int64_t(count) * p.group + M - 1) / M);
+        int sum = blocks;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int o = __shfl_up(sum, s);
+            if (lane >= s) sum += o;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > at);
+        if (past != 0) {
+            const int l = __builtin_ctzll(past);
+            r.b = b0 + l;
+            r.first = __builtin_amdgcn_readlane(first, l);
+            r.count = __builtin_amdgcn_readlane(count, l);
+            const int n = __builtin_amdgcn_readlane(blocks, l);
+            const int i = at - before - (__builtin_amdgcn_readlane(sum, l) - n);
+            r.row0 = (n - 1 - i) * M;
+            r.n_ctx = extend_context(p, r.b);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// Positions of a row block's first and last row.
+template <int M>
+__device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendRows& r, int& lo, int& hi) {
+    const int last = r.row0 + M < r.count * p.group ? r.row0 + M - 1 : r.count * p.group - 1;
+    lo = r.n_ctx - r.count + r.row0 / p.group;
+    hi = r.n_ctx - r.count + last / p.group;
+}
+
+// One 16-byte unit of a page's V codes (4 tokens x 8 channels) as eight pairs of
+// dwords: of each channel the 4 tokens in FP16 (H) or BF16.
+template <bool H>
+__device__ __forceinline__ void decode_unit(const uint4& v, uint32_t scale_bytes, uint2 (&out)[8]) {
+    float sc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) sc[t] = ue8m0_to_f32(scale_bytes >> (8 * t));
+    uint32_t w[4][4];   // [token][channel pair]
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const uint32_t d = t == 0 ? v.x : t == 1 ? v.y : t == 2 ? v.z : v.w;
+        if constexpr (H) {
+            w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 0));
+            w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 1));
+            w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 2));
+            w[t][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 3));
+        } else {
+            w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 0));
+            w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 1));
+            w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 2));
+            w[t][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 3));
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        out[2 * c] = make_uint2(__builtin_amdgcn_perm(w[1][c], w[0][c], 0x05040100u),
+                                __builtin_amdgcn_perm(w[3][c], w[2][c], 0x05040100u));
+        out[2 * c + 1] = make_uint2(__builtin_amdgcn_perm(w[1][c], w[0][c], 0x07060302u),
+                                    __builtin_amdgcn_perm(w[3][c], w[2][c], 0x07060302u));
+    }
+}
+
+// The rotation R of one column held as accumulators: channel 32 c + 8 (i / 4) + 4
+// half + i % 4 in acc[c][q][i], lanes l and l ^ 32 sharing the column.  Stage
+// order 1, 2, 4 (between the lanes), 8, ..., as wht_x.
+template <int CB, int NQ>
+__device__ __forceinline__ void wht_columns(v16f (&acc)[CB][NQ], int q, int half) {
+#pragma clang fp contract(off)
+    auto stage = [&](int h) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (i & h) continue;
+                const float a = acc[c][q][i], b = acc[c][q][i + h];
+                acc[c][q][i] = a + b;
+                acc[c][q][i + h] = a - b;
+            }
+    };
+    stage(1);
+    stage(2);
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float a = acc[c][q][i], b = a;
+            swap32(a, b);   // a: the lower half's value, b: the upper's, in both lanes
+            acc[c][q][i] = half ? a - b : a + b;
+        }
+    stage(4);
+    stage(8);
+#pragma unroll
+    for (int h = 1; h < CB; h <<= 1)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            if (c & h) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float a = acc[c][q][i], b = acc[c + h][q][i];
+                acc[c][q][i] = a + b;
+                acc[c + h][q][i] = a - b;
+            }
+        }
+    const float r = inv_sqrt_d<32 * CB>();
+#pragma unroll
+    for (int c = 0; c < CB; ++c) acc[c][q] *= r;
+}
+
+// Tiles per split of a row block with `tiles` of them.
+__host__ __device__ __forceinline__ int extend_per_split(int tiles, int splits) {
+    const int per = (tiles + splits - 1) / splits;
+    return per > 2 ? per : 2;
+}
+
+// The rows of a (sequence, KV head) pair: NQ blocks of 32 rows per wave, W waves.
+template <int D, int NQ, int W>
+__global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
+    constexpr int M = 32 * NQ * W;            // rows of the block
+    constexpr int NT = 64 * W;
+    constexpr int KS = D / 64;                // k steps of QK^T
+    constexpr int CB = D / 32;                // channel blocks of PV
+    constexpr int N = D / 16;                 // channels per lane of a 16-lane row
+    constexpr int kUnits = 2 * D;             // 16-byte units of a tile's K, and of its V
+    constexpr int UR = (kUnits + NT - 1) / NT;
+    constexpr int kPageUnits = D / 2;
+    constexpr int kPageScales = D;            // scale bytes of a page and KV head, K then V
+    constexpr int kVt = kTile * D * 2;        // decoded values of a tile
+    constexpr int kK = kTile * D / 2;         // K codes of a tile
+    __shared__ __attribute__((aligned(16))) uint8_t vt[2][kVt];
+    __shared__ __attribute__((aligned(16))) uint8_t kt[2][kK];
+    __shared__ __attribute__((aligned(16))) uint8_t kst[2][4 * D / 2];
+    __shared__ int wide[2];                   // a scale outside FP16's range in the tile
+    static_assert(M * D <= 2 * kVt, "the query operand is staged in the value buffers");
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, col = lane & 31;
+    const int hk = int(blockIdx.x % unsigned(p.num_kv_heads));
+    const int rest = int(blockIdx.x / unsigned(p.num_kv_heads));
+    const int split = rest % p.splits;
+    ExtendRows r;
+    if (!extend_find<M>(p, rest / p.splits, r)) return;
+    int lo, hi;
+    extend_span<M>(p, r, lo, hi);
+    extend_tiles(p, lo, hi, r);
+    int first_tile = 0, last_tile = r.tiles;
+    bool whole = true;
+    if (p.splits > 1) {
+        const int per = extend_per_split(r.tiles, p.splits);
+        whole = r.tiles <= per;
+        first_tile = split * per;
+        last_tile = first_tile + per < r.tiles ? first_tile + per : r.tiles;
+        if (first_tile >= last_tile && !(split == 0)) return;
+    }
+    const int rows = r.count * p.group;       // of the sequence and KV head
+
+    // ---- queries: rotated and cast to FP8 (unless they are), to the lane order
+    // of the B operand: k step s, lane (row, half): bytes 0..15 are channels
+    // 64 s + 16 half .., 16..31 are 64 s + 32 + 16 half ..
+    uint8_t* qs = &vt[0][0] + wave * (32 * NQ * D);
+    const int L = lane & 15;
+#pragma unroll 4
+    for (int i = 0; i < 8 * NQ; ++i) {
+        const int rr = 4 * i + (lane >> 4);                       // row of the wave
+        const int row = r.row0 + wave * (32 * NQ) + rr;
+        uint32_t w[N / 4];
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) w[j] = 0u;
+        const int tok = row / p.group;
+        if (row < rows) {
+            const int64_t elem = int64_t(r.first + tok) * p.q_stride + int64_t(hk * p.group + row - tok * p.group) * D + N * L;
+            if (p.q_dtype == 3) {
+                const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.q) + elem);
+#pragma unroll
+                for (int j = 0; j < N / 4; ++j) w[j] = src[j];
+            } else {
+                float x[N];
+#pragma unroll
+                for (int j = 0; j < N / 4; ++j) {
+                    float (&y)[4] = *reinterpret_cast<float(*)[4]>(&x[4 * j]);
+                    if (p.q_dtype == 0) load_x4<0>(p.q, elem + 4 * j, y);
+                    else if (p.q_dtype == 1) load_x4<1>(p.q, elem + 4 * j, y);
+                    else load_x4<2>(p.q, elem + 4 * j, y);
+                }
+                wht_x<N>(x, L);
+#pragma unroll
+                for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const int c = N * L + 4 * j;
+            const int dst = ((rr >> 5) * KS + (c >> 6)) * 2048 + (((c >> 4) & 1) * 32 + (rr & 31)) * 32 + ((c >> 5) & 1) * 16 + (c & 15);
+            *reinterpret_cast<uint32_t*>(qs + dst) = w[j];
+        }
+    }
+    if (tid < 2) wide[tid] = 0;
+    __syncthreads();
+    v8i qop[NQ][KS];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const uint4* src = reinterpret_cast<const uint4*>(qs + (q * KS + s) * 2048 + lane * 32);
+            const uint4 a = src[0], c = src[1];
+            qop[q][s] = v8i{int(a.x), int(a.y), int(a.z), int(a.w), int(c.x), int(c.y), int(c.z), int(c.w)};
+        }
+    __syncthreads();
+
+    // this lane's rows: position, and the first token of the window
+    int pos[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int row = r.row0 + wave * (32 * NQ) + 32 * q + col;
+        pos[q] = row < rows ? r.n_ctx - r.count + row / p.group : -1;
+    }
+    // the wave's first and last position (waves without rows: nothing to do)
+    const int w_row0 = r.row0 + wave * (32 * NQ);
+    const bool busy = w_row0 < rows;
+    const int w_last = w_row0 + 32 * NQ < rows ? w_row0 + 32 * NQ - 1 : rows - 1;
+    const int w_lo = r.n_ctx - r.count + w_row0 / p.group, w_hi = r.n_ctx - r.count + w_last / p.group;
+
+    const int64_t heads = p.num_kv_heads;
+    const int32_t* pt_row = p.page_table + int64_t(r.b) * p.max_pages_per_seq;
+    const int n_pages = (hi + kPage) / kPage;   // pages that hold a token a row sees, or earlier
+    auto token_of = [&](int t) { return kTile * (t < r.sink_tiles ? t : t - r.sink_tiles + r.tile0); };
+    auto page_id = [&](int tile, int pg) -> int64_t {
+        const int v = token_of(tile) / kPage + pg;
+        int32_t id = 0;
+        if (v < n_pages) id = pt_row[v];
+        return clamp_ids(id, p.num_pages);
+    };
+    // this thread's units of a tile: V codes and scales into registers, K codes and
+    // scales into LDS
+    uint4 vcode[UR];
+    uint32_t vscale[UR];
+    auto load_tile = [&](int tile, int slot) {
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            const int unit0 = 64 * wave + u * NT, unit = unit0 + lane;
+            if (unit0 < kUnits) {   // whole waves
+                const int in = unit % kPageUnits;
+                const int64_t ph = page_id(tile, unit / kPageUnits) * heads + hk;
+                const uint8_t* codes = p.codes + ph * (16 * D);
+                __builtin_amdgcn_global_load_lds(codes + 16 * in,
+                                                 (lds_ptr_t)(&kt[slot][0] + 16 * unit0), 16, 0, 0);
+                vcode[u] = *reinterpret_cast<const uint4*>(codes + 8 * D + 16 * in);
+                const int tq = in / (D / 8), oct = in % (D / 8);
+                vscale[u] = *reinterpret_cast<const uint32_t*>(p.scales + ph * kPageScales + D / 2 + (oct >> 2) * 16 + 4 * tq);
+            }
+        }
+        if (wave == W - 1 && lane < D / 8) {
+            const int64_t ph = page_id(tile, lane / (D / 32)) * heads + hk;
+            __builtin_amdgcn_global_load_lds(p.scales + ph * kPageScales + 16 * (lane % (D / 32)), (lds_ptr_t)&kst[slot][0],
+                                             16, 0, 0);
+        }
+    };
+    // decode this thread's units into the value buffer
+    auto store_units = [&](int tile, int slot, bool bf16) {
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            const int unit = tid + u * NT;
+            if (unit >= kUnits) continue;
+            const int pg = unit / kPageUnits, in = unit % kPageUnits;
+            const int tq = in / (D / 8), oct = in % (D / 8);
+            // tokens no row of the block sees may hold anything: zero scale
+            const int tok = token_of(tile) + kPage * pg + 4 * tq;
+            uint32_t sc = vscale[u];
+            if (tok + 4 > hi + 1 || (p.window > 0 && tok <= lo - p.window && tok + 4 > p.sinks)) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (tok + t > hi || (p.window > 0 && tok + t <= lo - p.window && tok + t >= p.sinks)) sc &= ~(0xFFu << (8 * t));
+            }
+            uint2 out[8];
+            if (bf16) {
+                decode_unit<false>(vcode[u], sc, out);
+            } else {
+                bool far = false;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint32_t b = (sc >> (8 * t)) & 0xFFu;
+                    far |= b != 0 && (b < 127 - 23 || b > 127 + 13);
+                }
+                if (far) wide[slot] = 1;
+                decode_unit<true>(vcode[u], sc, out);
+            }
+            const int cb = oct >> 2, h = tq & 1;
+            uint8_t* dst = &vt[slot][0] + ((pg * CB + cb) * 2 + h) * 512 + (tq >> 1) * 8;
+            const int f = (2 * cb + h) & 7;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + ((8 * (oct & 3) + i) ^ f) * 16) = out[i];
+        }
+    };
+
+    const float sl2 = p.scale_log2;
+    constexpr float kNoMax = -1e30f;
+    float m_run[NQ], l_run[NQ];
+    v16f acc[CB][NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        m_run[q] = kNoMax;
+        l_run[q] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[c][q] = v16f(0.f);
+    }
+    bool big_max = false;
+
+    if (first_tile < last_tile) load_tile(first_tile, 0);
+    for (int t = first_tile; t < last_tile; ++t) {
+        const int slot = (t - first_tile) & 1;
+        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);   // this thread's K copies and V units of the tile
+        store_units(t, slot, false);
+        __syncthreads();
+        const bool bf16 = wide[slot] != 0;
+        if (bf16) {
+            // rare: decode again in BF16
+            __syncthreads();
+            if (tid == 0) wide[slot] = 0;
+            store_units(t, slot, true);
+            __syncthreads();
+        }
+        if (t + 1 < last_tile) load_tile(t + 1, slot ^ 1);
+        const int tok0 = token_of(t);
+        // tiles past the wave's last row, or before its windows and after the sinks
+        if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + kTile <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
+        const bool clear = tok0 + kTile - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + kTile <= p.sinks);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {   // 32 tokens
+            v16f s[NQ];
+            const v16f zero = v16f(0.f);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int pg = 2 * tb + (col >> 4), at = (2 * k + half) * 16 + (col & 15);
+                const uint4 a = *reinterpret_cast<const uint4*>(&kt[slot][0] + pg * (8 * D) + at * 16);
+                const int sc = kst[slot][pg * (D / 2) + at];
+                const v8i ka = {int(a.x), int(a.y), int(a.z), int(a.w), 0, 0, 0, 0};
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+                    s[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qop[q][k], k == 0 ? zero : s[q], 4, 0, 0, sc,
+                                                                           0, 127);
+            }
+            // row i of a product: token 8 (i / 4) + 4 half + i % 4 of the 32
+            const int tok = tok0 + 32 * tb + 4 * half;
+            uint32_t ph[NQ][8], pl[NQ][8];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                if (!clear) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int tt = tok + 8 * (i >> 2) + (i & 3);
+                        bool seen = tt <= pos[q];
+                        if (p.window > 0) seen = seen && (tt > pos[q] - p.window || tt < p.sinks);
+                        s[q][i] = seen ? s[q][i] : -__builtin_inff();
+                    }
+                }
+                float mx = s[q][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) mx = __builtin_fmaxf(mx, s[q][i]);
+                if (__builtin_amdgcn_ballot_w64(mx * sl2 > m_run[q] + kLazyRescale) != 0) {
+                    float a = mx, b = mx;
+                    swap32(a, b);
+                    const float mloc = __builtin_fmaxf(a, b) * sl2;
+                    if (mloc > m_run[q] + kLazyRescale) {
+                        const float alpha = __builtin_amdgcn_exp2f(m_run[q] - mloc);
+                        l_run[q] *= alpha;
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) acc[c][q] *= alpha;
+                        m_run[q] = mloc;
+                    }
+                    bool big = false;
+#pragma unroll
+                    for (int qq = 0; qq < NQ; ++qq) big = big || (__builtin_fabsf(m_run[qq]) >= 0x1p20f && m_run[qq] != kNoMax);
+                    big_max = __builtin_amdgcn_ballot_w64(big) != 0;
+                }
+                float e[16];
+                if (!big_max) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i], sl2, -m_run[q]));
+                } else {
+                    // (see decode_kernel: the rounded product, as m_run was)
+#pragma clang fp contract(off)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(s[q][i] * sl2 - m_run[q]);
+                }
+                if (!bf16) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const v2h h = {_Float16(e[2 * i]), _Float16(e[2 * i + 1])};
+                        ph[q][i] = __builtin_bit_cast(uint32_t, h);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) split_p(e[2 * i], e[2 * i + 1], ph[q][i], pl[q][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) l_run[q] += e[i];
+            }
+#pragma unroll
+            for (int mm = 0; mm < 2; ++mm) {   // 16 tokens, one page
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    const int f = (2 * c + half) & 7;
+                    const uint4 a = *reinterpret_cast<const uint4*>(&vt[slot][0] + (((2 * tb + mm) * CB + c) * 2 + half) * 512 +
+                                                                    (col ^ f) * 16);
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q) {
+                        const uint4 h = {ph[q][4 * mm], ph[q][4 * mm + 1], ph[q][4 * mm + 2], ph[q][4 * mm + 3]};
+                        if (!bf16) {
+                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a),
+                                                                               __builtin_bit_cast(v8h, h), acc[c][q], 0, 0, 0);
+                        } else {
+                            const uint4 l = {pl[q][4 * mm], pl[q][4 * mm + 1], pl[q][4 * mm + 2], pl[q][4 * mm + 3]};
+                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a),
+                                                                                __builtin_bit_cast(v8bf, h), acc[c][q], 0, 0, 0);
+                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a),
+                                                                                __builtin_bit_cast(v8bf, l), acc[c][q], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- the row's sum over both halves, then the row itself or its partial
+    if (!busy) return;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        float a = l_run[q], b = l_run[q];
+        swap32(a, b);
+        const float l = a + b;
+        const int row = w_row0 + 32 * q + col;
+        const int tok = row / p.group;
+        const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
+        if (!whole) {
+            if (row < rows) {
+                const int64_t part = int64_t(split) * p.num_tokens * p.num_q_heads + out_row;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<float4*>(p.part_acc + part * D + 32 * c + 8 * i + 4 * half) =
+                            make_float4(acc[c][q][4 * i], acc[c][q][4 * i + 1], acc[c][q][4 * i + 2], acc[c][q][4 * i + 3]);
+                if (half == 0) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m_run[q], l);
+            }
+            continue;
+        }
+        const float inv = l > 0.f ? 1.0f / l : 0.f;   // a row that sees nothing is 0
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[c][q] *= inv;
+        if (p.rotate_v) wht_columns(acc, q, half);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x0 = acc[c][q][4 * i], x1 = acc[c][q][4 * i + 1], x2 = acc[c][q][4 * i + 2], x3 = acc[c][q][4 * i + 3];
+                const int64_t at = out_row * D + 32 * c + 8 * i + 4 * half;
+                if (row < rows) {
+                    if (p.out_dtype == 0) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(x0, x1, x2, x3);
+                    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(x0, x1), pack_bf16x2(x2, x3));
+                }
+            }
+    }
+}
+
+// Joins the partials of every (token, query head): 16 lanes per row, N channels
+// each.
+template <int D, int M>
+__global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
+    constexpr int N = D / 16;
+    const int L = threadIdx.x & 15;
+    const int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
+    const int t = int(row / p.num_q_heads);
+    if (t >= p.num_tokens) return;   // whole 16-lane rows
+    const int hq = int(row - int64_t(t) * p.num_q_heads);
+    // the sequence of token row t: the last that starts at or before it
+    int lo = 0, hi = p.batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (extend_first(p, mid) <= t) lo = mid; else hi = mid;
+    }
+    ExtendRows r;
+    r.b = lo;
+    r.first = extend_first(p, lo);
+    r.count = extend_first(p, lo + 1) - r.first;
+    if (t < r.first || t >= r.first + r.count) return;
+    r.n_ctx = extend_context(p, lo);
+    r.row0 = ((t - r.first) * p.group + hq % p.group) / M * M;
+    int plo, phi;
+    extend_span<M>(p, r, plo, phi);
+    extend_tiles(p, plo, phi, r);
+    const int per = extend_per_split(r.tiles, p.splits);
+    if (r.tiles <= per) return;   // written by the first launch
+    const int parts = (r.tiles + per - 1) / per;
+    const int64_t step = int64_t(p.num_tokens) * p.num_q_heads;
+    float m = -3e38f, l = 0.f, o[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < parts; ++s) {
+        const int64_t at = s * step + row;
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+        float a[N];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(p.part_acc + at * D + N * L + 4 * i);
+            a[4 * i] = v.x;
+            a[4 * i + 1] = v.y;
+            a[4 * i + 2] = v.z;
+            a[4 * i + 3] = v.w;
+        }
+        const float mn = __builtin_fmaxf(m, ml.x);
+        const float fo = __builtin_amdgcn_exp2f(m - mn), fn = __builtin_amdgcn_exp2f(ml.x - mn);
+        l = l * fo + ml.y * fn;
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = o[i] * fo + a[i] * fn;
+        m = mn;
+    }
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] *= inv;
+    if (p.rotate_v) wht_x<N>(o, L);
+    const int64_t at = row * D + N * L;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        if (p.out_dtype == 0)
+            *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at + 4 * i) =
+                make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        else
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at + 4 * i) =
+                make_uint2(pack_bf16x2(o[4 * i], o[4 * i + 1]), pack_bf16x2(o[4 * i + 2], o[4 * i + 3]));
+    }
+}
+
+template <int D, int NQ, int W>
+static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) {
+    const unsigned blocks = unsigned(int64_t(p.row_blocks) * p.num_kv_heads * p.splits);
+    launch_kernel(extend_kernel<D, NQ, W>, dim3(blocks), dim3(64 * W), stream, p);
+    if (p.splits > 1) {
+        const int64_t rows = int64_t(p.num_tokens) * p.num_q_heads;
+        hipLaunchKernelGGL((extend_merge_kernel<D, 32 * NQ * W>), dim3(unsigned((rows + 15) / 16)), dim3(256), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+int extend_block_rows(int) { return 128; }
+
+hipError_t launch_extend(const ExtendParams& p, hipStream_t stream) {
+    if (p.head_dim == 64) return launch_extend_with<64, 1, 4>(p, stream);
+    if (p.head_dim == 128) return launch_extend_with<128, 1, 4>(p, stream);
+    return launch_extend_with<256, 1, 4>(p, stream);
+}
+
+}  // namespace uq

@@ -28,6 +28,7 @@ struct TqTables {
     uint32_t lut[8];
 };
 constexpr int kNumCus = 256;     // compute units of an MI355X (8 XCDs x 32)
+constexpr int kPlanTokensBatch = 4096;   // sequences of a token plan (two sums in LDS)
 constexpr int kPlanBatch = 256;  // sequences a balanced split can hold
 // Granule of the balanced split in tokens: a page pair for each wave of a
 // 4-wave block (kFp4d64p2: two for every other wave).
@@ -146,6 +147,12 @@ struct DecodeParams {
     // the page-gather probe's checksums, one per wave of the partition
     // launch, sink[block * W + wave] (set only by launch_gather_probe)
     uint32_t* probe_sink;
+    // sliding window: the query sees the last `window` tokens of its context and
+    // the first `sinks` (0: all of them).  max_context, the partitions and
+    // num_partitions then count the visible pages (WindowView in uq_decode.hip)
+    int32_t window;
+    int32_t sinks;
+    int32_t context_bound;     // the caller's max_context
 };
 
 constexpr int kMaxErrorConstants = 256;   // constants per uq_quantize_error call
@@ -161,7 +168,83 @@ struct ErrorParams {
     double* sums;              // [num_c][2]: sum of squared errors, sum of squares (accumulated)
 };
 
+struct ExtendParams {
+    const void* q;             // [T][Hq][d] of q_dtype (0 f32, 1 bf16, 2 f16, 3 fp8), token stride q_stride
+    int32_t q_dtype;
+    int64_t q_stride;
+    int32_t num_tokens;
+    const int32_t* cu_seqlens;
+    int32_t batch;
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    int32_t group;
+    int32_t head_dim;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const int32_t* page_table;
+    int32_t max_pages_per_seq;
+    int64_t num_pages;
+    const int32_t* context_lens;
+    int32_t max_context;
+    int32_t window;            // 0: causal over the whole context
+    int32_t sinks;
+    float scale_log2;          // softmax_scale * log2(e)
+    int32_t rotate_v;
+    int32_t row_blocks;        // bound of the batch's row blocks per KV head
+    int32_t splits;            // blocks that share a row block's tiles
+    float* part_acc;           // [splits][T][Hq][d]
+    float* part_ml;            // [splits][T][Hq][2]
+    void* out;                 // [T][Hq][d]
+    int32_t out_dtype;         // 0 f32, 1 bf16
+};
+// Rows (query, query head of one KV head) of a block of the extend kernel.
+int extend_block_rows(int head_dim);
+hipError_t launch_extend(const ExtendParams& p, hipStream_t stream);
+
+struct PlanParams {
+    int32_t batch;
+    const int32_t* cached_lens;
+    const int32_t* new_lens;
+    const int32_t* free_pages;
+    int32_t num_free;
+    int32_t* page_table;
+    int32_t max_pages_per_seq;
+    int64_t num_tokens;
+    int32_t* context_lens;
+    int32_t* cu_seqlens;
+    int32_t* seq_ids;
+    int32_t* positions;
+    int64_t* slots;
+    int32_t* result;
+};
+
+struct NormRopeParams {
+    const void* q;
+    const void* k;
+    int64_t q_stride;          // elements between consecutive tokens
+    int64_t k_stride;
+    int32_t num_q_heads;
+    int32_t num_kv_heads;      // of k_out (no cache); the cache's come with QuantizeParams
+    int64_t num_tokens;
+    const float* q_weight;     // nullptr: no norm
+    const float* k_weight;
+    float eps;
+    const int32_t* positions;
+    const float* cos_sin;      // [max_position][rot]
+    int32_t max_position;
+    int32_t rot;
+    int32_t interleaved;
+    void* q_out;
+    void* k_out;               // without a cache
+    int32_t out_dtype;         // 0 f32, 1 bf16, 2 f16, 3 fp8 (queries, with a cache)
+    uint32_t q_blocks;         // blocks of the queries (set by the launcher)
+};
+
 hipError_t launch_quantize_kv(const QuantizeParams& p, int dtype, hipStream_t stream);
+hipError_t launch_plan_tokens(const PlanParams& p, hipStream_t stream);
+// c: the cache write of the keys and values (uq_norm_rope_write), or nullptr
+hipError_t launch_norm_rope(NormRopeParams p, const QuantizeParams* c, int head_dim, int dtype, hipStream_t stream);
+hipError_t launch_read_kv(const QuantizeParams& c, void* k_out, void* v_out, int dtype, hipStream_t stream);
 hipError_t launch_quantize_error(const ErrorParams& p, int dtype, hipStream_t stream);
 hipError_t launch_write_kv_ref(const RefWriteParams& p, int dtype, hipStream_t stream);
 hipError_t launch_prepare_query(const void* q, int dtype, int64_t rows, uint8_t* q8, hipStream_t stream);

@@ -171,11 +171,10 @@ __device__ __forceinline__ void wht128_x32(float (&x)[4][8], int L) { wht_quad<4
 // rounds x / 2^E_j to the nearest E2M1 level with ties to the even code,
 // saturates at 6 and keeps the sign (checked against a threshold encoder
 // over every tie, both zeros, subnormal inputs and scales 2^-127 .. 2^127).
-// `src` and `row` locate the vector's input (rows of dtype DT) for the
-// all-zero case.
-template <int DT, int NG>
+// `reload` gives the unrotated vector again, for the all-zero case.
+template <int NG, class RELOAD>
 __device__ __forceinline__ void quantize_xq(float (&x)[NG][8], int L, float c, bool rotate, uint32_t (&w)[NG],
-                                            uint32_t (&byte)[NG], const void* src, int64_t row) {
+                                            uint32_t (&byte)[NG], RELOAD reload) {
     if (rotate) wht_quad<NG>(x, L);
     float m[NG];
     float mall = 0.0f;
@@ -194,8 +193,7 @@ __device__ __forceinline__ void quantize_xq(float (&x)[NG][8], int L, float c, b
     // every rotated value zero (quad-uniform): the signs of the zeros, which
     // the codes keep, come from the plain form of the rotation
     if (rotate && __builtin_amdgcn_ballot_w64(mall == 0.0f) != 0 && mall == 0.0f) {
-#pragma unroll
-        for (int j = 0; j < NG; ++j) load_x8<DT>(src, row + 32 * j, x[j]);
+        reload(x);
         wht_quad_plain<NG>(x, L);
     }
 #pragma unroll
@@ -226,6 +224,34 @@ __device__ __forceinline__ uint8_t lane_byte(const uint32_t (&e)[NG], int q, int
     for (int j = 0; j < NG; ++j)
         if (j >> 2 == q) w |= e[j] << (8 * (j & 3));
     return uint8_t(w >> (8 * L));
+}
+
+// A quad's stores of one token at in-page offset `off`: one codes dword per
+// group, and the scale bytes of groups L, L + 4, ... (K tile: [group][token][16
+// bytes]; V tile: [token/4][channel/8][token%4][4 bytes]; scales
+// [group][token]).
+template <int NG>
+__device__ __forceinline__ void store_scales_quad(uint8_t* scales, int off, int L, const uint32_t (&byte)[NG]) {
+#pragma unroll
+    for (int q = 0; q < (NG + 3) / 4; ++q) {
+        const int j = L + 4 * q;
+        if (j < NG) scales[j * kPage + off] = lane_byte<NG>(byte, q, L);
+    }
+}
+template <int NG>
+__device__ __forceinline__ void store_k_quad(uint8_t* codes, uint8_t* scales, int off, int L, const uint32_t (&w)[NG],
+                                             const uint32_t (&byte)[NG]) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j) *reinterpret_cast<uint32_t*>(codes + (j * kPage + off) * 16 + 4 * L) = w[j];
+    store_scales_quad<NG>(scales, off, L, byte);
+}
+template <int NG>
+__device__ __forceinline__ void store_v_quad(uint8_t* codes, uint8_t* scales, int off, int L, const uint32_t (&w)[NG],
+                                             const uint32_t (&byte)[NG]) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+        *reinterpret_cast<uint32_t*>(codes + ((off >> 2) * (4 * NG) + 4 * j + L) * 16 + (off & 3) * 4) = w[j];
+    store_scales_quad<NG>(scales, off, L, byte);
 }
 
 // The page and in-page offset of a slot; false for a slot that is skipped
@@ -292,25 +318,15 @@ __global__ void __launch_bounds__(256) quantize_kv_kernel(QuantizeParams p) {
     uint32_t wk[NG], wv[NG], bk[NG], bv[NG];
     const int64_t ph = page * p.num_kv_heads + h;
     uint8_t* kc = p.codes + ph * (16 * D);
-    uint8_t* vc = kc + 8 * D;
     uint8_t* ks = p.scales + ph * D;
-    quantize_xq<DT, NG>(xk, L, p.c, true, wk, bk, p.k, row);
+    auto rows = [&](const void* base, float (&y)[NG][8]) {
 #pragma unroll
-    for (int j = 0; j < NG; ++j) *reinterpret_cast<uint32_t*>(kc + (j * kPage + off) * 16 + 4 * L) = wk[j];
-#pragma unroll
-    for (int q = 0; q < (NG + 3) / 4; ++q) {
-        const int j = L + 4 * q;
-        if (j < NG) ks[j * kPage + off] = lane_byte<NG>(bk, q, L);
-    }
-    quantize_xq<DT, NG>(xv, L, p.c, p.rotate_v != 0, wv, bv, p.v, row);
-#pragma unroll
-    for (int j = 0; j < NG; ++j)
-        *reinterpret_cast<uint32_t*>(vc + ((off >> 2) * (D / 8) + 4 * j + L) * 16 + (off & 3) * 4) = wv[j];
-#pragma unroll
-    for (int q = 0; q < (NG + 3) / 4; ++q) {
-        const int j = L + 4 * q;
-        if (j < NG) ks[D / 2 + j * kPage + off] = lane_byte<NG>(bv, q, L);
-    }
+        for (int j = 0; j < NG; ++j) load_x8<DT>(base, row + 32 * j, y[j]);
+    };
+    quantize_xq<NG>(xk, L, p.c, true, wk, bk, [&](float (&y)[NG][8]) { rows(p.k, y); });
+    store_k_quad<NG>(kc, ks, off, L, wk, bk);
+    quantize_xq<NG>(xv, L, p.c, p.rotate_v != 0, wv, bv, [&](float (&y)[NG][8]) { rows(p.v, y); });
+    store_v_quad<NG>(kc + 8 * D, ks + D / 2, off, L, wv, bv);
 }
 
 // Quantize-on-write at head size 256 for small writes: 16 lanes per (token, kv
@@ -653,3 +669,6 @@ hipError_t launch_prepare_query(const void* q, int dtype, int64_t rows, uint8_t*
 }
 
 }  // namespace uq
+
+#include "uq_plan.hpp"
+#include "uq_rows.hpp"

@@ -41,7 +41,8 @@ EXPORTS = (
     "uq_decode_cascade_partials", "uq_decode_cascade_merge", "uq_ref_decode_cascade",
     "uq_ref_decode_cascade_partials", "uq_ref_decode_cascade_merge", "uq_quantize_error", "uq_time_next_launch",
     "uq_decode_attention_noalloc", "uq_decode_attention_scaled_pv", "uq_probe_stream_read", "uq_probe_page_gather",
-    "uq_probe_page_gather_cascade", "uq_probe_mfma",
+    "uq_probe_page_gather_cascade", "uq_probe_mfma", "uq_plan_tokens", "uq_norm_rope", "uq_norm_rope_write", "uq_read_kv",
+    "uq_extend_workspace_bytes", "uq_extend_attention", "uq_decode_window_workspace_bytes", "uq_decode_window",
 )
 
 UQ_REF_FP8_E4M3, UQ_REF_BF16, UQ_REF_TQ4 = 1, 2, 3
@@ -84,6 +85,19 @@ class uq_shared_prefix(ctypes.Structure):
         ("lens", ctypes.c_void_p),
         ("num_tokens", ctypes.c_int32),
         ("partition_tokens", ctypes.c_int32),
+    ]
+
+
+class uq_norm_rope_desc(ctypes.Structure):
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+        ("positions", ctypes.c_void_p),
+        ("cos_sin", ctypes.c_void_p),
+        ("max_position", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
     ]
 
 
@@ -163,6 +177,25 @@ def _load():
         fn = getattr(L, name)
         fn.argtypes = [R, vp, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, i32, f32, i32, vp, sz, vp, i32, vp]
         fn.restype = i32
+    N = ctypes.POINTER(uq_norm_rope_desc)
+    L.uq_plan_tokens.argtypes = [i32, vp, vp, vp, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.uq_plan_tokens.restype = i32
+    L.uq_norm_rope.argtypes = [N, i32, vp, i64, i32, vp, i64, i32, i32, i64, vp, vp, i32, vp]
+    L.uq_norm_rope.restype = i32
+    L.uq_norm_rope_write.argtypes = [D, N, vp, i64, i32, vp, vp, i64, i32, i64, vp, i32, vp, i32, i32, vp, vp, vp, vp]
+    L.uq_norm_rope_write.restype = i32
+    L.uq_read_kv.argtypes = [D, vp, vp, vp, i32, i32, vp, i64, vp, vp, i32, vp]
+    L.uq_read_kv.restype = i32
+    L.uq_extend_workspace_bytes.argtypes = [D, i64, i32, i32, i32, i32, i32]
+    L.uq_extend_workspace_bytes.restype = sz
+    L.uq_extend_attention.argtypes = [D, vp, i32, i64, i64, vp, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, f32, vp, sz,
+                                      vp, i32, vp]
+    L.uq_extend_attention.restype = i32
+    L.uq_decode_window_workspace_bytes.argtypes = [D, i32, i32, i32, i32, i32, i32]
+    L.uq_decode_window_workspace_bytes.restype = sz
+    L.uq_decode_window.argtypes = [D, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, f32, i32, vp,
+                                   sz, vp, i32, vp]
+    L.uq_decode_window.restype = i32
     return L
 
 
@@ -529,6 +562,234 @@ def decode_merge(desc: CacheDesc, batch, num_q_heads, context_lens, max_context,
     st = lib.uq_decode_merge(ctypes.byref(d), batch, num_q_heads, _ptr(context_lens), max_context, partition_tokens,
                              _ptr(workspace), workspace.numel(), _ptr(out), _DT[out.dtype], _stream(stream))
     _check(st, "uq_decode_merge")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Around the cache: token plans, norm and position rotation, reading back,
+# attention of several new queries per sequence, sliding windows
+
+
+@dataclass
+class TokenPlan:
+    """Outputs of plan_tokens: the lengths, slots and positions of one step
+    (``include/uq.h``), reusable from step to step."""
+    context_lens: torch.Tensor   # int32 [batch]
+    cu_seqlens: torch.Tensor     # int32 [batch + 1]
+    seq_ids: torch.Tensor        # int32 [num_tokens]
+    positions: torch.Tensor      # int32 [num_tokens]
+    slots: torch.Tensor          # int64 [num_tokens]
+    result: torch.Tensor         # int32 [3]: rows in use, pages taken, sequences refused
+
+    @classmethod
+    def alloc(cls, batch, num_tokens, device="cuda"):
+        def i32(n):
+            return torch.empty(n, dtype=torch.int32, device=device)
+        return cls(i32(batch), i32(batch + 1), i32(num_tokens), i32(num_tokens),
+                   torch.empty(num_tokens, dtype=torch.int64, device=device), i32(3))
+
+
+def plan_tokens(cached_lens, new_lens, free_pages, page_table, plan: TokenPlan, stream=None):
+    """Pages, slots and positions of one step from its lengths: fills `plan`
+    and the new entries of `page_table` (int32 [batch, max_pages_per_seq]),
+    taking pages from the front of `free_pages` (int32)."""
+    _need(cached_lens, "cached_lens", _I32, (None,))
+    B = cached_lens.shape[0]
+    _need(new_lens, "new_lens", _I32, (B,))
+    _need(free_pages, "free_pages", _I32, (None,))
+    _need(page_table, "page_table", _I32, (B, None))
+    _need(plan.slots, "plan.slots", (torch.int64,), (None,))
+    T = plan.slots.shape[0]
+    _need(plan.context_lens, "plan.context_lens", _I32, (B,))
+    _need(plan.cu_seqlens, "plan.cu_seqlens", _I32, (B + 1,))
+    _need(plan.seq_ids, "plan.seq_ids", _I32, (T,))
+    _need(plan.positions, "plan.positions", _I32, (T,))
+    _need(plan.result, "plan.result", _I32, (3,))
+    st = lib.uq_plan_tokens(B, _ptr(cached_lens), _ptr(new_lens), _ptr(free_pages), free_pages.shape[0],
+                            _ptr(page_table), page_table.shape[1], T, _ptr(plan.context_lens), _ptr(plan.cu_seqlens),
+                            _ptr(plan.seq_ids), _ptr(plan.positions), _ptr(plan.slots), _ptr(plan.result),
+                            _stream(stream))
+    _check(st, "uq_plan_tokens")
+    return plan
+
+
+@dataclass
+class NormRope:
+    """Mirror of ``uq_norm_rope_desc``: `positions` int32 [T], `cos_sin`
+    float32 [max_position, rot_dim] (cosines, then sines; None: no rotation),
+    weights float32 [head_dim] or None (no norm)."""
+    positions: torch.Tensor = None
+    cos_sin: torch.Tensor = None
+    q_weight: torch.Tensor = None
+    k_weight: torch.Tensor = None
+    eps: float = 1e-6
+    interleaved: bool = False
+
+    def c_struct(self, num_tokens, head_dim):
+        rot = 0
+        if self.cos_sin is not None:
+            _need(self.cos_sin, "cos_sin", (torch.float32,), (None, None))
+            _need(self.positions, "positions", _I32, (num_tokens,))
+            rot = self.cos_sin.shape[1]
+        for w, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+            if w is not None:
+                _need(w, name, (torch.float32,), (head_dim,))
+        return uq_norm_rope_desc(_ptr(self.q_weight), _ptr(self.k_weight), self.eps,
+                                 _ptr(self.positions) if rot else None, _ptr(self.cos_sin),
+                                 self.cos_sin.shape[0] if rot else 0, rot, int(bool(self.interleaved)))
+
+
+def _head_rows(t, name, dtypes, shape):
+    """Rows [T, heads, head_dim] with contiguous heads and channels; returns
+    the token stride in elements."""
+    _need(t, name, dtypes, shape, contiguous=False)
+    T, H, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: heads and channels of a token must be contiguous")
+    return t.stride(0) if T > 1 else H * d
+
+
+def norm_rope(spec: NormRope, q, k=None, q_out=None, k_out=None, out_dtype=None, stream=None):
+    """Per-head norm and position rotation of q [T, Hq, d] and k [T, Hkv, d]
+    (strided token rows allowed) -> (q_out, k_out), contiguous rows of
+    `out_dtype` (default: the input's)."""
+    q_stride = _head_rows(q, "q", _ROWS, (None, None, None))
+    T, Hq, d = q.shape
+    out_dtype = out_dtype or (q.dtype if q_out is None else q_out.dtype)
+    if q_out is None:
+        q_out = torch.empty((T, Hq, d), dtype=out_dtype, device=q.device)
+    _need(q_out, "q_out", _ROWS, (T, Hq, d))
+    k_stride, Hkv = 0, 0
+    if k is not None:
+        k_stride = _head_rows(k, "k", (q.dtype,), (T, None, d))
+        Hkv = k.shape[1]
+        if k_out is None:
+            k_out = torch.empty((T, Hkv, d), dtype=q_out.dtype, device=q.device)
+        _need(k_out, "k_out", (q_out.dtype,), (T, Hkv, d))
+    elif k_out is not None:
+        raise ValueError("k_out: given without k")
+    s = spec.c_struct(T, d)
+    st = lib.uq_norm_rope(ctypes.byref(s), d, _ptr(q), q_stride, Hq, _ptr(k), k_stride, Hkv, _DT[q.dtype], T,
+                          _ptr(q_out), _ptr(k_out), _DT[q_out.dtype], _stream(stream))
+    _check(st, "uq_norm_rope")
+    return q_out, k_out
+
+
+def norm_rope_write(desc: CacheDesc, spec: NormRope, q, k, v, slot_mapping, codes, scales, q_out=None,
+                    q_out_dtype=torch.uint8, page_table=None, max_pages_per_seq=0, stream=None):
+    """norm_rope with the cache behind it: k and v [T, Hkv, d] go into the
+    pools at `slot_mapping`; returns the queries, prepared FP8 bytes
+    (uint8, the default) or rows."""
+    num_seqs, mpps = _write_table(page_table, max_pages_per_seq)
+    d = desc.head_dim
+    q_stride = _head_rows(q, "q", _ROWS, (None, None, d))
+    T, Hq = q.shape[0], q.shape[1]
+    kv_stride = _head_rows(k, "k", (q.dtype,), (T, desc.num_kv_heads, d))
+    if _head_rows(v, "v", (q.dtype,), (T, desc.num_kv_heads, d)) != kv_stride:
+        raise ValueError("k and v: one token stride expected")
+    _need(slot_mapping, "slot_mapping", (torch.int64,), (T,))
+    _pools(desc, codes, scales)
+    if q_out is None:
+        q_out = torch.empty((T, Hq, d), dtype=q_out_dtype, device=q.device)
+    _need(q_out, "q_out", _QUERY, (T, Hq, d))
+    s, c = spec.c_struct(T, d), desc.c_struct()
+    st = lib.uq_norm_rope_write(ctypes.byref(c), ctypes.byref(s), _ptr(q), q_stride, Hq, _ptr(k), _ptr(v), kv_stride,
+                                _DT[q.dtype], T, _ptr(q_out), _DT[q_out.dtype], _ptr(page_table), num_seqs, mpps,
+                                _ptr(slot_mapping), _ptr(codes), _ptr(scales), _stream(stream))
+    _check(st, "uq_norm_rope_write")
+    return q_out
+
+
+def read_kv(desc: CacheDesc, slot_mapping, codes, scales, page_table=None, max_pages_per_seq=0, k_out=None, v_out=None,
+            out_dtype=torch.bfloat16, stream=None):
+    """Stored tokens as rows [T, Hkv, d]: (k_out, v_out), rotated back.  Rows
+    of skipped slots are left as they were (zero in tensors made here)."""
+    num_seqs, mpps = _write_table(page_table, max_pages_per_seq)
+    _need(slot_mapping, "slot_mapping", (torch.int64,), (None,))
+    shape = (slot_mapping.shape[0], desc.num_kv_heads, desc.head_dim)
+    _pools(desc, codes, scales)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.zeros(shape, dtype=out_dtype, device=codes.device) for _ in range(2))
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None:
+            _need(t, name, _ROWS, shape)
+    if k_out is not None and v_out is not None and k_out.dtype != v_out.dtype:
+        raise ValueError("k_out and v_out: one dtype expected")
+    d = desc.c_struct()
+    st = lib.uq_read_kv(ctypes.byref(d), _ptr(codes), _ptr(scales), _ptr(page_table), num_seqs, mpps,
+                        _ptr(slot_mapping), shape[0], _ptr(k_out), _ptr(v_out),
+                        _DT[(v_out if k_out is None else k_out).dtype], _stream(stream))
+    _check(st, "uq_read_kv")
+    return k_out, v_out
+
+
+def extend_workspace_bytes(desc: CacheDesc, num_tokens, batch, num_q_heads, max_context, window=0, sinks=0):
+    d = desc.c_struct()
+    return int(lib.uq_extend_workspace_bytes(ctypes.byref(d), num_tokens, batch, num_q_heads, max_context, window, sinks))
+
+
+def extend_attention(desc: CacheDesc, q, cu_seqlens, codes, scales, page_table, context_lens, max_context, window=0,
+                     sinks=0, softmax_scale=None, workspace=None, out=None, out_dtype=torch.bfloat16, stream=None):
+    """Attention of the step's new tokens, in the cache already: q [T, Hq, d]
+    (rows, or prepared FP8 bytes) -> out [T, Hq, d].  cu_seqlens int32
+    [batch + 1]; window 0: causal over the whole context."""
+    q_stride = _head_rows(q, "q", _QUERY, (None, None, desc.head_dim))
+    T, Hq = q.shape[0], q.shape[1]
+    _need(cu_seqlens, "cu_seqlens", _I32, (None,))
+    B = cu_seqlens.shape[0] - 1
+    _pools(desc, codes, scales)
+    _table(page_table, context_lens, B)
+    if softmax_scale is None:
+        softmax_scale = desc.head_dim ** -0.5
+    d = desc.c_struct()
+    if workspace is None:
+        n = lib.uq_extend_workspace_bytes(ctypes.byref(d), T, B, Hq, max_context, window, sinks)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", _U8)
+    if out is None:
+        out = torch.zeros((T, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+    _need(out, "out", _OUT, (T, Hq, desc.head_dim))
+    st = lib.uq_extend_attention(ctypes.byref(d), _ptr(q), _DT[q.dtype], q_stride, T, _ptr(cu_seqlens), B, Hq,
+                                 _ptr(codes), _ptr(scales), _ptr(page_table), page_table.shape[1], _ptr(context_lens),
+                                 max_context, window, sinks, softmax_scale, _ptr(workspace), workspace.numel(),
+                                 _ptr(out), _DT[out.dtype], _stream(stream))
+    _check(st, "uq_extend_attention")
+    return out
+
+
+def decode_window_workspace_bytes(desc: CacheDesc, batch, num_q_heads, max_context, window, sinks=0,
+                                  partition_tokens=0):
+    d = desc.c_struct()
+    return int(lib.uq_decode_window_workspace_bytes(ctypes.byref(d), batch, num_q_heads, max_context, window, sinks,
+                                                    partition_tokens))
+
+
+def decode_window(desc: CacheDesc, q, codes, scales, page_table, context_lens, max_context, window, sinks=0,
+                  k_new=None, v_new=None, softmax_scale=None, partition_tokens=0, workspace=None, out=None,
+                  out_dtype=torch.float32, q_dtype=None, stream=None):
+    """decode_attention (or decode_step, with k_new and v_new) where the query
+    sees the last `window` tokens and the first `sinks`."""
+    B, Hq = _q_out(q, out, desc.head_dim)
+    _pools(desc, codes, scales)
+    _table(page_table, context_lens, B)
+    if k_new is not None or v_new is not None:
+        _new_token(k_new, v_new, B, desc.num_kv_heads)
+    if softmax_scale is None:
+        softmax_scale = desc.head_dim ** -0.5
+    if workspace is None:
+        n = decode_window_workspace_bytes(desc, B, Hq, max_context, window, sinks, partition_tokens)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", _U8)
+    if out is None:
+        out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+    d = desc.c_struct()
+    qdt = _DT[q.dtype] if q_dtype is None else q_dtype
+    st = lib.uq_decode_window(ctypes.byref(d), _ptr(q), qdt, _ptr(k_new), _ptr(v_new),
+                              UQ_F32 if k_new is None else _DT[k_new.dtype], B, Hq, _ptr(codes), _ptr(scales),
+                              _ptr(page_table), page_table.shape[1], _ptr(context_lens), max_context, window, sinks,
+                              softmax_scale, partition_tokens, _ptr(workspace), workspace.numel(), _ptr(out),
+                              _DT[out.dtype], _stream(stream))
+    _check(st, "uq_decode_window")
     return out
 
 
