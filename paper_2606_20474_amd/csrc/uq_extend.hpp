@@ -6,7 +6,7 @@
 // n - m + i, and G query heads per KV head, a row is a (query, head of the KV
 // head) pair, row r = query r / G, head r % G: all rows of a (sequence, KV head)
 // read the same keys and values, so a block takes M of them and walks the
-// visible context once in tiles of 64 tokens (4 pages).
+// visible context once in tiles of 64 tokens.
 //
 //   scores    S^T = K Q^T on v_mfma_scale_f32_32x32x64_f8f6f4: FP4 keys with
 //             their scale bytes as operand A (rows = tokens), the rotated FP8
@@ -21,10 +21,12 @@
 //             order), so P stays in registers.  V is decoded once per block and
 //             tile into FP16 in LDS, transposed to operand order.
 //
-// FP16 holds a code times 2^E exactly for E in [-23, 13], and P with 11
-// significant bits; a tile with a scale outside that range (|V| from 2^16 on, or a
-// group below 2^-22) takes BF16 values and P as two BF16 terms instead, as
-// decode_kernel does.
+// FP16 holds P with 11 significant bits and a code times 2^E exactly for E in
+// [-23, 13].  So the values of each block of 32 channels are taken relative to an
+// exponent of their own, v 2^-e, and the accumulators hold O 2^-e: e is 8 below the
+// largest scale exponent when it is set (in the first tile), and set again, the
+// accumulators rescaled, when a tile's largest passes e + 13.  Values more than
+// 2^31 below the largest of their 32 channels that the block has seen are lost.
 #pragma once
 
 #include "uq_device.hpp"
@@ -36,7 +38,10 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
-constexpr int kTile = 64;   // tokens per tile
+constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
+
+// Tokens per tile: 4 pages, 2 at head size 256 (two blocks fit a CU's LDS then).
+template <int D> constexpr int extend_tile() { return D == 256 ? 32 : 64; }
 
 // Where a block's rows stand and which tiles they see.
 struct ExtendRows {
@@ -50,16 +55,17 @@ struct ExtendRows {
 };
 
 // Tiles that rows with positions lo .. hi see.
+template <int TT>
 __device__ __forceinline__ void extend_tiles(const ExtendParams& p, int lo, int hi, ExtendRows& r) {
     const int end = hi + 1;
-    const int last = end > 0 ? (end + kTile - 1) / kTile : 0;
+    const int last = end > 0 ? (end + TT - 1) / TT : 0;
     r.sink_tiles = 0;
     r.tile0 = 0;
     if (p.window > 0) {
         const int from = lo - p.window + 1;   // the first row's window, the earliest
-        r.tile0 = from > 0 ? from / kTile : 0;
+        r.tile0 = from > 0 ? from / TT : 0;
         const int sinks = p.sinks < end ? p.sinks : end;
-        r.sink_tiles = sinks > 0 ? (sinks + kTile - 1) / kTile : 0;
+        r.sink_tiles = sinks > 0 ? (sinks + TT - 1) / TT : 0;
         if (r.sink_tiles >= r.tile0) r.sink_tiles = r.tile0 = 0;
     }
     r.tiles = r.sink_tiles + (last > r.tile0 ? last - r.tile0 : 0);
@@ -106,7 +112,7 @@ __device__ __forceinline__ bool extend_find(const ExtendParams& p, int at, Exten
             const int n = __builtin_amdgcn_readlane(blocks, l);
             const int i = at - before - (__builtin_amdgcn_readlane(sum, l) - n);
             r.row0 = (n - 1 - i) * M;
-            r.n_ctx = extend_context(p, r.b);
+            r.n_ctx = __builtin_amdgcn_readfirstlane(extend_context(p, r.b));
             return true;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
@@ -122,9 +128,8 @@ __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendR
     hi = r.n_ctx - r.count + last / p.group;
 }
 
-// One 16-byte unit of a page's V codes (4 tokens x 8 channels) as eight pairs of
-// dwords: of each channel the 4 tokens in FP16 (H) or BF16.
-template <bool H>
+// One 16-byte unit of a page's V codes (4 tokens x 8 channels, their scale bytes in
+// `scale_bytes`) as eight pairs of dwords: of each channel the 4 tokens in FP16.
 __device__ __forceinline__ void decode_unit(const uint4& v, uint32_t scale_bytes, uint2 (&out)[8]) {
     float sc[4];
 #pragma unroll
@@ -133,17 +138,10 @@ __device__ __forceinline__ void decode_unit(const uint4& v, uint32_t scale_bytes
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const uint32_t d = t == 0 ? v.x : t == 1 ? v.y : t == 2 ? v.z : v.w;
-        if constexpr (H) {
-            w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 0));
-            w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 1));
-            w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 2));
-            w[t][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 3));
-        } else {
-            w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 0));
-            w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 1));
-            w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 2));
-            w[t][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, sc[t], 3));
-        }
+        w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 0));
+        w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 1));
+        w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 2));
+        w[t][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 3));
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -206,25 +204,36 @@ __host__ __device__ __forceinline__ int extend_per_split(int tiles, int splits) 
     return per > 2 ? per : 2;
 }
 
-// The rows of a (sequence, KV head) pair: NQ blocks of 32 rows per wave, W waves.
+// One block's walk: NQ blocks of 32 rows per wave, W waves.  Per tile a thread
+// moves one or two 16-byte units of K and of V: loaded into registers while the
+// tile before is computed (the page ids one tile earlier still), stored to the
+// other of two LDS buffers after it, K as it is and V decoded; one barrier per
+// tile.
 template <int D, int NQ, int W>
 __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
+    constexpr int TT = extend_tile<D>();
     constexpr int M = 32 * NQ * W;            // rows of the block
     constexpr int NT = 64 * W;
     constexpr int KS = D / 64;                // k steps of QK^T
     constexpr int CB = D / 32;                // channel blocks of PV
     constexpr int N = D / 16;                 // channels per lane of a 16-lane row
-    constexpr int kUnits = 2 * D;             // 16-byte units of a tile's K, and of its V
+    constexpr int kPageUnits = D / 2;         // 16-byte units of a page's K, and of its V
+    constexpr int kUnits = TT / kPage * kPageUnits;
     constexpr int UR = (kUnits + NT - 1) / NT;
-    constexpr int kPageUnits = D / 2;
-    constexpr int kPageScales = D;            // scale bytes of a page and KV head, K then V
-    constexpr int kVt = kTile * D * 2;        // decoded values of a tile
-    constexpr int kK = kTile * D / 2;         // K codes of a tile
+    // decoded values of a tile: [page][32 channels][half][channel][8 tokens], the
+    // (channel block, half) rows 16 bytes apart in banks, so that neither the stores
+    // (8 bytes per channel) nor the loads (16 bytes per lane) meet in a bank
+    constexpr int kVRow = 32 * 16 + 16;
+    constexpr int kVt = TT / kPage * CB * 2 * kVRow;
+    constexpr int kK = TT * D / 2;            // K codes of a tile
     __shared__ __attribute__((aligned(16))) uint8_t vt[2][kVt];
     __shared__ __attribute__((aligned(16))) uint8_t kt[2][kK];
-    __shared__ __attribute__((aligned(16))) uint8_t kst[2][4 * D / 2];
-    __shared__ int wide[2];                   // a scale outside FP16's range in the tile
+    __shared__ __attribute__((aligned(16))) uint8_t kst[2][TT / kPage * D / 2];
+    __shared__ int grow[2];                   // a scale above FP16's range in the tile
+    __shared__ int top[CB];                   // largest scale byte of the tile, per 32 channels (when one grows)
+    __shared__ int base[CB];                  // scale byte the values are relative to: 127 + e
     static_assert(M * D <= 2 * kVt, "the query operand is staged in the value buffers");
+    static_assert(kUnits % 64 == 0 && kUnits % NT % 64 == 0, "units go to whole waves");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -236,7 +245,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     if (!extend_find<M>(p, rest / p.splits, r)) return;
     int lo, hi;
     extend_span<M>(p, r, lo, hi);
-    extend_tiles(p, lo, hi, r);
+    extend_tiles<TT>(p, lo, hi, r);
     int first_tile = 0, last_tile = r.tiles;
     bool whole = true;
     if (p.splits > 1) {
@@ -244,7 +253,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         whole = r.tiles <= per;
         first_tile = split * per;
         last_tile = first_tile + per < r.tiles ? first_tile + per : r.tiles;
-        if (first_tile >= last_tile && !(split == 0)) return;
+        if (first_tile >= last_tile && split != 0) return;
     }
     const int rows = r.count * p.group;       // of the sequence and KV head
 
@@ -253,15 +262,15 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // 64 s + 16 half .., 16..31 are 64 s + 32 + 16 half ..
     uint8_t* qs = &vt[0][0] + wave * (32 * NQ * D);
     const int L = lane & 15;
-#pragma unroll 4
+#pragma unroll 2
     for (int i = 0; i < 8 * NQ; ++i) {
         const int rr = 4 * i + (lane >> 4);                       // row of the wave
         const int row = r.row0 + wave * (32 * NQ) + rr;
         uint32_t w[N / 4];
 #pragma unroll
         for (int j = 0; j < N / 4; ++j) w[j] = 0u;
-        const int tok = row / p.group;
         if (row < rows) {
+            const int tok = int(unsigned(row) / unsigned(p.group));
             const int64_t elem = int64_t(r.first + tok) * p.q_stride + int64_t(hk * p.group + row - tok * p.group) * D + N * L;
             if (p.q_dtype == 3) {
                 const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.q) + elem);
@@ -288,7 +297,11 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             *reinterpret_cast<uint32_t*>(qs + dst) = w[j];
         }
     }
-    if (tid < 2) wide[tid] = 0;
+    if (tid < 2) grow[tid] = 0;
+    if (tid < CB) {
+        top[tid] = 0;
+        base[tid] = kNoBase;
+    }
     __syncthreads();
     v8i qop[NQ][KS];
 #pragma unroll
@@ -301,88 +314,120 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         }
     __syncthreads();
 
-    // this lane's rows: position, and the first token of the window
+    // position of this lane's rows
+    const int w_row0 = r.row0 + wave * (32 * NQ);
     int pos[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-        const int row = r.row0 + wave * (32 * NQ) + 32 * q + col;
-        pos[q] = row < rows ? r.n_ctx - r.count + row / p.group : -1;
+        const int row = w_row0 + 32 * q + col;
+        pos[q] = row < rows ? r.n_ctx - r.count + int(unsigned(row) / unsigned(p.group)) : -1;
     }
-    // the wave's first and last position (waves without rows: nothing to do)
-    const int w_row0 = r.row0 + wave * (32 * NQ);
+    // the wave's first and last position (a wave without rows only moves tiles)
     const bool busy = w_row0 < rows;
     const int w_last = w_row0 + 32 * NQ < rows ? w_row0 + 32 * NQ - 1 : rows - 1;
     const int w_lo = r.n_ctx - r.count + w_row0 / p.group, w_hi = r.n_ctx - r.count + w_last / p.group;
 
-    const int64_t heads = p.num_kv_heads;
     const int32_t* pt_row = p.page_table + int64_t(r.b) * p.max_pages_per_seq;
-    const int n_pages = (hi + kPage) / kPage;   // pages that hold a token a row sees, or earlier
-    auto token_of = [&](int t) { return kTile * (t < r.sink_tiles ? t : t - r.sink_tiles + r.tile0); };
-    auto page_id = [&](int tile, int pg) -> int64_t {
-        const int v = token_of(tile) / kPage + pg;
-        int32_t id = 0;
-        if (v < n_pages) id = pt_row[v];
-        return clamp_ids(id, p.num_pages);
+    const int n_pages = (hi + kPage) / kPage;   // pages up to the last that holds a visible token
+    auto token_of = [&](int t) { return TT * (t < r.sink_tiles ? t : t - r.sink_tiles + r.tile0); };
+
+    // ---- this thread's part of a tile: unit tid + u NT, `in` of its page; the first
+    // D / 8 units of a page also move 4 of its K scales each.  A page takes whole
+    // waves from head size 128 on: its id and addresses are scalars then.
+    int32_t ids[UR];
+    uint4 kcode[UR], vcode[UR];
+    uint32_t vscale[UR], kscale[UR];
+    int my_base = kNoBase;      // base[] of its units' channels
+    constexpr bool kWavePages = kPageUnits % 64 == 0;
+    // The lane, computed anew in each tile: addresses that follow from it are then
+    // made where they are used instead of living in registers through the walk (with
+    // them the accumulators did not fit, and every spilled one waited for the
+    // loads of the next tile).
+    auto fresh_lane = [&]() {
+        unsigned l = unsigned(lane);
+        asm volatile("" : "+v"(l));
+        return l;
     };
-    // this thread's units of a tile: V codes and scales into registers, K codes and
-    // scales into LDS
-    uint4 vcode[UR];
-    uint32_t vscale[UR];
-    auto load_tile = [&](int tile, int slot) {
+    auto unit_page = [&](unsigned l, int u) {
+        return kWavePages ? (64 * wave + u * NT) / kPageUnits : int(64 * wave + u * NT + l) / kPageUnits;
+    };
+    auto unit_in = [&](unsigned l, int u) {
+        return kWavePages ? unsigned((64 * wave + u * NT) % kPageUnits) + l : (64u * wave + u * NT + l) % kPageUnits;
+    };
+    auto has_unit = [&](int u) { return (u + 1) * NT <= kUnits || 64 * wave + u * NT < kUnits; };   // whole waves
+    auto load_ids = [&](int tile) {
+        const unsigned l = fresh_lane();
+        const int page0 = token_of(tile) / kPage;
 #pragma unroll
         for (int u = 0; u < UR; ++u) {
-            const int unit0 = 64 * wave + u * NT, unit = unit0 + lane;
-            if (unit0 < kUnits) {   // whole waves
-                const int in = unit % kPageUnits;
-                const int64_t ph = page_id(tile, unit / kPageUnits) * heads + hk;
-                const uint8_t* codes = p.codes + ph * (16 * D);
-                __builtin_amdgcn_global_load_lds(codes + 16 * in,
-                                                 (lds_ptr_t)(&kt[slot][0] + 16 * unit0), 16, 0, 0);
-                vcode[u] = *reinterpret_cast<const uint4*>(codes + 8 * D + 16 * in);
-                const int tq = in / (D / 8), oct = in % (D / 8);
-                vscale[u] = *reinterpret_cast<const uint32_t*>(p.scales + ph * kPageScales + D / 2 + (oct >> 2) * 16 + 4 * tq);
-            }
-        }
-        if (wave == W - 1 && lane < D / 8) {
-            const int64_t ph = page_id(tile, lane / (D / 32)) * heads + hk;
-            __builtin_amdgcn_global_load_lds(p.scales + ph * kPageScales + 16 * (lane % (D / 32)), (lds_ptr_t)&kst[slot][0],
-                                             16, 0, 0);
+            // (pages past the last visible token's: that one again, masked)
+            const int v = page0 + unit_page(l, u);
+            ids[u] = pt_row[v < n_pages ? v : n_pages - 1];
         }
     };
-    // decode this thread's units into the value buffer
-    auto store_units = [&](int tile, int slot, bool bf16) {
+    auto load_tile = [&]() {
+        const unsigned l = fresh_lane();
 #pragma unroll
         for (int u = 0; u < UR; ++u) {
-            const int unit = tid + u * NT;
-            if (unit >= kUnits) continue;
-            const int pg = unit / kPageUnits, in = unit % kPageUnits;
-            const int tq = in / (D / 8), oct = in % (D / 8);
-            // tokens no row of the block sees may hold anything: zero scale
-            const int tok = token_of(tile) + kPage * pg + 4 * tq;
-            uint32_t sc = vscale[u];
-            if (tok + 4 > hi + 1 || (p.window > 0 && tok <= lo - p.window && tok + 4 > p.sinks)) {
+            if (!has_unit(u)) continue;
+            const int32_t id = clamp_ids(kWavePages ? __builtin_amdgcn_readfirstlane(ids[u]) : ids[u], p.num_pages);
+            const int64_t ph = int64_t(id) * p.num_kv_heads + hk;
+            const unsigned in = unit_in(l, u);
+            const uint8_t* codes = p.codes + ph * (16 * D);
+            const uint8_t* scales = p.scales + ph * D;
+            kcode[u] = *reinterpret_cast<const uint4*>(codes + 16 * in);
+            vcode[u] = *reinterpret_cast<const uint4*>(codes + 8 * D + 16 * in);
+            vscale[u] = *reinterpret_cast<const uint32_t*>(scales + D / 2 + (in % (D / 8) >> 2) * 16 + 4 * (in / (D / 8)));
+            if (in < D / 8) kscale[u] = *reinterpret_cast<const uint32_t*>(scales + 4 * in);
+        }
+    };
+    auto store_k = [&](int slot) {
+        const unsigned l = fresh_lane();
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (tok + t > hi || (p.window > 0 && tok + t <= lo - p.window && tok + t >= p.sinks)) sc &= ~(0xFFu << (8 * t));
+        for (int u = 0; u < UR; ++u) {
+            if (!has_unit(u)) continue;
+            const unsigned in = unit_in(l, u);
+            *reinterpret_cast<uint4*>(&kt[slot][0] + 16 * (64 * wave + u * NT + l)) = kcode[u];
+            if (in < D / 8) *reinterpret_cast<uint32_t*>(&kst[slot][0] + unit_page(l, u) * (D / 2) + 4 * in) = kscale[u];
+        }
+    };
+    // The scale bytes of unit u; tokens that no row of the block sees may hold
+    // anything, so theirs become 0.
+    static_assert(NT % (D / 8) == 0, "a thread's units are of the same channels");
+    auto octet = [&](unsigned l) { return int(l % (D / 8)); };   // (D / 8 divides 64)
+    auto unit_scales = [&](unsigned l, int tile, int u) {
+        const int tok = token_of(tile) + kPage * unit_page(l, u) + 4 * int(unit_in(l, u) / (D / 8));
+        uint32_t sc = vscale[u];
+        if (tok + 3 > hi || (p.window > 0 && tok <= lo - p.window && tok + 4 > p.sinks)) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (tok + t > hi || (p.window > 0 && tok + t <= lo - p.window && tok + t >= p.sinks)) sc &= ~(0xFFu << (8 * t));
+        }
+        return sc;
+    };
+    // Decodes this thread's units into the value buffer, relative to my_base.
+    auto store_v = [&](int tile, int slot) {
+        const unsigned l = fresh_lane();
+        const int oct = octet(l);
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            if (!has_unit(u)) continue;
+            const int pg = unit_page(l, u), tq = int(unit_in(l, u) / (D / 8));
+            const uint32_t bytes = unit_scales(l, tile, u);
+            uint32_t sc = 0u;
+            bool above = false;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int rel = int((bytes >> (8 * t)) & 0xFFu) + (127 - my_base);
+                above = above || rel > 127 + 13;
+                sc |= uint32_t(rel > 0 ? rel : 0) << (8 * t);
             }
+            if (above) grow[slot] = 1;
             uint2 out[8];
-            if (bf16) {
-                decode_unit<false>(vcode[u], sc, out);
-            } else {
-                bool far = false;
+            decode_unit(vcode[u], sc, out);
+            uint8_t* dst = &vt[slot][0] + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const uint32_t b = (sc >> (8 * t)) & 0xFFu;
-                    far |= b != 0 && (b < 127 - 23 || b > 127 + 13);
-                }
-                if (far) wide[slot] = 1;
-                decode_unit<true>(vcode[u], sc, out);
-            }
-            const int cb = oct >> 2, h = tq & 1;
-            uint8_t* dst = &vt[slot][0] + ((pg * CB + cb) * 2 + h) * 512 + (tq >> 1) * 8;
-            const int f = (2 * cb + h) & 7;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + ((8 * (oct & 3) + i) ^ f) * 16) = out[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + 16 * i) = out[i];
         }
     };
 
@@ -397,59 +442,45 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
 #pragma unroll
         for (int c = 0; c < CB; ++c) acc[c][q] = v16f(0.f);
     }
-    bool big_max = false;
+    bool big_max = false;   // wave-uniform: a running maximum of magnitude 2^20 or more (see decode_kernel)
 
-    if (first_tile < last_tile) load_tile(first_tile, 0);
-    for (int t = first_tile; t < last_tile; ++t) {
-        const int slot = (t - first_tile) & 1;
-        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);   // this thread's K copies and V units of the tile
-        store_units(t, slot, false);
-        __syncthreads();
-        const bool bf16 = wide[slot] != 0;
-        if (bf16) {
-            // rare: decode again in BF16
-            __syncthreads();
-            if (tid == 0) wide[slot] = 0;
-            store_units(t, slot, true);
-            __syncthreads();
-        }
-        if (t + 1 < last_tile) load_tile(t + 1, slot ^ 1);
-        const int tok0 = token_of(t);
-        // tiles past the wave's last row, or before its windows and after the sinks
-        if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + kTile <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
-        const bool clear = tok0 + kTile - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + kTile <= p.sinks);
+    // The wave's rows against the tile in `slot`; `clear`: every row sees all of it.
+    auto compute = [&](int tok0, int slot, bool clear) {
+        const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
+        const uint8_t* v_at = &vt[slot][0] + lh * kVRow + 16 * lc;
+        const uint8_t* k_at = &kt[slot][0] + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
+        const uint8_t* s_at = &kst[slot][0] + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb) {   // 32 tokens
-            v16f s[NQ];
-            const v16f zero = v16f(0.f);
+        for (int tb = 0; tb < TT / 32; ++tb) {
+            uint4 ka[KS];
+            int ksc[KS];
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const int pg = 2 * tb + (col >> 4), at = (2 * k + half) * 16 + (col & 15);
-                const uint4 a = *reinterpret_cast<const uint4*>(&kt[slot][0] + pg * (8 * D) + at * 16);
-                const int sc = kst[slot][pg * (D / 2) + at];
-                const v8i ka = {int(a.x), int(a.y), int(a.z), int(a.w), 0, 0, 0, 0};
-#pragma unroll
-                for (int q = 0; q < NQ; ++q)
-                    s[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qop[q][k], k == 0 ? zero : s[q], 4, 0, 0, sc,
-                                                                           0, 127);
+                ka[k] = *reinterpret_cast<const uint4*>(k_at + tb * (16 * D) + k * 512);
+                ksc[k] = s_at[tb * D + k * 32];
             }
-            // row i of a product: token 8 (i / 4) + 4 half + i % 4 of the 32
-            const int tok = tok0 + 32 * tb + 4 * half;
-            uint32_t ph[NQ][8], pl[NQ][8];
+            uint32_t ph[NQ][8];
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
+                v16f s = v16f(0.f);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const v8i a = {int(ka[k].x), int(ka[k].y), int(ka[k].z), int(ka[k].w), 0, 0, 0, 0};
+                    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qop[q][k], s, 4, 0, 0, ksc[k], 0, 127);
+                }
                 if (!clear) {
+                    // row i of the product: token 8 (i / 4) + 4 half + i % 4 of the 32
+                    const int tok = tok0 + 32 * tb + 4 * int(lh);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int tt = tok + 8 * (i >> 2) + (i & 3);
-                        bool seen = tt <= pos[q];
-                        if (p.window > 0) seen = seen && (tt > pos[q] - p.window || tt < p.sinks);
-                        s[q][i] = seen ? s[q][i] : -__builtin_inff();
+                        const bool seen = tt <= pos[q] && (p.window == 0 || tt > pos[q] - p.window || tt < p.sinks);
+                        s[i] = seen ? s[i] : -__builtin_inff();
                     }
                 }
-                float mx = s[q][0];
+                float mx = s[0];
 #pragma unroll
-                for (int i = 1; i < 16; ++i) mx = __builtin_fmaxf(mx, s[q][i]);
+                for (int i = 1; i < 16; ++i) mx = __builtin_fmaxf(mx, s[i]);
                 if (__builtin_amdgcn_ballot_w64(mx * sl2 > m_run[q] + kLazyRescale) != 0) {
                     float a = mx, b = mx;
                     swap32(a, b);
@@ -463,56 +494,100 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                     }
                     bool big = false;
 #pragma unroll
-                    for (int qq = 0; qq < NQ; ++qq) big = big || (__builtin_fabsf(m_run[qq]) >= 0x1p20f && m_run[qq] != kNoMax);
+                    for (int o = 0; o < NQ; ++o) big = big || (__builtin_fabsf(m_run[o]) >= 0x1p20f && m_run[o] != kNoMax);
                     big_max = __builtin_amdgcn_ballot_w64(big) != 0;
                 }
-                float e[16];
-                if (!big_max) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i], sl2, -m_run[q]));
-                } else {
-                    // (see decode_kernel: the rounded product, as m_run was)
+                if (big_max) {
+                    // the rounded product, as m_run was
 #pragma clang fp contract(off)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(s[q][i] * sl2 - m_run[q]);
-                }
-                if (!bf16) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const v2h h = {_Float16(e[2 * i]), _Float16(e[2 * i + 1])};
-                        ph[q][i] = __builtin_bit_cast(uint32_t, h);
-                    }
+                    for (int i = 0; i < 16; ++i) s[i] = s[i] * sl2 - m_run[q];
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) split_p(e[2 * i], e[2 * i + 1], ph[q][i], pl[q][i]);
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], sl2, -m_run[q]);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) l_run[q] += e[i];
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    // the sum is of the weights as PV sees them
+                    const v2h h = {_Float16(s[2 * i]), _Float16(s[2 * i + 1])};
+                    const v2h one = {_Float16(1.0f), _Float16(1.0f)};
+                    ph[q][i] = __builtin_bit_cast(uint32_t, h);
+                    l_run[q] = __builtin_amdgcn_fdot2(h, one, l_run[q], false);
+                }
             }
 #pragma unroll
             for (int mm = 0; mm < 2; ++mm) {   // 16 tokens, one page
 #pragma unroll
                 for (int c = 0; c < CB; ++c) {
-                    const int f = (2 * c + half) & 7;
-                    const uint4 a = *reinterpret_cast<const uint4*>(&vt[slot][0] + (((2 * tb + mm) * CB + c) * 2 + half) * 512 +
-                                                                    (col ^ f) * 16);
+                    const uint4 a = *reinterpret_cast<const uint4*>(v_at + ((2 * tb + mm) * CB + c) * 2 * kVRow);
 #pragma unroll
                     for (int q = 0; q < NQ; ++q) {
                         const uint4 h = {ph[q][4 * mm], ph[q][4 * mm + 1], ph[q][4 * mm + 2], ph[q][4 * mm + 3]};
-                        if (!bf16) {
-                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a),
-                                                                               __builtin_bit_cast(v8h, h), acc[c][q], 0, 0, 0);
-                        } else {
-                            const uint4 l = {pl[q][4 * mm], pl[q][4 * mm + 1], pl[q][4 * mm + 2], pl[q][4 * mm + 3]};
-                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a),
-                                                                                __builtin_bit_cast(v8bf, h), acc[c][q], 0, 0, 0);
-                            acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a),
-                                                                                __builtin_bit_cast(v8bf, l), acc[c][q], 0, 0, 0);
-                        }
+                        acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, h),
+                                                                           acc[c][q], 0, 0, 0);
                     }
                 }
             }
         }
+    };
+
+    if (first_tile < last_tile) {
+        load_ids(first_tile);
+        load_tile();
+        load_ids(first_tile + 1);
+    }
+    for (int t = first_tile; t < last_tile; ++t) {
+        const int slot = (t - first_tile) & 1;
+        store_k(slot);
+        store_v(t, slot);
+        __syncthreads();
+        if (grow[slot] != 0) {
+            // rare (and the first tile): set the exponents from the tile's largest
+            // scales, rescale the accumulators, decode the tile again
+#pragma unroll
+            for (int u = 0; u < UR; ++u) {
+                if (!has_unit(u)) continue;
+                const uint32_t bytes = unit_scales(lane, t, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) atomicMax(&top[octet(lane) >> 2], int((bytes >> (8 * i)) & 0xFFu));
+            }
+            __syncthreads();
+            if (tid == 0) grow[slot] = 0;
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                const int old = base[c], now = top[c] - 8 > old ? top[c] - 8 : old;
+                if (now == old) continue;
+                const float f = old == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, old - now);
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
+            }
+            my_base = top[octet(lane) >> 2] - 8 > my_base ? top[octet(lane) >> 2] - 8 : my_base;
+            __syncthreads();
+            if (tid < CB) {
+                base[tid] = top[tid] - 8 > base[tid] ? top[tid] - 8 : base[tid];
+                top[tid] = 0;
+            }
+            store_v(t, slot);
+            __syncthreads();
+        }
+        if (t + 1 < last_tile) {
+            load_tile();
+            load_ids(t + 2);
+        }
+        const int tok0 = token_of(t);
+        // tiles past the wave's last row, or before its windows and after the sinks
+        if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + TT <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
+        const bool clear = tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks);
+        compute(tok0, slot, clear);
+    }
+    // the accumulators back to O
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+        const float f = base[c] == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, base[c] - 127);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
     }
 
     // ---- the row's sum over both halves, then the row itself or its partial
@@ -523,7 +598,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         swap32(a, b);
         const float l = a + b;
         const int row = w_row0 + 32 * q + col;
-        const int tok = row / p.group;
+        const int tok = int(unsigned(row) / unsigned(p.group));
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
         if (!whole) {
             if (row < rows) {
@@ -581,7 +656,7 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     r.row0 = ((t - r.first) * p.group + hq % p.group) / M * M;
     int plo, phi;
     extend_span<M>(p, r, plo, phi);
-    extend_tiles(p, plo, phi, r);
+    extend_tiles<extend_tile<D>()>(p, plo, phi, r);
     const int per = extend_per_split(r.tiles, p.splits);
     if (r.tiles <= per) return;   // written by the first launch
     const int parts = (r.tiles + per - 1) / per;
@@ -636,11 +711,11 @@ static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) 
     return hipGetLastError();
 }
 
-int extend_block_rows(int) { return 128; }
+int extend_block_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
 hipError_t launch_extend(const ExtendParams& p, hipStream_t stream) {
-    if (p.head_dim == 64) return launch_extend_with<64, 1, 4>(p, stream);
-    if (p.head_dim == 128) return launch_extend_with<128, 1, 4>(p, stream);
+    if (p.head_dim == 64) return launch_extend_with<64, 2, 4>(p, stream);
+    if (p.head_dim == 128) return launch_extend_with<128, 2, 4>(p, stream);
     return launch_extend_with<256, 1, 4>(p, stream);
 }
 
