@@ -722,14 +722,14 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  *                   position below 0: more queries than context) gives 0.
  *                   Rows behind cu_seqlens[batch] are left as they were.
  * QK^T is that of uq_decode_attention (FP8 query, FP4 keys); the softmax
- * runs in fp32; its weights enter PV rounded once to BF16 (relative error up
- * to 2^-8 / 2 each, while uq_decode_attention carries 16 bits of them).
+ * runs in fp32; its weights enter PV rounded once to FP16 (relative error up
+ * to 2^-11 each, while uq_decode_attention carries 16 bits of them).
  * A long context with few queries is split over blocks and joined by a second
  * launch; the bits of a row depend on num_tokens, batch and max_context then.
  * num_tokens == 0 or batch == 0 is a no-op.
  * Errors: as uq_decode_attention, plus INVALID_ARGUMENT for a null
  * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for
- * num_tokens >= 2^26 or more blocks than a grid holds.
+ * num_tokens >= 2^24 or more blocks than a grid holds.
  */
 size_t uq_extend_workspace_bytes(const uq_cache_desc *desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
                                  int32_t max_context, int32_t window, int32_t sinks);

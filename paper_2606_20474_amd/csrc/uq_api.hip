@@ -717,7 +717,7 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
     if (num_q_heads % desc->num_kv_heads != 0) return UQ_ERR_INVALID_ARGUMENT;
     const int32_t group = num_q_heads / desc->num_kv_heads;
     if (group > kMaxGroup || batch > 65535 || desc->num_kv_heads > 65535) return UQ_ERR_UNSUPPORTED;
-    if (num_tokens >= (int64_t(1) << 26)) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens >= (int64_t(1) << 24)) return UQ_ERR_UNSUPPORTED;   // rows of a KV head are numbered in 28 bits
     const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
     e.row_blocks = rows / m + seqs;
@@ -780,6 +780,7 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     p.num_q_heads = num_q_heads;
     p.num_kv_heads = desc->num_kv_heads;
     p.group = num_q_heads / desc->num_kv_heads;
+    p.group_magic = uint32_t((uint64_t(1) << 32) / uint64_t(p.group)) + 1;
     p.head_dim = desc->head_dim;
     p.codes = kv_codes;
     p.scales = kv_scales;

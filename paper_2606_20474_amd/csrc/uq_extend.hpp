@@ -31,6 +31,7 @@
 
 #include "uq_device.hpp"
 #include "uq_internal.hpp"
+#include "uq_quad.hpp"
 
 namespace uq {
 
@@ -152,11 +153,13 @@ __device__ __forceinline__ void decode_unit(const uint4& v, uint32_t scale_bytes
     }
 }
 
-// The rotation R of one column held as accumulators: channel 32 c + 8 (i / 4) + 4
-// half + i % 4 in acc[c][q][i], lanes l and l ^ 32 sharing the column.  Stage
-// order 1, 2, 4 (between the lanes), 8, ..., as wht_x.
+// One column of the accumulators, channel 32 c + 8 (i / 4) + 4 half + i % 4 in
+// acc[c][q][i] with lanes l and l ^ 32 sharing it, to channel 32 c + 16 (i / 8) + 8
+// half + i % 8: runs of 8 channels per lane, for the stores.  On the way, with
+// `rotate`, the rotation R: the halves' exchange brings both values of a pair of
+// its stage (width 4) into one lane.
 template <int CB, int NQ>
-__device__ __forceinline__ void wht_columns(v16f (&acc)[CB][NQ], int q, int half) {
+__device__ __forceinline__ void gather_columns(v16f (&acc)[CB][NQ], int q, bool rotate) {
 #pragma clang fp contract(off)
     auto stage = [&](int h) {
 #pragma unroll
@@ -169,39 +172,97 @@ __device__ __forceinline__ void wht_columns(v16f (&acc)[CB][NQ], int q, int half
                 acc[c][q][i + h] = a - b;
             }
     };
-    stage(1);
-    stage(2);
+    if (rotate) {
+        stage(1);
+        stage(2);
+        stage(4);
+        stage(8);
+#pragma unroll
+        for (int h = 1; h < CB; h <<= 1)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                if (c & h) continue;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float a = acc[c][q][i], b = acc[c + h][q][i];
+                    acc[c][q][i] = a + b;
+                    acc[c + h][q][i] = a - b;
+                }
+            }
+    }
+    const float r = rotate ? inv_sqrt_d<32 * CB>() : 1.0f;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float a = acc[c][q][i], b = a;
-            swap32(a, b);   // a: the lower half's value, b: the upper's, in both lanes
-            acc[c][q][i] = half ? a - b : a + b;
+            if (i & 4) continue;
+            float a = acc[c][q][i], b = acc[c][q][i + 4];
+            swap32(a, b);   // lane l: both halves' values of acc[i] (l < 32) or of acc[i + 4]
+            acc[c][q][i] = rotate ? (a + b) * r : a;
+            acc[c][q][i + 4] = rotate ? (a - b) * r : b;
         }
-    stage(4);
-    stage(8);
-#pragma unroll
-    for (int h = 1; h < CB; h <<= 1)
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-            if (c & h) continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float a = acc[c][q][i], b = acc[c + h][q][i];
-                acc[c][q][i] = a + b;
-                acc[c + h][q][i] = a - b;
-            }
-        }
-    const float r = inv_sqrt_d<32 * CB>();
-#pragma unroll
-    for (int c = 0; c < CB; ++c) acc[c][q] *= r;
+}
+
+// n / group, exact for n < 2^28.
+__device__ __forceinline__ int div_group(const ExtendParams& p, int n) {
+    return p.group == 1 ? n : int(__umulhi(unsigned(n), p.group_magic));
 }
 
 // Tiles per split of a row block with `tiles` of them.
 __host__ __device__ __forceinline__ int extend_per_split(int tiles, int splits) {
     const int per = (tiles + splits - 1) / splits;
     return per > 2 ? per : 2;
+}
+
+// The wave's 32 NQ query rows from row0 on, as FP8 in operand order at `qs`: a quad
+// of lanes per row, 16 rows at a time, all loads in flight before the first
+// rotation.
+template <int DT, int D, int NQ>
+__device__ __forceinline__ void stage_queries(const ExtendParams& p, const ExtendRows& r, int hk, int row0, uint8_t* qs) {
+    constexpr int NG = D / 32, KS = D / 64;
+    const int lane = threadIdx.x & 63, L = lane & 3;
+    const int rows = r.count * p.group;
+    // the rows of a pass together fill up to 64 registers
+    constexpr int PASS = D == 256 ? 1 : 2;
+#pragma unroll
+    for (int i = 0; i < 2 * NQ; i += PASS) {
+        float x[DT == 3 ? 1 : PASS][NG][8];
+        uint2 w[PASS][NG];
+#pragma unroll
+        for (int u = 0; u < PASS; ++u) {
+            const int row = row0 + 16 * (i + u) + (lane >> 2);
+            const int tok = div_group(p, row);
+            const int64_t elem = int64_t(r.first + tok) * p.q_stride + int64_t(hk * p.group + row - tok * p.group) * D + 8 * L;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                if constexpr (DT == 3) {
+                    w[u][j] = make_uint2(0u, 0u);
+                    if (row < rows) w[u][j] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.q) + elem + 32 * j);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[u][j][k] = 0.f;
+                    if (row < rows) load_x8<DT>(p.q, elem + 32 * j, x[u][j]);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < PASS; ++u) {
+            if constexpr (DT != 3) {
+                wht_quad<NG>(x[u], L);
+#pragma unroll
+                for (int j = 0; j < NG; ++j)
+                    w[u][j] = make_uint2(e4m3x4(x[u][j][0], x[u][j][1], x[u][j][2], x[u][j][3]),
+                                         e4m3x4(x[u][j][4], x[u][j][5], x[u][j][6], x[u][j][7]));
+            }
+            const int rr = 16 * (i + u) + (lane >> 2);   // row of the wave
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const int c = 32 * j + 8 * L;
+                const int dst = ((rr >> 5) * KS + (c >> 6)) * 2048 + (((c >> 4) & 1) * 32 + (rr & 31)) * 32 + ((c >> 5) & 1) * 16 + (c & 15);
+                *reinterpret_cast<uint2*>(qs + dst) = w[u][j];
+            }
+        }
+    }
 }
 
 // One block's walk: NQ blocks of 32 rows per wave, W waves.  Per tile a thread
@@ -216,7 +277,6 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     constexpr int NT = 64 * W;
     constexpr int KS = D / 64;                // k steps of QK^T
     constexpr int CB = D / 32;                // channel blocks of PV
-    constexpr int N = D / 16;                 // channels per lane of a 16-lane row
     constexpr int kPageUnits = D / 2;         // 16-byte units of a page's K, and of its V
     constexpr int kUnits = TT / kPage * kPageUnits;
     constexpr int UR = (kUnits + NT - 1) / NT;
@@ -261,42 +321,11 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // of the B operand: k step s, lane (row, half): bytes 0..15 are channels
     // 64 s + 16 half .., 16..31 are 64 s + 32 + 16 half ..
     uint8_t* qs = &vt[0][0] + wave * (32 * NQ * D);
-    const int L = lane & 15;
-#pragma unroll 2
-    for (int i = 0; i < 8 * NQ; ++i) {
-        const int rr = 4 * i + (lane >> 4);                       // row of the wave
-        const int row = r.row0 + wave * (32 * NQ) + rr;
-        uint32_t w[N / 4];
-#pragma unroll
-        for (int j = 0; j < N / 4; ++j) w[j] = 0u;
-        if (row < rows) {
-            const int tok = int(unsigned(row) / unsigned(p.group));
-            const int64_t elem = int64_t(r.first + tok) * p.q_stride + int64_t(hk * p.group + row - tok * p.group) * D + N * L;
-            if (p.q_dtype == 3) {
-                const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.q) + elem);
-#pragma unroll
-                for (int j = 0; j < N / 4; ++j) w[j] = src[j];
-            } else {
-                float x[N];
-#pragma unroll
-                for (int j = 0; j < N / 4; ++j) {
-                    float (&y)[4] = *reinterpret_cast<float(*)[4]>(&x[4 * j]);
-                    if (p.q_dtype == 0) load_x4<0>(p.q, elem + 4 * j, y);
-                    else if (p.q_dtype == 1) load_x4<1>(p.q, elem + 4 * j, y);
-                    else load_x4<2>(p.q, elem + 4 * j, y);
-                }
-                wht_x<N>(x, L);
-#pragma unroll
-                for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < N / 4; ++j) {
-            const int c = N * L + 4 * j;
-            const int dst = ((rr >> 5) * KS + (c >> 6)) * 2048 + (((c >> 4) & 1) * 32 + (rr & 31)) * 32 + ((c >> 5) & 1) * 16 + (c & 15);
-            *reinterpret_cast<uint32_t*>(qs + dst) = w[j];
-        }
-    }
+    const int w_row0 = r.row0 + wave * (32 * NQ);
+    if (p.q_dtype == 0) stage_queries<0, D, NQ>(p, r, hk, w_row0, qs);
+    else if (p.q_dtype == 1) stage_queries<1, D, NQ>(p, r, hk, w_row0, qs);
+    else if (p.q_dtype == 2) stage_queries<2, D, NQ>(p, r, hk, w_row0, qs);
+    else stage_queries<3, D, NQ>(p, r, hk, w_row0, qs);
     if (tid < 2) grow[tid] = 0;
     if (tid < CB) {
         top[tid] = 0;
@@ -315,12 +344,11 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     __syncthreads();
 
     // position of this lane's rows
-    const int w_row0 = r.row0 + wave * (32 * NQ);
     int pos[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
         const int row = w_row0 + 32 * q + col;
-        pos[q] = row < rows ? r.n_ctx - r.count + int(unsigned(row) / unsigned(p.group)) : -1;
+        pos[q] = row < rows ? r.n_ctx - r.count + div_group(p, row) : -1;
     }
     // the wave's first and last position (a wave without rows only moves tiles)
     const bool busy = w_row0 < rows;
@@ -445,44 +473,66 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     bool big_max = false;   // wave-uniform: a running maximum of magnitude 2^20 or more (see decode_kernel)
 
     // The wave's rows against the tile in `slot`; `clear`: every row sees all of it.
+    // Masks, rescaling and large maxima are one branch, so that the rest is one
+    // block of instructions, in which the exponentials of the second 16 tokens
+    // run beside the products of the first.
     auto compute = [&](int tok0, int slot, bool clear) {
         const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
         const uint8_t* v_at = &vt[slot][0] + lh * kVRow + 16 * lc;
         const uint8_t* k_at = &kt[slot][0] + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
         const uint8_t* s_at = &kst[slot][0] + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
-#pragma unroll
-        for (int tb = 0; tb < TT / 32; ++tb) {
-            uint4 ka[KS];
-            int ksc[KS];
+        uint4 ka[KS];
+        int ksc[KS];
+        auto load_k = [&](int tb) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 ka[k] = *reinterpret_cast<const uint4*>(k_at + tb * (16 * D) + k * 512);
                 ksc[k] = s_at[tb * D + k * 32];
             }
-            uint32_t ph[NQ][8];
+        };
+        load_k(0);
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                v16f s = v16f(0.f);
+        for (int tb = 0; tb < TT / 32; ++tb) {
+            v16f s[NQ];
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const v8i a = {int(ka[k].x), int(ka[k].y), int(ka[k].z), int(ka[k].w), 0, 0, 0, 0};
-                    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qop[q][k], s, 4, 0, 0, ksc[k], 0, 127);
-                }
-                if (!clear) {
-                    // row i of the product: token 8 (i / 4) + 4 half + i % 4 of the 32
-                    const int tok = tok0 + 32 * tb + 4 * int(lh);
+            for (int q = 0; q < NQ; ++q) s[q] = v16f(0.f);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int tt = tok + 8 * (i >> 2) + (i & 3);
-                        const bool seen = tt <= pos[q] && (p.window == 0 || tt > pos[q] - p.window || tt < p.sinks);
-                        s[i] = seen ? s[i] : -__builtin_inff();
+            for (int k = 0; k < KS; ++k) {
+                const v8i a = {int(ka[k].x), int(ka[k].y), int(ka[k].z), int(ka[k].w), 0, 0, 0, 0};
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+                    s[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qop[q][k], s[q], 4, 0, 0, ksc[k], 0, 127);
+            }
+            auto load_v = [&](int mm, uint4 (&v)[CB]) {
+#pragma unroll
+                for (int c = 0; c < CB; ++c) v[c] = *reinterpret_cast<const uint4*>(v_at + ((2 * tb + mm) * CB + c) * 2 * kVRow);
+            };
+            auto max_of = [&](int q) {
+                float mx = __builtin_fmaxf(__builtin_fmaxf(s[q][0], s[q][1]), s[q][2]);
+#pragma unroll
+                for (int i = 3; i < 15; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[q][i]), s[q][i + 1]);
+                return __builtin_fmaxf(mx, s[q][15]);
+            };
+            bool grows = !clear || big_max;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+                grows = __builtin_amdgcn_ballot_w64(max_of(q) * sl2 > m_run[q] + kLazyRescale) != 0 || grows;
+            float scale = sl2, shift[NQ];
+            if (grows) {
+                big_max = false;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    if (!clear) {
+                        // row i of the product: token 8 (i / 4) + 4 half + i % 4 of the 32
+                        const int tok = tok0 + 32 * tb + 4 * int(lh);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int tt = tok + 8 * (i >> 2) + (i & 3);
+                            const bool seen = tt <= pos[q] && (p.window == 0 || tt > pos[q] - p.window || tt < p.sinks);
+                            s[q][i] = seen ? s[q][i] : -__builtin_inff();
+                        }
                     }
-                }
-                float mx = s[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) mx = __builtin_fmaxf(mx, s[i]);
-                if (__builtin_amdgcn_ballot_w64(mx * sl2 > m_run[q] + kLazyRescale) != 0) {
-                    float a = mx, b = mx;
+                    float a = max_of(q), b = a;
                     swap32(a, b);
                     const float mloc = __builtin_fmaxf(a, b) * sl2;
                     if (mloc > m_run[q] + kLazyRescale) {
@@ -492,44 +542,56 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                         for (int c = 0; c < CB; ++c) acc[c][q] *= alpha;
                         m_run[q] = mloc;
                     }
-                    bool big = false;
-#pragma unroll
-                    for (int o = 0; o < NQ; ++o) big = big || (__builtin_fabsf(m_run[o]) >= 0x1p20f && m_run[o] != kNoMax);
-                    big_max = __builtin_amdgcn_ballot_w64(big) != 0;
+                    big_max = big_max || __builtin_amdgcn_ballot_w64(__builtin_fabsf(m_run[q]) >= 0x1p20f && m_run[q] != kNoMax) != 0;
                 }
-                if (big_max) {
-                    // the rounded product, as m_run was
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) shift[q] = -m_run[q];
+            if (big_max) {
+                // the difference to the rounded product, as m_run was
 #pragma clang fp contract(off)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = s[i] * sl2 - m_run[q];
-                } else {
+                for (int q = 0; q < NQ; ++q) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], sl2, -m_run[q]);
+                    for (int i = 0; i < 16; ++i) s[q][i] = s[q][i] * sl2 - m_run[q];
+                    shift[q] = 0.f;
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    // the sum is of the weights as PV sees them
-                    const v2h h = {_Float16(s[2 * i]), _Float16(s[2 * i + 1])};
-                    const v2h one = {_Float16(1.0f), _Float16(1.0f)};
-                    ph[q][i] = __builtin_bit_cast(uint32_t, h);
-                    l_run[q] = __builtin_amdgcn_fdot2(h, one, l_run[q], false);
-                }
+                scale = 1.f;
             }
+            // P of tokens 16 mm .. 16 mm + 15 as operand B; the sum is of the weights as PV
+            // sees them
+            auto weights = [&](int mm, uint4 (&ph)[NQ]) {
 #pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {   // 16 tokens, one page
+                for (int q = 0; q < NQ; ++q) {
+                    uint32_t w[4];
 #pragma unroll
-                for (int c = 0; c < CB; ++c) {
-                    const uint4 a = *reinterpret_cast<const uint4*>(v_at + ((2 * tb + mm) * CB + c) * 2 * kVRow);
-#pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
-                        const uint4 h = {ph[q][4 * mm], ph[q][4 * mm + 1], ph[q][4 * mm + 2], ph[q][4 * mm + 3]};
-                        acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, h),
-                                                                           acc[c][q], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][8 * mm + 2 * i], scale, shift[q]));
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][8 * mm + 2 * i + 1], scale, shift[q]));
+                        const v2h h = {_Float16(x), _Float16(y)};
+                        const v2h one = {_Float16(1.0f), _Float16(1.0f)};
+                        w[i] = __builtin_bit_cast(uint32_t, h);
+                        l_run[q] = __builtin_amdgcn_fdot2(h, one, l_run[q], false);
                     }
+                    ph[q] = uint4{w[0], w[1], w[2], w[3]};
                 }
-            }
+            };
+            auto values = [&](const uint4 (&v)[CB], const uint4 (&ph)[NQ]) {
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+                        acc[c][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, v[c]),
+                                                                           __builtin_bit_cast(v8h, ph[q]), acc[c][q], 0, 0, 0);
+            };
+            uint4 p0[NQ], p1[NQ], va[CB], vb[CB];
+            load_v(0, va);
+            weights(0, p0);
+            load_v(1, vb);
+            values(va, p0);
+            weights(1, p1);
+            if (tb + 1 < TT / 32) load_k(tb + 1);
+            values(vb, p1);
         }
     };
 
@@ -598,7 +660,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         swap32(a, b);
         const float l = a + b;
         const int row = w_row0 + 32 * q + col;
-        const int tok = int(unsigned(row) / unsigned(p.group));
+        const int tok = div_group(p, row);
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
         if (!whole) {
             if (row < rows) {
@@ -616,16 +678,22 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         const float inv = l > 0.f ? 1.0f / l : 0.f;   // a row that sees nothing is 0
 #pragma unroll
         for (int c = 0; c < CB; ++c) acc[c][q] *= inv;
-        if (p.rotate_v) wht_columns(acc, q, half);
+        gather_columns(acc, q, p.rotate_v != 0);
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float x0 = acc[c][q][4 * i], x1 = acc[c][q][4 * i + 1], x2 = acc[c][q][4 * i + 2], x3 = acc[c][q][4 * i + 3];
-                const int64_t at = out_row * D + 32 * c + 8 * i + 4 * half;
-                if (row < rows) {
-                    if (p.out_dtype == 0) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(x0, x1, x2, x3);
-                    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(x0, x1), pack_bf16x2(x2, x3));
+            for (int i = 0; i < 16; i += 8) {
+                const v16f& o = acc[c][q];
+                const int64_t at = out_row * D + 32 * c + 2 * i + 8 * half;
+                if (row >= rows) continue;
+                if (p.out_dtype == 0) {
+                    float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+                    dst[0] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    dst[1] = make_float4(o[i + 4], o[i + 5], o[i + 6], o[i + 7]);
+                } else {
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at) =
+                        uint4{pack_bf16x2(o[i], o[i + 1]), pack_bf16x2(o[i + 2], o[i + 3]), pack_bf16x2(o[i + 4], o[i + 5]),
+                              pack_bf16x2(o[i + 6], o[i + 7])};
                 }
             }
     }

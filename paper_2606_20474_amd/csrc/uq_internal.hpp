@@ -178,6 +178,7 @@ struct ExtendParams {
     int32_t num_q_heads;
     int32_t num_kv_heads;
     int32_t group;
+    uint32_t group_magic;      // floor(2^32 / group) + 1: n / group = high word of n * group_magic for n < 2^28
     int32_t head_dim;
     const uint8_t* codes;
     const uint8_t* scales;

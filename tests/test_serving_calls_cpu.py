@@ -100,7 +100,7 @@ def test_extend_attention():
                dict(ctx=None), dict(maxctx=6401), dict(maxctx=-1), dict(window=-1), dict(sinks=-1), dict(scale=0.0),
                dict(scale=float("inf")), dict(ws=None), dict(ws=ODD), dict(out=None), dict(out=ODD)):
         assert extend(**kw) == INVALID, kw
-    for kw in (dict(dt=4), dict(odt=2), dict(hq=34), dict(D=desc(head_dim=96)), dict(T=1 << 26), dict(B=65536)):
+    for kw in (dict(dt=4), dict(odt=2), dict(hq=34), dict(D=desc(head_dim=96)), dict(T=1 << 24), dict(B=65536)):
         assert extend(**kw) == UNSUPPORTED, kw
     D = desc()
     need = uq.lib.uq_extend_workspace_bytes(ctypes.byref(D), 64, 2, 4, 6400, 0, 0)
