@@ -41,8 +41,8 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
 
-// Tokens per tile: 4 pages, 2 at head size 256 (two blocks fit a CU's LDS then).
-template <int D> constexpr int extend_tile() { return D == 256 ? 32 : 64; }
+// Tokens per tile: one 16-byte unit of K and one of V for each of 256 threads.
+template <int D> constexpr int extend_tile() { return 8192 / D; }
 
 // Where a block's rows stand and which tiles they see.
 struct ExtendRows {
@@ -343,13 +343,6 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         }
     __syncthreads();
 
-    // position of this lane's rows
-    int pos[NQ];
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const int row = w_row0 + 32 * q + col;
-        pos[q] = row < rows ? r.n_ctx - r.count + div_group(p, row) : -1;
-    }
     // the wave's first and last position (a wave without rows only moves tiles)
     const bool busy = w_row0 < rows;
     const int w_last = w_row0 + 32 * NQ < rows ? w_row0 + 32 * NQ - 1 : rows - 1;
@@ -423,18 +416,20 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // anything, so theirs become 0.
     static_assert(NT % (D / 8) == 0, "a thread's units are of the same channels");
     auto octet = [&](unsigned l) { return int(l % (D / 8)); };   // (D / 8 divides 64)
+    const int seen_from = p.window > 0 ? lo - p.window + 1 : 0;
     auto unit_scales = [&](unsigned l, int tile, int u) {
         const int tok = token_of(tile) + kPage * unit_page(l, u) + 4 * int(unit_in(l, u) / (D / 8));
-        uint32_t sc = vscale[u];
-        if (tok + 3 > hi || (p.window > 0 && tok <= lo - p.window && tok + 4 > p.sinks)) {
+        // seen by some row: up to the last, and in the first row's window or a first token
+        uint32_t sc = 0u;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (tok + t > hi || (p.window > 0 && tok + t <= lo - p.window && tok + t >= p.sinks)) sc &= ~(0xFFu << (8 * t));
-        }
+        for (int t = 0; t < 4; ++t)
+            sc |= (tok + t <= hi) & ((tok + t >= seen_from) | (tok + t < p.sinks)) ? vscale[u] & (0xFFu << (8 * t)) : 0u;
         return sc;
     };
-    // Decodes this thread's units into the value buffer, relative to my_base.
+    // Decodes this thread's units into the value buffer, relative to my_base; true
+    // if a scale is above the range.
     auto store_v = [&](int tile, int slot) {
+        bool above = false;
         const unsigned l = fresh_lane();
         const int oct = octet(l);
 #pragma unroll
@@ -443,20 +438,19 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             const int pg = unit_page(l, u), tq = int(unit_in(l, u) / (D / 8));
             const uint32_t bytes = unit_scales(l, tile, u);
             uint32_t sc = 0u;
-            bool above = false;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int rel = int((bytes >> (8 * t)) & 0xFFu) + (127 - my_base);
                 above = above || rel > 127 + 13;
                 sc |= uint32_t(rel > 0 ? rel : 0) << (8 * t);
             }
-            if (above) grow[slot] = 1;
             uint2 out[8];
             decode_unit(vcode[u], sc, out);
             uint8_t* dst = &vt[slot][0] + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + 16 * i) = out[i];
         }
+        return above;
     };
 
     const float sl2 = p.scale_log2;
@@ -474,26 +468,22 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
 
     // The wave's rows against the tile in `slot`; `clear`: every row sees all of it.
     // Masks, rescaling and large maxima are one branch, so that the rest is one
-    // block of instructions, in which the exponentials of the second 16 tokens
-    // run beside the products of the first.
+    // block of instructions, in which the exponentials of the second 16 tokens run
+    // beside the products of the first.
     auto compute = [&](int tok0, int slot, bool clear) {
         const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
         const uint8_t* v_at = &vt[slot][0] + lh * kVRow + 16 * lc;
         const uint8_t* k_at = &kt[slot][0] + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
         const uint8_t* s_at = &kst[slot][0] + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
-        uint4 ka[KS];
-        int ksc[KS];
-        auto load_k = [&](int tb) {
+        v16f s[NQ];
+        auto scores = [&](int tb) {
+            uint4 ka[KS];
+            int ksc[KS];
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 ka[k] = *reinterpret_cast<const uint4*>(k_at + tb * (16 * D) + k * 512);
                 ksc[k] = s_at[tb * D + k * 32];
             }
-        };
-        load_k(0);
-#pragma unroll
-        for (int tb = 0; tb < TT / 32; ++tb) {
-            v16f s[NQ];
 #pragma unroll
             for (int q = 0; q < NQ; ++q) s[q] = v16f(0.f);
 #pragma unroll
@@ -503,6 +493,10 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                 for (int q = 0; q < NQ; ++q)
                     s[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qop[q][k], s[q], 4, 0, 0, ksc[k], 0, 127);
             }
+        };
+        scores(0);
+#pragma unroll
+        for (int tb = 0; tb < TT / 32; ++tb) {
             auto load_v = [&](int mm, uint4 (&v)[CB]) {
 #pragma unroll
                 for (int c = 0; c < CB; ++c) v[c] = *reinterpret_cast<const uint4*>(v_at + ((2 * tb + mm) * CB + c) * 2 * kVRow);
@@ -518,17 +512,21 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             for (int q = 0; q < NQ; ++q)
                 grows = __builtin_amdgcn_ballot_w64(max_of(q) * sl2 > m_run[q] + kLazyRescale) != 0 || grows;
             float scale = sl2, shift[NQ];
-            if (grows) {
+            if (__builtin_expect(grows, 0)) {
                 big_max = false;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
                     if (!clear) {
-                        // row i of the product: token 8 (i / 4) + 4 half + i % 4 of the 32
-                        const int tok = tok0 + 32 * tb + 4 * int(lh);
+                        // element i: token 8 (i / 4) + 4 half + i % 4 of the 32; it is seen when 0 <=
+                        // position - token < window, or among the first tokens
+                        const int tok = tok0 + 32 * tb + 4 * int(lh), row = w_row0 + 32 * q + int(lc);
+                        const int pos = row < rows ? r.n_ctx - r.count + div_group(p, row) : -1;
+                        const unsigned reach = p.window > 0 ? unsigned(p.window) : 0x80000000u;
+                        const int sinks = pos + 1 < p.sinks ? pos + 1 : p.sinks;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int tt = tok + 8 * (i >> 2) + (i & 3);
-                            const bool seen = tt <= pos[q] && (p.window == 0 || tt > pos[q] - p.window || tt < p.sinks);
+                            const bool seen = (unsigned(pos - tt) < reach) | (tt < sinks);
                             s[q][i] = seen ? s[q][i] : -__builtin_inff();
                         }
                     }
@@ -547,7 +545,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             }
 #pragma unroll
             for (int q = 0; q < NQ; ++q) shift[q] = -m_run[q];
-            if (big_max) {
+            if (__builtin_expect(big_max, 0)) {
                 // the difference to the rounded product, as m_run was
 #pragma clang fp contract(off)
 #pragma unroll
@@ -590,59 +588,65 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             load_v(1, vb);
             values(va, p0);
             weights(1, p1);
-            if (tb + 1 < TT / 32) load_k(tb + 1);
             values(vb, p1);
+            if (tb + 1 < TT / 32) scores(tb + 1);
         }
     };
 
+    // The exponents from the largest scales of the tile whose units this thread
+    // holds, the accumulators rescaled to them.
+    auto set_base = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            if (!has_unit(u)) continue;
+            const uint32_t bytes = unit_scales(lane, tile, u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicMax(&top[octet(lane) >> 2], int((bytes >> (8 * i)) & 0xFFu));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            const int old = base[c], now = top[c] - 8 > old ? top[c] - 8 : old;
+            const float f = old == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, old - now);   // (1 where nothing changes)
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
+        }
+        my_base = top[octet(lane) >> 2] - 8 > my_base ? top[octet(lane) >> 2] - 8 : my_base;
+        __syncthreads();
+        if (tid < CB) {
+            base[tid] = top[tid] - 8 > base[tid] ? top[tid] - 8 : base[tid];
+            top[tid] = 0;
+        }
+    };
+
+    // ---- the walk.  While tile t is computed, t + 1 is on its way into registers and
+    // t + 2's page ids too.  (Past the last tile in pages that exist.)  Nobody is left
+    // in tile t - 2 when t is stored, to its buffers.
     if (first_tile < last_tile) {
         load_ids(first_tile);
         load_tile();
         load_ids(first_tile + 1);
+        set_base(first_tile);
     }
     for (int t = first_tile; t < last_tile; ++t) {
         const int slot = (t - first_tile) & 1;
         store_k(slot);
-        store_v(t, slot);
+        if (store_v(t, slot)) grow[slot] = 1;
         __syncthreads();
-        if (grow[slot] != 0) {
-            // rare (and the first tile): set the exponents from the tile's largest
-            // scales, rescale the accumulators, decode the tile again
-#pragma unroll
-            for (int u = 0; u < UR; ++u) {
-                if (!has_unit(u)) continue;
-                const uint32_t bytes = unit_scales(lane, t, u);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) atomicMax(&top[octet(lane) >> 2], int((bytes >> (8 * i)) & 0xFFu));
-            }
+        if (__builtin_expect(grow[slot] != 0, 0)) {
+            // rare: a scale above the range.  The tile is decoded again.
             __syncthreads();
             if (tid == 0) grow[slot] = 0;
-#pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                const int old = base[c], now = top[c] - 8 > old ? top[c] - 8 : old;
-                if (now == old) continue;
-                const float f = old == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, old - now);
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
-            }
-            my_base = top[octet(lane) >> 2] - 8 > my_base ? top[octet(lane) >> 2] - 8 : my_base;
-            __syncthreads();
-            if (tid < CB) {
-                base[tid] = top[tid] - 8 > base[tid] ? top[tid] - 8 : base[tid];
-                top[tid] = 0;
-            }
+            set_base(t);
             store_v(t, slot);
             __syncthreads();
         }
-        if (t + 1 < last_tile) {
-            load_tile();
-            load_ids(t + 2);
-        }
+        load_tile();
+        load_ids(t + 2);
         const int tok0 = token_of(t);
         // tiles past the wave's last row, or before its windows and after the sinks
         if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + TT <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
-        const bool clear = tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks);
-        compute(tok0, slot, clear);
+        compute(tok0, slot, tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks));
     }
     // the accumulators back to O
 #pragma unroll
