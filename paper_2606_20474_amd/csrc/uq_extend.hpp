@@ -129,12 +129,9 @@ __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendR
     hi = r.n_ctx - r.count + last / p.group;
 }
 
-// One 16-byte unit of a page's V codes (4 tokens x 8 channels, their scale bytes in
-// `scale_bytes`) as eight pairs of dwords: of each channel the 4 tokens in FP16.
-__device__ __forceinline__ void decode_unit(const uint4& v, uint32_t scale_bytes, uint2 (&out)[8]) {
-    float sc[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) sc[t] = ue8m0_to_f32(scale_bytes >> (8 * t));
+// One 16-byte unit of a page's V codes (4 tokens x 8 channels, the tokens' scales in
+// sc) as eight pairs of dwords: of each channel the 4 tokens in FP16.
+__device__ __forceinline__ void decode_unit(const uint4& v, const float (&sc)[4], uint2 (&out)[8]) {
     uint32_t w[4][4];   // [token][channel pair]
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -222,27 +219,23 @@ __device__ __forceinline__ void stage_queries(const ExtendParams& p, const Exten
     constexpr int NG = D / 32, KS = D / 64;
     const int lane = threadIdx.x & 63, L = lane & 3;
     const int rows = r.count * p.group;
-    // the rows of a pass together fill up to 64 registers
-    constexpr int PASS = D == 256 ? 1 : 2;
+    // the rows of a pass together fill 64 registers, 128 at head size 256
+    constexpr int PASS = D == 64 ? 4 : 2;
 #pragma unroll
     for (int i = 0; i < 2 * NQ; i += PASS) {
         float x[DT == 3 ? 1 : PASS][NG][8];
         uint2 w[PASS][NG];
 #pragma unroll
         for (int u = 0; u < PASS; ++u) {
-            const int row = row0 + 16 * (i + u) + (lane >> 2);
+            // (rows past the last: that one again, so that no load waits for a branch)
+            int row = row0 + 16 * (i + u) + (lane >> 2);
+            row = row < rows ? row : rows - 1;
             const int tok = div_group(p, row);
             const int64_t elem = int64_t(r.first + tok) * p.q_stride + int64_t(hk * p.group + row - tok * p.group) * D + 8 * L;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-                if constexpr (DT == 3) {
-                    w[u][j] = make_uint2(0u, 0u);
-                    if (row < rows) w[u][j] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.q) + elem + 32 * j);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) x[u][j][k] = 0.f;
-                    if (row < rows) load_x8<DT>(p.q, elem + 32 * j, x[u][j]);
-                }
+                if constexpr (DT == 3) w[u][j] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.q) + elem + 32 * j);
+                else load_x8<DT>(p.q, elem + 32 * j, x[u][j]);
             }
         }
 #pragma unroll
@@ -418,12 +411,14 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     auto octet = [&](unsigned l) { return int(l % (D / 8)); };   // (D / 8 divides 64)
     const int seen_from = p.window > 0 ? lo - p.window + 1 : 0;
     auto unit_scales = [&](unsigned l, int tile, int u) {
-        const int tok = token_of(tile) + kPage * unit_page(l, u) + 4 * int(unit_in(l, u) / (D / 8));
-        // seen by some row: up to the last, and in the first row's window or a first token
-        uint32_t sc = 0u;
+        const int tok0 = token_of(tile), tok = tok0 + kPage * unit_page(l, u) + 4 * int(unit_in(l, u) / (D / 8));
+        uint32_t sc = vscale[u];
+        if (tok0 + TT - 1 > hi || (tok0 < seen_from && tok0 + TT > p.sinks)) {
+            // seen by some row: up to the last, and in the first row's window or a first token
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-            sc |= (tok + t <= hi) & ((tok + t >= seen_from) | (tok + t < p.sinks)) ? vscale[u] & (0xFFu << (8 * t)) : 0u;
+            for (int t = 0; t < 4; ++t)
+                if (!((tok + t <= hi) & ((tok + t >= seen_from) | (tok + t < p.sinks)))) sc &= ~(0xFFu << (8 * t));
+        }
         return sc;
     };
     // Decodes this thread's units into the value buffer, relative to my_base; true
@@ -437,13 +432,22 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             if (!has_unit(u)) continue;
             const int pg = unit_page(l, u), tq = int(unit_in(l, u) / (D / 8));
             const uint32_t bytes = unit_scales(l, tile, u);
-            uint32_t sc = 0u;
+            // the float 2^(byte - base): the byte at a float's exponent, moved by 127 - base
+            // and 0 below the exponent range (a byte above base + 13 may leave it, and
+            // the tile is decoded again)
+            const uint32_t k23 = 23u;
+            const int b[4] = {int(f32_bits(byte_scale0(bytes, k23))), int(f32_bits(byte_scale1(bytes, k23))),
+                              int(f32_bits(byte_scale2(bytes, k23))), int(f32_bits(byte_scale3(bytes, k23)))};
+            const int shift = (127 - my_base) * (1 << 23), limit = (my_base + 13 < 255 ? my_base + 13 : 255) * (1 << 23);
+            float sc[4];
+            int most = b[0];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int rel = int((bytes >> (8 * t)) & 0xFFu) + (127 - my_base);
-                above = above || rel > 127 + 13;
-                sc |= uint32_t(rel > 0 ? rel : 0) << (8 * t);
+                most = most > b[t] ? most : b[t];
+                const int e = int(uint32_t(b[t]) + uint32_t(shift));
+                sc[t] = bits_f32(uint32_t(e > 0 ? e : 0));
             }
+            above = above || most > limit;
             uint2 out[8];
             decode_unit(vcode[u], sc, out);
             uint8_t* dst = &vt[slot][0] + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
@@ -648,16 +652,13 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + TT <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
         compute(tok0, slot, tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks));
     }
-    // the accumulators back to O
-#pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const float f = base[c] == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, base[c] - 127);
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
-    }
-
-    // ---- the row's sum over both halves, then the row itself or its partial
+    // ---- the row's sum over both halves, then the row itself or its partial; the
+    // accumulators back to O (a whole row's after the division by its sum, so that
+    // no finite result overflows on the way)
     if (!busy) return;
+    float back[CB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) back[c] = base[c] == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, base[c] - 127);
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
         float a = l_run[q], b = l_run[q];
@@ -667,6 +668,8 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         const int tok = div_group(p, row);
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
         if (!whole) {
+#pragma unroll
+            for (int c = 0; c < CB; ++c) acc[c][q] *= back[c];
             if (row < rows) {
                 const int64_t part = int64_t(split) * p.num_tokens * p.num_q_heads + out_row;
 #pragma unroll
@@ -681,7 +684,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         }
         const float inv = l > 0.f ? 1.0f / l : 0.f;   // a row that sees nothing is 0
 #pragma unroll
-        for (int c = 0; c < CB; ++c) acc[c][q] *= inv;
+        for (int c = 0; c < CB; ++c) acc[c][q] = acc[c][q] * inv * back[c];
         gather_columns(acc, q, p.rotate_v != 0);
 #pragma unroll
         for (int c = 0; c < CB; ++c)

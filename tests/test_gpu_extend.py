@@ -150,6 +150,26 @@ def test_one_far_scale_in_a_tile(uq):
         assert rel <= REL
 
 
+@pytest.mark.parametrize("first,later", [(0, 124), (0, 254), (124, 254), (254, 120), (100, 113), (100, 114), (1, 140)])
+def test_scales_that_grow_and_shrink_along_the_context(uq, first, later):
+    """A context whose first 100 tokens have one V scale and whose others another: scores are equal (a zero
+    query), so that both weigh in.  Against the sums themselves, at the larger scale's precision."""
+    dev = torch.device("cuda:0")
+    n = 333
+    table, pages = ref.tables([n], dev, 21)
+    desc = uq.CacheDesc(num_kv_heads=1, num_pages=pages, rotate_v=False, head_dim=128)
+    codes, scales = ref.fill_pools(desc, dev, 21)
+    s = scales.view(pages, 1, 2, 4, 16)
+    for t in range(n):
+        s[int(table[0, t // 16]), 0, 1, :, t % 16] = first if t < 100 else later
+    kv = ref.pool_values(desc, codes, scales)
+    q = torch.zeros((3, 4, 128), device=dev)
+    out = uq.extend_attention(desc, q, torch.tensor([0, 3], dtype=torch.int32, device=dev), codes, scales, table,
+                              torch.tensor([n], dtype=torch.int32, device=dev), n, out_dtype=torch.float32)
+    want = ref.attend(desc, kv, q, [0, 3], table, [n])
+    assert float((out.double() - want).norm() / want.norm()) <= REL
+
+
 @pytest.mark.parametrize("gain", [0.0, 30.0, 1e4])
 def test_score_ranges(uq, gain):
     case(uq, [200, 64], [80, 2], 8, 2, 128, seed=10, q_gain=gain)
