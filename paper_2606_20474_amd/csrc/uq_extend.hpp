@@ -39,6 +39,13 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
+// A weight of the binade [2^k, 2^(k+1)) loses 2^-11 2^k on average when it is cut to
+// 11 significant bits, a share of 2^-11 / (2 ln 2) over log-uniform weights: log2 of
+// one plus that, and the inverse of one plus that.  (A weight of 1, lifted and cut,
+// is 1 again.)
+constexpr float kLift = 5.08057e-4f;
+constexpr float kLower = 0.99964790f;
+
 constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
 
 // Tokens per tile: one 16-byte unit of K and one of V for each of 256 threads.
@@ -548,7 +555,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                 }
             }
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) shift[q] = -m_run[q];
+            for (int q = 0; q < NQ; ++q) shift[q] = kLift - m_run[q];
             if (__builtin_expect(big_max, 0)) {
                 // the difference to the rounded product, as m_run was
 #pragma clang fp contract(off)
@@ -556,12 +563,14 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                 for (int q = 0; q < NQ; ++q) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[q][i] = s[q][i] * sl2 - m_run[q];
-                    shift[q] = 0.f;
+                    shift[q] = kLift;
                 }
                 scale = 1.f;
             }
-            // P of tokens 16 mm .. 16 mm + 15 as operand B; the sum is of the weights as PV
-            // sees them
+            // P of tokens 16 mm .. 16 mm + 15 as operand B, cut to FP16 (the conversion that
+            // rounds to nearest takes twice as long, and the sum of pairs by a dot product
+            // shuts out the matrix instructions).  kLift, in the shift, makes up for the
+            // mean of what is cut; the sum, of the lifted weights, is lowered at the end.
             auto weights = [&](int mm, uint4 (&ph)[NQ]) {
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
@@ -570,10 +579,8 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                     for (int i = 0; i < 4; ++i) {
                         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][8 * mm + 2 * i], scale, shift[q]));
                         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][8 * mm + 2 * i + 1], scale, shift[q]));
-                        const v2h h = {_Float16(x), _Float16(y)};
-                        const v2h one = {_Float16(1.0f), _Float16(1.0f)};
-                        w[i] = __builtin_bit_cast(uint32_t, h);
-                        l_run[q] = __builtin_amdgcn_fdot2(h, one, l_run[q], false);
+                        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+                        l_run[q] += x + y;
                     }
                     ph[q] = uint4{w[0], w[1], w[2], w[3]};
                 }
@@ -663,7 +670,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     for (int q = 0; q < NQ; ++q) {
         float a = l_run[q], b = l_run[q];
         swap32(a, b);
-        const float l = a + b;
+        const float l = (a + b) * kLower;
         const int row = w_row0 + 32 * q + col;
         const int tok = div_group(p, row);
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
