@@ -706,6 +706,7 @@ uq_status uq_decode_attention(const uq_cache_desc* desc, const void* q, uq_dtype
 struct ExtendShape {
     int64_t row_blocks;
     int32_t splits;
+    int32_t alone_rows;
     size_t workspace;
 };
 static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
@@ -720,6 +721,9 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
     if (num_tokens >= (int64_t(1) << 24)) return UQ_ERR_UNSUPPORTED;   // rows of a KV head are numbered in 28 bits
     const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
+    // the waves split the tokens of the sequences with few rows where such sequences
+    // are likely the most: few rows on average
+    e.alone_rows = rows <= seqs * uq::extend_alone_rows(desc->head_dim) ? uq::extend_alone_rows(desc->head_dim) : 0;
     e.row_blocks = rows / m + seqs;
     int64_t blocks = (rows + m - 1) / m;   // of a batch of full sequences; at least one each
     blocks = (blocks > seqs ? blocks : seqs) * desc->num_kv_heads;
@@ -795,6 +799,7 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     p.rotate_v = desc->rotate_v != 0;
     p.row_blocks = int32_t(e.row_blocks);
     p.splits = e.splits;
+    p.alone_rows = e.alone_rows;
     p.part_acc = static_cast<float*>(workspace);
     p.part_ml = p.part_acc != nullptr ? p.part_acc + int64_t(e.splits) * num_tokens * num_q_heads * desc->head_dim : nullptr;
     p.out = out;

@@ -138,11 +138,11 @@ __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendR
 
 // One 16-byte unit of a page's V codes (4 tokens x 8 channels, the tokens' scales in
 // sc) as eight pairs of dwords: of each channel the 4 tokens in FP16.
-__device__ __forceinline__ void decode_unit(const uint4& v, const float (&sc)[4], uint2 (&out)[8]) {
+__device__ __forceinline__ void decode_unit(const u32x4& v, const float (&sc)[4], uint2 (&out)[8]) {
     uint32_t w[4][4];   // [token][channel pair]
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const uint32_t d = t == 0 ? v.x : t == 1 ? v.y : t == 2 ? v.z : v.w;
+        const uint32_t d = v[t];
         w[t][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 0));
         w[t][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 1));
         w[t][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, sc[t], 2));
@@ -215,7 +215,7 @@ __device__ __forceinline__ int div_group(const ExtendParams& p, int n) {
 // Tiles per split of a row block with `tiles` of them.
 __host__ __device__ __forceinline__ int extend_per_split(int tiles, int splits) {
     const int per = (tiles + splits - 1) / splits;
-    return per > 2 ? per : 2;
+    return per > 4 ? per : 4;
 }
 
 // The wave's 32 NQ query rows from row0 on, as FP8 in operand order at `qs`: a quad
@@ -265,44 +265,76 @@ __device__ __forceinline__ void stage_queries(const ExtendParams& p, const Exten
     }
 }
 
-// One block's walk: NQ blocks of 32 rows per wave, W waves.  Per tile a thread
-// moves one or two 16-byte units of K and of V: loaded into registers while the
-// tile before is computed (the page ids one tile earlier still), stored to the
-// other of two LDS buffers after it, K as it is and V decoded; one barrier per
-// tile.
-template <int D, int NQ, int W>
-__global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
-    constexpr int TT = extend_tile<D>();
-    constexpr int M = 32 * NQ * W;            // rows of the block
-    constexpr int NT = 64 * W;
-    constexpr int KS = D / 64;                // k steps of QK^T
-    constexpr int CB = D / 32;                // channel blocks of PV
-    constexpr int kPageUnits = D / 2;         // 16-byte units of a page's K, and of its V
-    constexpr int kUnits = TT / kPage * kPageUnits;
-    constexpr int UR = (kUnits + NT - 1) / NT;
+// Two parts of a row, running maxima m and sums l: the first becomes both, and the
+// share of the second in it is returned.
+__device__ __forceinline__ float join_share(float& m, float& l, float m2, float l2) {
+    const float top = __builtin_fmaxf(m, m2);
+    const float a = l * __builtin_amdgcn_exp2f(m - top), b = l2 * __builtin_amdgcn_exp2f(m2 - top);
+    m = top;
+    l = a + b;
+    return b > 0.f ? b / l : 0.f;
+}
+
+// Tokens per tile and shared memory of a walk.  ALONE: a wave walks tiles of its
+// own (one in W), with buffers of its own.
+template <int D, int W, bool ALONE> struct ExtendShape {
+    static constexpr int CB = D / 32;
+    static constexpr int TT = !ALONE ? extend_tile<D>() : D == 64 ? 64 : 32;
     // decoded values of a tile: [page][32 channels][half][channel][8 tokens], the
     // (channel block, half) rows 16 bytes apart in banks, so that neither the stores
     // (8 bytes per channel) nor the loads (16 bytes per lane) meet in a bank
-    constexpr int kVRow = 32 * 16 + 16;
-    constexpr int kVt = TT / kPage * CB * 2 * kVRow;
-    constexpr int kK = TT * D / 2;            // K codes of a tile
-    __shared__ __attribute__((aligned(16))) uint8_t vt[2][kVt];
-    __shared__ __attribute__((aligned(16))) uint8_t kt[2][kK];
-    __shared__ __attribute__((aligned(16))) uint8_t kst[2][TT / kPage * D / 2];
-    __shared__ int grow[2];                   // a scale above FP16's range in the tile
-    __shared__ int top[CB];                   // largest scale byte of the tile, per 32 channels (when one grows)
-    __shared__ int base[CB];                  // scale byte the values are relative to: 127 + e
-    static_assert(M * D <= 2 * kVt, "the query operand is staged in the value buffers");
+    static constexpr int kVRow = 32 * 16 + 16;
+    static constexpr int kVt = TT / kPage * CB * 2 * kVRow;
+    static constexpr int kK = TT * D / 2;                 // K codes of a tile
+    static constexpr int kKs = TT / kPage * D / 2;        // and their scales
+    static constexpr int kBuffers = ALONE ? 1 : 2;
+    static constexpr int kState = 16 + 8 * CB;            // grow, top, base
+    static constexpr int kWalker = kBuffers * (kVt + kK + kKs) + kState;
+    static constexpr int kLds = (ALONE ? W : 1) * kWalker;
+};
+
+// The walk of a block over tiles first_tile .. last_tile - 1, NQ blocks of 32 rows per
+// wave, W waves: of different rows that share each tile, or (ALONE) of the same
+// rows, every wave with tiles of its own.  Per tile a thread moves 16-byte units of
+// K and of V: loaded into registers while the tile before is computed (the page ids
+// one tile earlier still), stored to LDS after it, K as it is and V decoded.  Two
+// buffers and one barrier per tile; a wave alone needs one buffer and none.
+template <int D, int NQ, int W, bool ALONE>
+__device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r, int hk, int split, uint8_t* smem) {
+    using Shape = ExtendShape<D, W, ALONE>;
+    constexpr int TT = Shape::TT, CB = Shape::CB, kVRow = Shape::kVRow;
+    constexpr int M = 32 * NQ * (ALONE ? 1 : W);   // rows of the block
+    constexpr int NT = ALONE ? 64 : 64 * W;        // threads that share a tile
+    constexpr int KS = D / 64;                     // k steps of QK^T
+    constexpr int kPageUnits = D / 2;              // 16-byte units of a page's K, and of its V
+    constexpr int kUnits = TT / kPage * kPageUnits;
+    constexpr int UR = (kUnits + NT - 1) / NT;
+    constexpr int STEP = ALONE ? W : 1;            // tiles from one of this walker's to the next
+    static_assert(32 * NQ * D * (ALONE ? 1 : W) <= Shape::kBuffers * Shape::kVt, "the query operand is staged in the value buffers");
     static_assert(kUnits % 64 == 0 && kUnits % NT % 64 == 0, "units go to whole waves");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int uw = ALONE ? 0 : wave;               // wave among those that share a tile
     const int half = lane >> 5, col = lane & 31;
-    const int hk = int(blockIdx.x % unsigned(p.num_kv_heads));
-    const int rest = int(blockIdx.x / unsigned(p.num_kv_heads));
-    const int split = rest % p.splits;
-    ExtendRows r;
-    if (!extend_find<M>(p, rest / p.splits, r)) return;
+    uint8_t* const mine = smem + (ALONE ? wave : 0) * Shape::kWalker;
+    auto vt = [&](int slot) { return mine + slot * Shape::kVt; };
+    auto kt = [&](int slot) { return mine + Shape::kBuffers * Shape::kVt + slot * Shape::kK; };
+    auto kst = [&](int slot) { return mine + Shape::kBuffers * (Shape::kVt + Shape::kK) + slot * Shape::kKs; };
+    int* const grow = reinterpret_cast<int*>(mine + Shape::kWalker - Shape::kState);   // a scale above FP16's range in the tile
+    int* const top = grow + 4;     // largest scale byte of the tile, per 32 channels (when one grows)
+    int* const base = top + CB;    // scale byte the values are relative to: 127 + e
+    // the waves that share a tile; a wave's own LDS accesses are in order
+    auto sync = [&]() {
+        if constexpr (ALONE) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        } else {
+            __syncthreads();
+        }
+    };
+
     int lo, hi;
     extend_span<M>(p, r, lo, hi);
     extend_tiles<TT>(p, lo, hi, r);
@@ -320,18 +352,19 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // ---- queries: rotated and cast to FP8 (unless they are), to the lane order
     // of the B operand: k step s, lane (row, half): bytes 0..15 are channels
     // 64 s + 16 half .., 16..31 are 64 s + 32 + 16 half ..
-    uint8_t* qs = &vt[0][0] + wave * (32 * NQ * D);
-    const int w_row0 = r.row0 + wave * (32 * NQ);
+    uint8_t* qs = vt(0) + uw * (32 * NQ * D);
+    const int w_row0 = r.row0 + uw * (32 * NQ);
     if (p.q_dtype == 0) stage_queries<0, D, NQ>(p, r, hk, w_row0, qs);
     else if (p.q_dtype == 1) stage_queries<1, D, NQ>(p, r, hk, w_row0, qs);
     else if (p.q_dtype == 2) stage_queries<2, D, NQ>(p, r, hk, w_row0, qs);
     else stage_queries<3, D, NQ>(p, r, hk, w_row0, qs);
-    if (tid < 2) grow[tid] = 0;
-    if (tid < CB) {
-        top[tid] = 0;
-        base[tid] = kNoBase;
+    const int wtid = ALONE ? lane : tid;
+    if (wtid < 2) grow[wtid] = 0;
+    if (wtid < CB) {
+        top[wtid] = 0;
+        base[wtid] = kNoBase;
     }
-    __syncthreads();
+    sync();
     v8i qop[NQ][KS];
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
@@ -341,7 +374,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             const uint4 a = src[0], c = src[1];
             qop[q][s] = v8i{int(a.x), int(a.y), int(a.z), int(a.w), int(c.x), int(c.y), int(c.z), int(c.w)};
         }
-    __syncthreads();
+    sync();
 
     // the wave's first and last position (a wave without rows only moves tiles)
     const bool busy = w_row0 < rows;
@@ -356,7 +389,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // D / 8 units of a page also move 4 of its K scales each.  A page takes whole
     // waves from head size 128 on: its id and addresses are scalars then.
     int32_t ids[UR];
-    uint4 kcode[UR], vcode[UR];
+    u32x4 kcode[UR], vcode[UR];
     uint32_t vscale[UR], kscale[UR];
     int my_base = kNoBase;      // base[] of its units' channels
     constexpr bool kWavePages = kPageUnits % 64 == 0;
@@ -370,12 +403,12 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         return l;
     };
     auto unit_page = [&](unsigned l, int u) {
-        return kWavePages ? (64 * wave + u * NT) / kPageUnits : int(64 * wave + u * NT + l) / kPageUnits;
+        return kWavePages ? (64 * uw + u * NT) / kPageUnits : int(64 * uw + u * NT + l) / kPageUnits;
     };
     auto unit_in = [&](unsigned l, int u) {
-        return kWavePages ? unsigned((64 * wave + u * NT) % kPageUnits) + l : (64u * wave + u * NT + l) % kPageUnits;
+        return kWavePages ? unsigned((64 * uw + u * NT) % kPageUnits) + l : (64u * uw + u * NT + l) % kPageUnits;
     };
-    auto has_unit = [&](int u) { return (u + 1) * NT <= kUnits || 64 * wave + u * NT < kUnits; };   // whole waves
+    auto has_unit = [&](int u) { return (u + 1) * NT <= kUnits || 64 * uw + u * NT < kUnits; };   // whole waves
     auto load_ids = [&](int tile) {
         const unsigned l = fresh_lane();
         const int page0 = token_of(tile) / kPage;
@@ -396,8 +429,8 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             const unsigned in = unit_in(l, u);
             const uint8_t* codes = p.codes + ph * (16 * D);
             const uint8_t* scales = p.scales + ph * D;
-            kcode[u] = *reinterpret_cast<const uint4*>(codes + 16 * in);
-            vcode[u] = *reinterpret_cast<const uint4*>(codes + 8 * D + 16 * in);
+            kcode[u] = *reinterpret_cast<const u32x4*>(codes + 16 * in);
+            vcode[u] = *reinterpret_cast<const u32x4*>(codes + 8 * D + 16 * in);
             vscale[u] = *reinterpret_cast<const uint32_t*>(scales + D / 2 + (in % (D / 8) >> 2) * 16 + 4 * (in / (D / 8)));
             if (in < D / 8) kscale[u] = *reinterpret_cast<const uint32_t*>(scales + 4 * in);
         }
@@ -408,8 +441,8 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
         for (int u = 0; u < UR; ++u) {
             if (!has_unit(u)) continue;
             const unsigned in = unit_in(l, u);
-            *reinterpret_cast<uint4*>(&kt[slot][0] + 16 * (64 * wave + u * NT + l)) = kcode[u];
-            if (in < D / 8) *reinterpret_cast<uint32_t*>(&kst[slot][0] + unit_page(l, u) * (D / 2) + 4 * in) = kscale[u];
+            *reinterpret_cast<u32x4*>(kt(slot) + 16 * (64 * uw + u * NT + l)) = kcode[u];
+            if (in < D / 8) *reinterpret_cast<uint32_t*>(kst(slot) + unit_page(l, u) * (D / 2) + 4 * in) = kscale[u];
         }
     };
     // The scale bytes of unit u; tokens that no row of the block sees may hold
@@ -457,7 +490,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             above = above || most > limit;
             uint2 out[8];
             decode_unit(vcode[u], sc, out);
-            uint8_t* dst = &vt[slot][0] + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
+            uint8_t* dst = vt(slot) + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + 16 * i) = out[i];
         }
@@ -483,9 +516,9 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     // beside the products of the first.
     auto compute = [&](int tok0, int slot, bool clear) {
         const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
-        const uint8_t* v_at = &vt[slot][0] + lh * kVRow + 16 * lc;
-        const uint8_t* k_at = &kt[slot][0] + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
-        const uint8_t* s_at = &kst[slot][0] + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
+        const uint8_t* v_at = vt(slot) + lh * kVRow + 16 * lc;
+        const uint8_t* k_at = kt(slot) + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
+        const uint8_t* s_at = kst(slot) + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
         v16f s[NQ];
         auto scores = [&](int tb) {
             uint4 ka[KS];
@@ -614,7 +647,7 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) atomicMax(&top[octet(lane) >> 2], int((bytes >> (8 * i)) & 0xFFu));
         }
-        __syncthreads();
+        sync();
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             const int old = base[c], now = top[c] - 8 > old ? top[c] - 8 : old;
@@ -623,60 +656,108 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             for (int q = 0; q < NQ; ++q) acc[c][q] *= f;
         }
         my_base = top[octet(lane) >> 2] - 8 > my_base ? top[octet(lane) >> 2] - 8 : my_base;
-        __syncthreads();
-        if (tid < CB) {
-            base[tid] = top[tid] - 8 > base[tid] ? top[tid] - 8 : base[tid];
-            top[tid] = 0;
+        sync();
+        if (wtid < CB) {
+            base[wtid] = top[wtid] - 8 > base[wtid] ? top[wtid] - 8 : base[wtid];
+            top[wtid] = 0;
         }
     };
 
-    // ---- the walk.  While tile t is computed, t + 1 is on its way into registers and
-    // t + 2's page ids too.  (Past the last tile in pages that exist.)  Nobody is left
-    // in tile t - 2 when t is stored, to its buffers.
+    // ---- the walk.  While a tile is computed, the walker's next is on its way into
+    // registers and the page ids of the one after too.  (Past the last tile in pages
+    // that exist.)  Nobody is left in the tile before the last when a tile is stored
+    // to its buffers.
+    if constexpr (ALONE) first_tile += wave;
     if (first_tile < last_tile) {
         load_ids(first_tile);
         load_tile();
-        load_ids(first_tile + 1);
+        load_ids(first_tile + STEP);
         set_base(first_tile);
     }
-    for (int t = first_tile; t < last_tile; ++t) {
-        const int slot = (t - first_tile) & 1;
+    for (int t = first_tile, slot = 0; t < last_tile; t += STEP, slot ^= ALONE ? 0 : 1) {
         store_k(slot);
         if (store_v(t, slot)) grow[slot] = 1;
-        __syncthreads();
+        sync();
         if (__builtin_expect(grow[slot] != 0, 0)) {
             // rare: a scale above the range.  The tile is decoded again.
-            __syncthreads();
-            if (tid == 0) grow[slot] = 0;
+            sync();
+            if (wtid == 0) grow[slot] = 0;
             set_base(t);
             store_v(t, slot);
-            __syncthreads();
+            sync();
         }
         load_tile();
-        load_ids(t + 2);
+        load_ids(t + 2 * STEP);
         const int tok0 = token_of(t);
         // tiles past the wave's last row, or before its windows and after the sinks
         if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + TT <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
         compute(tok0, slot, tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks));
     }
-    // ---- the row's sum over both halves, then the row itself or its partial; the
-    // accumulators back to O (a whole row's after the division by its sum, so that
-    // no finite result overflows on the way)
-    if (!busy) return;
+
+    // ---- the row's sum over both halves, the accumulators divided by it and back to
+    // O, then the row itself or its partial.  (Parts of a row are averages with their
+    // sums as weights, so that no finite result overflows on the way.)
+    if (!ALONE && !busy) return;
     float back[CB];
 #pragma unroll
     for (int c = 0; c < CB; ++c) back[c] = base[c] == kNoBase ? 0.0f : __builtin_ldexpf(1.0f, base[c] - 127);
+    float l_row[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
         float a = l_run[q], b = l_run[q];
         swap32(a, b);
-        const float l = (a + b) * kLower;
+        l_row[q] = (a + b) * kLower;
+        const float inv = l_row[q] > 0.f ? 1.0f / l_row[q] : 0.f;   // a row that sees nothing is 0
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[c][q] = acc[c][q] * inv * back[c];
+    }
+    if constexpr (ALONE) {
+        // the waves' parts of the rows, one after another through LDS into wave 0's
+        float4* const part = reinterpret_cast<float4*>(smem);
+        float2* const ml = reinterpret_cast<float2*>(smem + CB * NQ * 4 * 1024);
+        static_assert(CB * NQ * 4 * 1024 + NQ * 512 <= Shape::kLds, "a wave's part fits");
+        for (int w = 1; w < W; ++w) {
+            __syncthreads();
+            if (wave == w) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            part[((q * CB + c) * 4 + i) * 64 + lane] =
+                                make_float4(acc[c][q][4 * i], acc[c][q][4 * i + 1], acc[c][q][4 * i + 2], acc[c][q][4 * i + 3]);
+                    ml[q * 64 + lane] = make_float2(m_run[q], l_row[q]);
+                }
+            }
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    const float2 o = ml[q * 64 + lane];
+                    const float g = join_share(m_run[q], l_row[q], o.x, o.y);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 x = part[((q * CB + c) * 4 + i) * 64 + lane];
+                            acc[c][q][4 * i] = acc[c][q][4 * i] * (1.0f - g) + x.x * g;
+                            acc[c][q][4 * i + 1] = acc[c][q][4 * i + 1] * (1.0f - g) + x.y * g;
+                            acc[c][q][4 * i + 2] = acc[c][q][4 * i + 2] * (1.0f - g) + x.z * g;
+                            acc[c][q][4 * i + 3] = acc[c][q][4 * i + 3] * (1.0f - g) + x.w * g;
+                        }
+                }
+            }
+        }
+        if (wave != 0) return;
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const float l = l_row[q];
         const int row = w_row0 + 32 * q + col;
         const int tok = div_group(p, row);
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
         if (!whole) {
-#pragma unroll
-            for (int c = 0; c < CB; ++c) acc[c][q] *= back[c];
             if (row < rows) {
                 const int64_t part = int64_t(split) * p.num_tokens * p.num_q_heads + out_row;
 #pragma unroll
@@ -689,9 +770,6 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             }
             continue;
         }
-        const float inv = l > 0.f ? 1.0f / l : 0.f;   // a row that sees nothing is 0
-#pragma unroll
-        for (int c = 0; c < CB; ++c) acc[c][q] = acc[c][q] * inv * back[c];
         gather_columns(acc, q, p.rotate_v != 0);
 #pragma unroll
         for (int c = 0; c < CB; ++c)
@@ -711,6 +789,26 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
                 }
             }
     }
+}
+
+// MIXED: sequences with up to p.alone_rows rows of a KV head are walked by waves that
+// split the tokens.  (Both walks in one kernel cost the other some registers, so it
+// is a kernel of its own.)
+template <int D, int NQ, int W, bool MIXED>
+__global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
+    constexpr int kTogetherLds = ExtendShape<D, W, false>::kLds, kAloneLds = MIXED ? ExtendShape<D, W, true>::kLds : 0;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[kTogetherLds > kAloneLds ? kTogetherLds : kAloneLds];
+    const int hk = int(blockIdx.x % unsigned(p.num_kv_heads));
+    const int rest = int(blockIdx.x / unsigned(p.num_kv_heads));
+    ExtendRows r;
+    if (!extend_find<32 * NQ * W>(p, rest / p.splits, r)) return;
+    if constexpr (MIXED) {
+        if (r.count * p.group <= p.alone_rows) {
+            extend_walk<D, 2, W, true>(p, r, hk, rest % p.splits, smem);
+            return;
+        }
+    }
+    extend_walk<D, NQ, W, false>(p, r, hk, rest % p.splits, smem);
 }
 
 // Joins the partials of every (token, query head): 16 lanes per row, N channels
@@ -738,7 +836,8 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     r.row0 = ((t - r.first) * p.group + hq % p.group) / M * M;
     int plo, phi;
     extend_span<M>(p, r, plo, phi);
-    extend_tiles<extend_tile<D>()>(p, plo, phi, r);
+    if (r.count * p.group <= p.alone_rows) extend_tiles<ExtendShape<D, 4, true>::TT>(p, plo, phi, r);
+    else extend_tiles<extend_tile<D>()>(p, plo, phi, r);
     const int per = extend_per_split(r.tiles, p.splits);
     if (r.tiles <= per) return;   // written by the first launch
     const int parts = (r.tiles + per - 1) / per;
@@ -759,16 +858,10 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
             a[4 * i + 2] = v.z;
             a[4 * i + 3] = v.w;
         }
-        const float mn = __builtin_fmaxf(m, ml.x);
-        const float fo = __builtin_amdgcn_exp2f(m - mn), fn = __builtin_amdgcn_exp2f(ml.x - mn);
-        l = l * fo + ml.y * fn;
+        const float g = join_share(m, l, ml.x, ml.y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = o[i] * fo + a[i] * fn;
-        m = mn;
+        for (int i = 0; i < N; ++i) o[i] = o[i] * (1.0f - g) + a[i] * g;
     }
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] *= inv;
     if (p.rotate_v) wht_x<N>(o, L);
     const int64_t at = row * D + N * L;
 #pragma unroll
@@ -784,8 +877,13 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
 
 template <int D, int NQ, int W>
 static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) {
-    const unsigned blocks = unsigned(int64_t(p.row_blocks) * p.num_kv_heads * p.splits);
-    launch_kernel(extend_kernel<D, NQ, W>, dim3(blocks), dim3(64 * W), stream, p);
+    const dim3 grid{unsigned(int64_t(p.row_blocks) * p.num_kv_heads * p.splits)}, block{64u * W};
+    if (p.alone_rows > 0) {
+        if constexpr (D <= 128) launch_kernel(extend_kernel<D, NQ, W, true>, grid, block, stream, p);
+        else return hipErrorInvalidValue;   // (not asked for)
+    } else {
+        launch_kernel(extend_kernel<D, NQ, W, false>, grid, block, stream, p);
+    }
     if (p.splits > 1) {
         const int64_t rows = int64_t(p.num_tokens) * p.num_q_heads;
         hipLaunchKernelGGL((extend_merge_kernel<D, 32 * NQ * W>), dim3(unsigned((rows + 15) / 16)), dim3(256), 0, stream, p);
@@ -794,6 +892,7 @@ static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) 
 }
 
 int extend_block_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
+int extend_alone_rows(int head_dim) { return head_dim == 256 ? 0 : 64; }
 
 hipError_t launch_extend(const ExtendParams& p, hipStream_t stream) {
     if (p.head_dim == 64) return launch_extend_with<64, 2, 4>(p, stream);

@@ -193,6 +193,7 @@ struct ExtendParams {
     int32_t rotate_v;
     int32_t row_blocks;        // bound of the batch's row blocks per KV head
     int32_t splits;            // blocks that share a row block's tiles
+    int32_t alone_rows;        // rows of a sequence and KV head up to which the waves split its tokens, or 0
     float* part_acc;           // [splits][T][Hq][d]
     float* part_ml;            // [splits][T][Hq][2]
     void* out;                 // [T][Hq][d]
@@ -200,6 +201,10 @@ struct ExtendParams {
 };
 // Rows (query, query head of one KV head) of a block of the extend kernel.
 int extend_block_rows(int head_dim);
+// Rows of a (sequence, KV head) up to which its block's waves can split the tokens
+// instead of the rows (0: they cannot; 4 walkers' buffers of head size 256 would
+// leave a CU one block).
+int extend_alone_rows(int head_dim);
 hipError_t launch_extend(const ExtendParams& p, hipStream_t stream);
 
 struct PlanParams {
