@@ -128,6 +128,64 @@ __device__ __forceinline__ bool extend_find(const ExtendParams& p, int at, Exten
     return false;
 }
 
+// The same with the row blocks of all sequences (at most 64, one per lane) in
+// descending order of their last position, to a 32nd of the longest context: blocks
+// of different sequences differ by the whole context, and a long one that starts
+// last leaves the others' CUs idle.  above(j): blocks that end at or past the j-th
+// 32nd; `at` falls into the largest j with more than `at` of them.
+template <int M>
+__device__ __forceinline__ bool extend_find_longest(const ExtendParams& p, int at, ExtendRows& r) {
+    const int lane = threadIdx.x & 63;
+    int first = 0, count = 0, n = 0;
+    if (lane < p.batch) {
+        first = extend_first(p, lane);
+        count = extend_first(p, lane + 1) - first;
+        count = count > 0 ? count : 0;
+        n = extend_context(p, lane);
+    }
+    const int blocks = int((int64_t(count) * p.group + M - 1) / M);
+    const int start = n - count;
+    auto total = [&](int x) {
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
+        return __builtin_amdgcn_readfirstlane(x);
+    };
+    int top = n;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int o = __shfl_xor(top, s);
+        top = top > o ? top : o;
+    }
+    const int width = __builtin_amdgcn_readfirstlane(top) / 32 + 1;
+    auto above = [&](int j) {
+        const int64_t from = int64_t(j) * width;
+        if (j == 0 || from <= start) return blocks;
+        return from >= n ? 0 : blocks - int((from - start) * p.group / M);
+    };
+    if (total(blocks) <= at) return false;
+    int lo = 0, hi = 32;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (total(above(mid)) > at) lo = mid; else hi = mid;
+    }
+    const int longer = above(hi), here = above(lo) - longer;
+    const int rank = at - total(longer);
+    int sum = here;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int o = __shfl_up(sum, s);
+        if (lane >= s) sum += o;
+    }
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > rank));
+    r.b = l;
+    r.first = __builtin_amdgcn_readlane(first, l);
+    r.count = __builtin_amdgcn_readlane(count, l);
+    r.n_ctx = __builtin_amdgcn_readlane(n, l);
+    const int i = rank - __builtin_amdgcn_readlane(sum - here, l);
+    r.row0 = (__builtin_amdgcn_readlane(blocks - longer, l) - 1 - i) * M;
+    return true;
+}
+
 // Positions of a row block's first and last row.
 template <int M>
 __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendRows& r, int& lo, int& hi) {
@@ -801,7 +859,9 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     const int hk = int(blockIdx.x % unsigned(p.num_kv_heads));
     const int rest = int(blockIdx.x / unsigned(p.num_kv_heads));
     ExtendRows r;
-    if (!extend_find<32 * NQ * W>(p, rest / p.splits, r)) return;
+    const bool found = p.longest_first ? extend_find_longest<32 * NQ * W>(p, rest / p.splits, r)
+                                       : extend_find<32 * NQ * W>(p, rest / p.splits, r);
+    if (!found) return;
     if constexpr (MIXED) {
         if (r.count * p.group <= p.alone_rows) {
             extend_walk<D, 2, W, true>(p, r, hk, rest % p.splits, smem);

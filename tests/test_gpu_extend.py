@@ -222,3 +222,16 @@ def test_bad_device_indices_stay_in_bounds(uq):
                                   torch.tensor([1000, -3], dtype=torch.int32, device=dev), 64, window=20, sinks=1)
         torch.cuda.synchronize()
         assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("batch", [2, 40, 64, 65])
+def test_more_blocks_than_run_at_once(uq, d, batch):
+    """Ragged sequences, also empty ones and ones with more queries than context: their blocks run
+    longest first up to 64 sequences, in order beyond."""
+    g = torch.Generator().manual_seed(batch)
+    lens = [int(x) for x in torch.randint(0, 400, (batch,), generator=g)]
+    news = [int(x) for x in torch.randint(0, 5000 if batch == 2 else 200, (batch,), generator=g)]
+    news = [n if i % 7 == 0 or batch == 2 else min(n, m) for i, (n, m) in enumerate(zip(news, lens))]
+    lens[1], news[1] = (3500, 3400) if batch == 2 else (0, 0)
+    case(uq, lens, news, 32 if batch > 2 else 256, 16, d, seed=batch + d)
