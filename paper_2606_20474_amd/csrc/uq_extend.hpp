@@ -338,10 +338,13 @@ __device__ __forceinline__ float join_share(float& m, float& l, float m2, float 
 template <int D, int W, bool ALONE> struct ExtendShape {
     static constexpr int CB = D / 32;
     static constexpr int TT = !ALONE ? extend_tile<D>() : D == 64 ? 64 : 32;
-    // decoded values of a tile: [page][32 channels][half][channel][8 tokens], the
-    // (channel block, half) rows 16 bytes apart in banks, so that neither the stores
-    // (8 bytes per channel) nor the loads (16 bytes per lane) meet in a bank
-    static constexpr int kVRow = 32 * 16 + 16;
+    // decoded values of a tile: [page][32 channels][half][8 channels][channel][8 tokens].
+    // The loads take 16 bytes per lane, lane = channel; the stores 16 bytes (of a
+    // channel) per lane, lane = octet of channels.  Octets 144 bytes and the 32-channel
+    // blocks 16 banks apart: 8 lanes of either meet in no bank.
+    static constexpr int kVOctet = 8 * 16 + 16;
+    static constexpr int kVRow = 4 * kVOctet + 32;
+    static_assert(2 * kVRow % 128 == 64 && kVOctet % 128 == 16, "bank layout");
     static constexpr int kVt = TT / kPage * CB * 2 * kVRow;
     static constexpr int kK = TT * D / 2;                 // K codes of a tile
     static constexpr int kKs = TT / kPage * D / 2;        // and their scales
@@ -360,7 +363,7 @@ template <int D, int W, bool ALONE> struct ExtendShape {
 template <int D, int NQ, int W, bool ALONE>
 __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r, int hk, int split, uint8_t* smem) {
     using Shape = ExtendShape<D, W, ALONE>;
-    constexpr int TT = Shape::TT, CB = Shape::CB, kVRow = Shape::kVRow;
+    constexpr int TT = Shape::TT, CB = Shape::CB, kVRow = Shape::kVRow, kVOctet = Shape::kVOctet;
     constexpr int M = 32 * NQ * (ALONE ? 1 : W);   // rows of the block
     constexpr int NT = ALONE ? 64 : 64 * W;        // threads that share a tile
     constexpr int KS = D / 64;                     // k steps of QK^T
@@ -548,9 +551,26 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
             above = above || most > limit;
             uint2 out[8];
             decode_unit(vcode[u], sc, out);
-            uint8_t* dst = vt(slot) + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + 128 * (oct & 3) + (tq >> 1) * 8;
+            uint8_t* dst = vt(slot) + ((pg * CB + (oct >> 2)) * 2 + (tq & 1)) * kVRow + kVOctet * (oct & 3);
+            if constexpr (D <= 128) {
+                // the lane of tq ^ 2, D / 4 lanes away, has the other 4 tokens of the 16 bytes:
+                // the two exchange, and each stores 4 of the 8 channels (8-byte stores
+                // meet in a bank four at a time and took the LDS 4 times as long)
+                dst += (tq >> 1) * 64;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + 16 * i) = out[i];
+                for (int i = 0; i < 4; ++i) {
+                    const uint2 a = out[i], b = out[i + 4];
+                    const auto x = D == 128 ? __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false)
+                                            : __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
+                    const auto y = D == 128 ? __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false)
+                                            : __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+                    *reinterpret_cast<uint4*>(dst + 16 * i) = make_uint4(x[0], y[0], x[1], y[1]);
+                }
+            } else {
+                // (that lane is one of another wave)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(dst + 8 * (tq >> 1) + 16 * i) = out[i];
+            }
         }
         return above;
     };
@@ -574,7 +594,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     // beside the products of the first.
     auto compute = [&](int tok0, int slot, bool clear) {
         const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
-        const uint8_t* v_at = vt(slot) + lh * kVRow + 16 * lc;
+        const uint8_t* v_at = vt(slot) + lh * kVRow + 16 * lc + (kVOctet - 128) * (lc >> 3);
         const uint8_t* k_at = kt(slot) + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
         const uint8_t* s_at = kst(slot) + (lc >> 4) * (D / 2) + lh * 16 + (lc & 15);
         v16f s[NQ];
