@@ -707,6 +707,8 @@ struct ExtendShape {
     int64_t row_blocks;
     int32_t splits;
     int32_t alone_rows;
+    bool shared;           // contexts are split into shares of one length
+    size_t partials;       // bytes of them
     size_t workspace;
 };
 static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
@@ -722,7 +724,8 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
     const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
     // the waves split the tokens of the sequences with few rows where such sequences
-    // are likely the most: few rows on average
+    // are likely the most: few rows on average (the same batch, 40 rows each: 130 us,
+    // 207 us where the waves split the rows, most of them idle)
     e.alone_rows = rows <= seqs * uq::extend_alone_rows(desc->head_dim) ? uq::extend_alone_rows(desc->head_dim) : 0;
     e.row_blocks = rows / m + seqs;
     int64_t blocks = (rows + m - 1) / m;   // of a batch of full sequences; at least one each
@@ -733,14 +736,27 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
         walk = most < walk ? most : walk;
     }
     const int64_t tiles = (walk + 63) / 64;
+    // two blocks per CU (16 sequences of 5 tokens over 8k to 24k, 128 row blocks: 132
+    // us; 4, 8 and 16 per CU 141, 159 and 212 us)
     int64_t splits = blocks > 0 ? (2 * uq::kNumCus + blocks - 1) / blocks : 1;
     splits = splits < tiles / 4 ? splits : tiles / 4;
     e.splits = int32_t(splits < 1 ? 1 : splits);
-    if (e.row_blocks * desc->num_kv_heads * e.splits > 0x7FFFFFFF) return UQ_ERR_UNSUPPORTED;
+    // few rows of sequences with different contexts: shares of one length rather than
+    // as many for each (16 sequences of 5 tokens over 8k to 24k: 117 us, 130 with equal
+    // numbers), in as many blocks as run at once; a sequence may have 4 times the
+    // mean number
+    e.shared = e.splits > 1 && e.alone_rows > 0 && window == 0 && batch > 1 && batch <= 64;
+    if (e.shared) {
+        const int64_t at_once = 2 * uq::kNumCus / desc->num_kv_heads;
+        e.row_blocks = e.row_blocks > at_once ? e.row_blocks : at_once;
+        e.splits *= 4;
+    }
+    if (e.row_blocks * desc->num_kv_heads * (e.shared ? 1 : e.splits) > 0x7FFFFFFF) return UQ_ERR_UNSUPPORTED;
     if (num_tokens * num_q_heads > (int64_t(1) << 34)) return UQ_ERR_UNSUPPORTED;   // blocks of the join
-    e.workspace = e.splits > 1 ? size_t(e.splits) * size_t(num_tokens) * size_t(num_q_heads) *
-                                     size_t(desc->head_dim + 2) * sizeof(float)
-                               : 0;
+    e.partials = e.splits > 1 ? size_t(e.splits) * size_t(num_tokens) * size_t(num_q_heads) *
+                                    size_t(desc->head_dim + 2) * sizeof(float)
+                              : 0;
+    e.workspace = e.partials + (e.shared ? 16 : 0);
     return UQ_OK;
 }
 
@@ -803,9 +819,10 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     // blocks that do not all run at once, of sequences with different contexts (12
     // chunks behind contexts of up to 32k tokens, 2576 blocks: 2356 us, 2797 in the
     // sequences' order; the order is kept where every block has a window's length)
-    p.longest_first = window == 0 && batch > 1 && batch <= 64 && e.row_blocks * p.num_kv_heads > 2 * uq::kNumCus;
+    p.longest_first = window == 0 && !e.shared && batch > 1 && batch <= 64 && e.row_blocks * p.num_kv_heads > 2 * uq::kNumCus;
     p.part_acc = static_cast<float*>(workspace);
     p.part_ml = p.part_acc != nullptr ? p.part_acc + int64_t(e.splits) * num_tokens * num_q_heads * desc->head_dim : nullptr;
+    p.share = e.shared ? reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + e.partials) : nullptr;
     p.out = out;
     p.out_dtype = out_dtype == UQ_F32 ? 0 : 1;
     return from_hip(uq::launch_extend(p, static_cast<hipStream_t>(stream)));

@@ -60,6 +60,8 @@ struct ExtendRows {
     int sink_tiles;     // tiles of the first tokens, ahead of the others
     int tile0;          // first of the other tiles
     int tiles;          // all of them
+    int split;          // the block's share of the tiles
+    int share;          // tokens per split, or 0: p.splits equal ones
 };
 
 // Tiles that rows with positions lo .. hi see.
@@ -87,6 +89,14 @@ __device__ __forceinline__ int extend_context(const ExtendParams& p, int b) {
     int n = p.context_lens[b];
     n = n < p.max_context ? n : p.max_context;
     return n > 0 ? n : 0;
+}
+
+// Tiles per split of a row block with `tiles` of them: of a number of splits, or of
+// `share` tokens each.
+template <int TT>
+__device__ __forceinline__ int extend_per_split(int tiles, int splits, int share) {
+    const int per = share > 0 ? (share - 1) / TT + 1 : (tiles + splits - 1) / splits;
+    return per > 4 ? per : 4;
 }
 
 // Row block `at` of the batch, M rows each, the blocks of one sequence from its
@@ -186,6 +196,73 @@ __device__ __forceinline__ bool extend_find_longest(const ExtendParams& p, int a
     return true;
 }
 
+// Block `at` where every row block has p.splits of them.
+template <int M>
+__device__ __forceinline__ bool extend_find_split(const ExtendParams& p, int at, ExtendRows& r) {
+    r.split = at % p.splits;
+    r.share = 0;
+    return p.longest_first ? extend_find_longest<M>(p, at / p.splits, r) : extend_find<M>(p, at / p.splits, r);
+}
+
+// Row block and split `at` of a batch (at most 64 sequences, one per lane, no
+// window) whose contexts are split into shares of the same length: the smallest
+// whose blocks fit p.row_blocks, tried from the mean on in steps of a 16th, and at
+// least a p.splits-th of the longest context, as a row has no more partials.  TT, TA:
+// tokens per tile of a sequence whose rows, or tokens (p.alone_rows), the waves split.
+template <int M, int TT, int TA>
+__device__ __forceinline__ bool extend_find_share(const ExtendParams& p, int at, ExtendRows& r) {
+    const int lane = threadIdx.x & 63;
+    int first = 0, count = 0, n = 0;
+    if (lane < p.batch) {
+        first = extend_first(p, lane);
+        count = extend_first(p, lane + 1) - first;
+        count = count > 0 ? count : 0;
+        n = extend_context(p, lane);
+    }
+    const int blocks = int((int64_t(count) * p.group + M - 1) / M);
+    const bool alone = count * p.group <= p.alone_rows;
+    int top = blocks > 0 ? n : 0;
+    float tokens = float(n) * float(blocks);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int o = __shfl_xor(top, s);
+        top = top > o ? top : o;
+        tokens += __shfl_xor(tokens, s);
+    }
+    top = __builtin_amdgcn_readfirstlane(top);
+    const float mean = tokens / float(p.row_blocks);
+    int share = top / p.splits + 1;
+    if (mean > float(share)) share = __builtin_amdgcn_readfirstlane(mean < float(top) ? int(mean) : top);
+    int parts, sum;
+    while (true) {
+        const int tiles = n > 0 ? (n - 1) / (alone ? TA : TT) + 1 : 0;
+        const int per = alone ? extend_per_split<TA>(0, 1, share) : extend_per_split<TT>(0, 1, share);
+        parts = tiles > per ? (tiles + per - 1) / per : 1;
+        sum = blocks * parts;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int o = __shfl_up(sum, s);
+            if (lane >= s) sum += o;
+        }
+        if (share >= top || __builtin_amdgcn_readlane(sum, 63) <= p.row_blocks) break;
+        const int step = share / 16 + 1;
+        share = step < top - share ? share + step : top;
+    }
+    r.share = share;
+    const uint64_t past = __builtin_amdgcn_ballot_w64(sum > at);
+    if (past == 0) return false;
+    const int l = __builtin_ctzll(past);
+    r.b = l;
+    r.first = __builtin_amdgcn_readlane(first, l);
+    r.count = __builtin_amdgcn_readlane(count, l);
+    r.n_ctx = __builtin_amdgcn_readlane(n, l);
+    const int of = __builtin_amdgcn_readlane(parts, l), all = __builtin_amdgcn_readlane(blocks, l);
+    const int i = at - (__builtin_amdgcn_readlane(sum, l) - all * of);
+    r.row0 = (all - 1 - i / of) * M;
+    r.split = i % of;
+    return true;
+}
+
 // Positions of a row block's first and last row.
 template <int M>
 __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendRows& r, int& lo, int& hi) {
@@ -268,12 +345,6 @@ __device__ __forceinline__ void gather_columns(v16f (&acc)[CB][NQ], int q, bool 
 // n / group, exact for n < 2^28.
 __device__ __forceinline__ int div_group(const ExtendParams& p, int n) {
     return p.group == 1 ? n : int(__umulhi(unsigned(n), p.group_magic));
-}
-
-// Tiles per split of a row block with `tiles` of them.
-__host__ __device__ __forceinline__ int extend_per_split(int tiles, int splits) {
-    const int per = (tiles + splits - 1) / splits;
-    return per > 4 ? per : 4;
 }
 
 // The wave's 32 NQ query rows from row0 on, as FP8 in operand order at `qs`: a quad
@@ -361,7 +432,7 @@ template <int D, int W, bool ALONE> struct ExtendShape {
 // one tile earlier still), stored to LDS after it, K as it is and V decoded.  Two
 // buffers and one barrier per tile; a wave alone needs one buffer and none.
 template <int D, int NQ, int W, bool ALONE>
-__device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r, int hk, int split, uint8_t* smem) {
+__device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r, int hk, uint8_t* smem) {
     using Shape = ExtendShape<D, W, ALONE>;
     constexpr int TT = Shape::TT, CB = Shape::CB, kVRow = Shape::kVRow, kVOctet = Shape::kVOctet;
     constexpr int M = 32 * NQ * (ALONE ? 1 : W);   // rows of the block
@@ -402,11 +473,11 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     int first_tile = 0, last_tile = r.tiles;
     bool whole = true;
     if (p.splits > 1) {
-        const int per = extend_per_split(r.tiles, p.splits);
+        const int per = extend_per_split<TT>(r.tiles, p.splits, r.share);
         whole = r.tiles <= per;
-        first_tile = split * per;
+        first_tile = r.split * per;
         last_tile = first_tile + per < r.tiles ? first_tile + per : r.tiles;
-        if (first_tile >= last_tile && split != 0) return;
+        if (first_tile >= last_tile && r.split != 0) return;
     }
     const int rows = r.count * p.group;       // of the sequence and KV head
 
@@ -837,7 +908,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
         const int64_t out_row = int64_t(r.first + tok) * p.num_q_heads + hk * p.group + (row - tok * p.group);
         if (!whole) {
             if (row < rows) {
-                const int64_t part = int64_t(split) * p.num_tokens * p.num_q_heads + out_row;
+                const int64_t part = int64_t(r.split) * p.num_tokens * p.num_q_heads + out_row;
 #pragma unroll
                 for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -878,17 +949,24 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     __shared__ __attribute__((aligned(16))) uint8_t smem[kTogetherLds > kAloneLds ? kTogetherLds : kAloneLds];
     const int hk = int(blockIdx.x % unsigned(p.num_kv_heads));
     const int rest = int(blockIdx.x / unsigned(p.num_kv_heads));
+    constexpr int M = 32 * NQ * W;
     ExtendRows r;
-    const bool found = p.longest_first ? extend_find_longest<32 * NQ * W>(p, rest / p.splits, r)
-                                       : extend_find<32 * NQ * W>(p, rest / p.splits, r);
-    if (!found) return;
     if constexpr (MIXED) {
-        if (r.count * p.group <= p.alone_rows) {
-            extend_walk<D, 2, W, true>(p, r, hk, rest % p.splits, smem);
+        if (p.share != nullptr) {
+            const bool found = extend_find_share<M, extend_tile<D>(), ExtendShape<D, W, true>::TT>(p, rest, r);
+            if (blockIdx.x == 0 && threadIdx.x == 0) *p.share = r.share;   // for the join
+            if (!found) return;
+        } else if (!extend_find_split<M>(p, rest, r)) {
             return;
         }
+        if (r.count * p.group <= p.alone_rows) {
+            extend_walk<D, 2, W, true>(p, r, hk, smem);
+            return;
+        }
+    } else if (!extend_find_split<M>(p, rest, r)) {
+        return;
     }
-    extend_walk<D, NQ, W, false>(p, r, hk, rest % p.splits, smem);
+    extend_walk<D, NQ, W, false>(p, r, hk, smem);
 }
 
 // Joins the partials of every (token, query head): 16 lanes per row, N channels
@@ -916,9 +994,16 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     r.row0 = ((t - r.first) * p.group + hq % p.group) / M * M;
     int plo, phi;
     extend_span<M>(p, r, plo, phi);
-    if (r.count * p.group <= p.alone_rows) extend_tiles<ExtendShape<D, 4, true>::TT>(p, plo, phi, r);
-    else extend_tiles<extend_tile<D>()>(p, plo, phi, r);
-    const int per = extend_per_split(r.tiles, p.splits);
+    constexpr int TT = extend_tile<D>(), TA = ExtendShape<D, 4, true>::TT;
+    const int share = p.share != nullptr ? *p.share : 0;
+    int per;
+    if (r.count * p.group <= p.alone_rows) {
+        extend_tiles<TA>(p, plo, phi, r);
+        per = extend_per_split<TA>(r.tiles, p.splits, share);
+    } else {
+        extend_tiles<TT>(p, plo, phi, r);
+        per = extend_per_split<TT>(r.tiles, p.splits, share);
+    }
     if (r.tiles <= per) return;   // written by the first launch
     const int parts = (r.tiles + per - 1) / per;
     const int64_t step = int64_t(p.num_tokens) * p.num_q_heads;
@@ -957,7 +1042,7 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
 
 template <int D, int NQ, int W>
 static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) {
-    const dim3 grid{unsigned(int64_t(p.row_blocks) * p.num_kv_heads * p.splits)}, block{64u * W};
+    const dim3 grid{unsigned(int64_t(p.row_blocks) * p.num_kv_heads * (p.share != nullptr ? 1 : p.splits))}, block{64u * W};
     if (p.alone_rows > 0) {
         if constexpr (D <= 128) launch_kernel(extend_kernel<D, NQ, W, true>, grid, block, stream, p);
         else return hipErrorInvalidValue;   // (not asked for)

@@ -191,10 +191,11 @@ struct ExtendParams {
     int32_t sinks;
     float scale_log2;          // softmax_scale * log2(e)
     int32_t rotate_v;
-    int32_t row_blocks;        // bound of the batch's row blocks per KV head
-    int32_t splits;            // blocks that share a row block's tiles
+    int32_t row_blocks;        // bound of the batch's row blocks per KV head (with share: blocks per KV head)
+    int32_t splits;            // blocks that share a row block's tiles (with share: at most)
     int32_t longest_first;     // row blocks of all sequences in descending order of their last position
     int32_t alone_rows;        // rows of a sequence and KV head up to which the waves split its tokens, or 0
+    int32_t* share;            // NULL, or (for the join) the tokens per split of a batch with equal shares
     float* part_acc;           // [splits][T][Hq][d]
     float* part_ml;            // [splits][T][Hq][2]
     void* out;                 // [T][Hq][d]

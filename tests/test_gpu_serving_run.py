@@ -317,3 +317,33 @@ def test_pools_beyond_32_bits(uq, d):
     for x, y in zip(*results):
         assert torch.equal(x, y)
     assert torch.equal(c0, codes) and torch.equal(s0, scales)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hkv", [1, 3, 8])
+def test_few_queries_over_contexts_of_all_lengths(uq, d, hkv):
+    """Contexts split into shares of one length: one far above the others, empty ones, no rows, more queries
+    than context."""
+    dev = torch.device("cuda:0")
+    lens = [9000, 0, 30, 3, 700, 2500, 1, 4000]
+    news = [3, 1, 0, 5, 8, 2, 1, 4]
+    table, pages = ref.tables(lens, dev, 13)
+    desc = uq.CacheDesc(num_kv_heads=hkv, num_pages=pages, rotate_v=True, head_dim=d)
+    codes, scales = ref.fill_pools(desc, dev, 13)
+    kv = ref.pool_values(desc, codes, scales)
+    for step in range(2):
+        cu = [0]
+        for m in news:
+            cu.append(cu[-1] + m)
+        q = torch.randn((cu[-1] + 2, 4 * hkv, d), generator=torch.Generator(device=dev).manual_seed(d), device=dev)
+        out = torch.full(q.shape, 7.0, device=dev)
+        uq.extend_attention(desc, q, i32(cu, dev), codes, scales, table, i32(lens, dev), 9000, out=out)
+        want = ref.attend(desc, kv, q, cu, table, lens)[:cu[-1]]
+        assert torch.all(out[cu[-1]:] == 7.0)
+        got = out[:cu[-1]]
+        close(got, want, REL, f"d {d} heads {hkv}")
+        norm = want.flatten(1).norm(dim=1)
+        worst = ((got - want).flatten(1).norm(dim=1)[norm > 0] / norm[norm > 0]).max()
+        assert worst <= 20 * REL
+        assert torch.all(got[norm == 0] == 0)
+        news = news[::-1]
