@@ -722,10 +722,11 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  *                   position below 0: more queries than context) gives 0.
  *                   Rows behind cu_seqlens[batch] are left as they were.
  * QK^T is that of uq_decode_attention (FP8 query, FP4 keys); the softmax
- * runs in fp32; its weights enter PV rounded once to FP16 (relative error up
- * to 2^-11 each, while uq_decode_attention carries 16 bits of them).
+ * runs in fp32; its weights enter PV cut to FP16 (relative error up to 2^-10
+ * each, its mean made up for; uq_decode_attention carries 16 bits of them).
  * A long context with few queries is split over blocks and joined by a second
- * launch; the bits of a row depend on num_tokens, batch and max_context then.
+ * launch; the bits of a row depend on num_tokens, batch, max_context and the
+ * other sequences' lengths then.
  * num_tokens == 0 or batch == 0 is a no-op.
  * Errors: as uq_decode_attention, plus INVALID_ARGUMENT for a null
  * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for

@@ -6,7 +6,7 @@
 // n - m + i, and G query heads per KV head, a row is a (query, head of the KV
 // head) pair, row r = query r / G, head r % G: all rows of a (sequence, KV head)
 // read the same keys and values, so a block takes M of them and walks the
-// visible context once in tiles of 64 tokens.
+// visible context once in tiles of 8192 / d tokens.
 //
 //   scores    S^T = K Q^T on v_mfma_scale_f32_32x32x64_f8f6f4: FP4 keys with
 //             their scale bytes as operand A (rows = tokens), the rotated FP8
@@ -20,6 +20,21 @@
 //             token of a k index is free as long as V's operand uses the same
 //             order), so P stays in registers.  V is decoded once per block and
 //             tile into FP16 in LDS, transposed to operand order.
+//
+// M = 256 (4 waves of 64 rows; 128 at d = 256, where the accumulators leave room
+// for 32 rows per wave): a decoded tile serves as many rows as registers hold.  A wave
+// of d = 128 takes all 256 VGPRs, two waves per SIMD.  For sequences of at most 64
+// rows per KV head the four waves take tiles of their own instead, each all the
+// rows, and are joined at the end; long contexts with few rows are split over blocks
+// (extend_shape in uq_api.hip has the rules and both sides' times).
+//
+// What bounds it: the issue of the softmax's and the decode's vector instructions
+// beside the matrix instructions.  8192 new tokens of 64 heads over 4, d = 128: 0.89
+// ms, 1.24 PFLOP/s of the 1.1e12 that causality leaves; the matrix cores are busy
+// 38 % of the time and vector instructions issue 60 % of it.  5 tokens of 64 heads over
+// 8 in 16 sequences of 8k to 24k: 117 us, 2.2 TB/s of codes and scales, the four
+// waves' work on 64 rows of which 40 are used (vector 42 %, matrix 16 %, a third of
+// the time waiting with two waves per SIMD).
 //
 // FP16 holds P with 11 significant bits and a code times 2^E exactly for E in
 // [-23, 13].  So the values of each block of 32 channels are taken relative to an

@@ -143,8 +143,16 @@ __device__ __forceinline__ void norm_rope_quad(float (&x)[NG][8], const NormRope
 // of the table; the others 64 (token, kv head) vectors of k in the same
 // order, or (WRITE) the units of quantize_kv_kernel: 16 tokens of one kv head
 // per wave, whose stores then fill a page's tiles.
+//
+// Bound by memory: 16381 tokens, 64 query heads to FP8 and 8 KV heads to the cache
+// at d = 128, 487 MB, take 116 us (4.2 TB/s; a copy moves 5.0); 8191 tokens of 64 + 8
+// heads at d = 64 rotated to FP16 rows, 151 MB, 30 us; 32 tokens, as a decode step
+// writes them, 5 us, a launch.  More than three waves per SIMD need V in the registers
+// after K is done with them (130 us with both at once; five waves' worth of spills
+// are none); several heads per quad, the weights and angles loaded once for all,
+// gave 126 us.
 template <int DT, int NG, bool WRITE>
-__global__ void __launch_bounds__(256) norm_rope_kernel(NormRopeParams p, QuantizeParams c) {
+__global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRopeParams p, QuantizeParams c) {
     constexpr int D = 32 * NG;
     const int L = threadIdx.x & 3;
     float x[NG][8];
@@ -185,8 +193,6 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(NormRopeParams p, Quanti
         int64_t page;
         int off;
         const bool valid = page_of_slot(c, slot, page, off);
-#pragma unroll
-        for (int j = 0; j < NG; ++j) load_x8<DT>(c.v, row + 32 * j, xv[j]);
         if (!valid) return;
         norm_rope_quad<NG>(x, p, t, p.k_weight, L);
         const int64_t ph = page * c.num_kv_heads + h;
@@ -199,6 +205,8 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(NormRopeParams p, Quanti
             norm_rope_quad<NG>(y, p, t, p.k_weight, L);
         });
         store_k_quad<NG>(kc, ks, off, L, w, b);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) load_x8<DT>(c.v, row + 32 * j, xv[j]);
         quantize_xq<NG>(xv, L, c.c, c.rotate_v != 0, w, b, [&](float (&y)[NG][8]) {
 #pragma unroll
             for (int j = 0; j < NG; ++j) load_x8<DT>(c.v, row + 32 * j, y[j]);
@@ -210,7 +218,9 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(NormRopeParams p, Quanti
 // Stored tokens back to rows: the writer's quad reads the dwords it would
 // write, decodes them by the hardware conversion and rotates the vector back
 // (R is its own inverse).  Units of 16 tokens of one kv head per wave, kv head
-// fastest, as the writer's.
+// fastest, as the writer's.  Bound by memory: 65530 tokens of 8 heads at d = 128 to
+// BF16 rows, 340 MB of which four fifths are written, take 76 to 81 us (4.2 to 4.5
+// TB/s; a copy moves 5.0).
 template <int NG>
 __global__ void __launch_bounds__(256) read_kv_kernel(QuantizeParams c, void* k_out, void* v_out, int dt) {
     constexpr int D = 32 * NG;
