@@ -851,8 +851,8 @@ uq_status uq_probe_mfma(int32_t kind, const void *a, const void *b, const uint8_
  * processor's dispatch and completion latency (a few microseconds).  After
  * uq_time_next_launch(start, stop), the next launch of the decode partition
  * kernel (by uq_decode_attention, uq_decode_partials,
- * uq_decode_step(_partials), the cascade calls or their comparison-cache
- * forms), of the quantize-on-write kernel (uq_quantize_kv) or of a bandwidth
+ * uq_decode_step(_partials), uq_decode_window, the cascade calls or their
+ * comparison-cache forms), of uq_extend_attention's first kernel, of the quantize-on-write kernel (uq_quantize_kv) or of a bandwidth
  * probe (uq_probe_stream_read, uq_probe_page_gather(_cascade)) made from the calling
  * host thread is dispatched with hipExtLaunchKernel, which sets
  * `start` and `stop` (hipEvent_t, created by the caller, not owned by the

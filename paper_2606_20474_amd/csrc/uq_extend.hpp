@@ -29,9 +29,9 @@
 // (extend_shape in uq_api.hip has the rules and both sides' times).
 //
 // What bounds it: the issue of the softmax's and the decode's vector instructions
-// beside the matrix instructions.  8192 new tokens of 64 heads over 4, d = 128: 0.89
-// ms, 1.24 PFLOP/s of the 1.1e12 that causality leaves; the matrix cores are busy
-// 38 % of the time and vector instructions issue 60 % of it.  5 tokens of 64 heads over
+// beside the matrix instructions.  8192 new tokens of 64 heads over 4, d = 128: 0.80
+// to 0.90 ms, 1.2 to 1.4 PFLOP/s of the 1.1e12 that causality leaves; the matrix
+// cores are busy 47 % of the time and vector instructions issue 71 % of it.  5 tokens of 64 heads over
 // 8 in 16 sequences of 8k to 24k: 117 us, 2.2 TB/s of codes and scales, the four
 // waves' work on 64 rows of which 40 are used (vector 42 %, matrix 16 %, a third of
 // the time waiting with two waves per SIMD).
