@@ -652,7 +652,8 @@ typedef struct uq_norm_rope_desc {
  * range.  head_dim: 64, 128 or 256.  num_tokens == 0 is a no-op.
  * Errors: INVALID_ARGUMENT for null or misaligned pointers, negative sizes,
  * num_q_heads < 1, a stride too small or misaligned, a bad eps or max_position;
- * UNSUPPORTED for other head_dim, rot_dim or dtypes, or 2^31 rows or more.
+ * UNSUPPORTED for other head_dim, rot_dim or dtypes, or 2^30 vectors (a token's
+ * head of q or k) or more.
  */
 uq_status uq_norm_rope(const uq_norm_rope_desc *spec, int32_t head_dim, const void *q, int64_t q_stride,
                        int32_t num_q_heads, const void *k, int64_t k_stride, int32_t num_kv_heads,
@@ -688,7 +689,8 @@ uq_status uq_norm_rope_write(const uq_cache_desc *desc, const uq_norm_rope_desc 
  *                   skipped there leaves its rows as they were.
  *   k_out, v_out  : [num_tokens][num_kv_heads][head_dim], contiguous, 16-byte
  *                   aligned; either may be NULL.
- * Errors: as uq_quantize_kv; INVALID_ARGUMENT when both outputs are NULL.
+ * Errors: as uq_quantize_kv; INVALID_ARGUMENT when both outputs are NULL;
+ * UNSUPPORTED for 2^30 (token, head) pairs or more.
  */
 uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const uint8_t *kv_scales,
                      const int32_t *page_table, int32_t num_seqs, int32_t max_pages_per_seq,

@@ -15,6 +15,8 @@ constexpr int kHeadDim = 128;
 constexpr int kPageSize = 16;
 constexpr int kGroupSize = 32;
 constexpr int kMaxGroup = 16;
+constexpr int64_t kMaxBlocks = int64_t(1) << 24;      // of 256 threads: a grid has fewer than 2^32
+constexpr int64_t kMaxVectors = 64 * kMaxBlocks;      // a quad of lanes each
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -520,7 +522,7 @@ static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim
         return UQ_ERR_INVALID_ARGUMENT;
     if (num_tokens > 0 && (!rows_ok(q, q_stride, num_q_heads, head_dim, in_dtype) || q_out == nullptr || !aligned16(q_out)))
         return UQ_ERR_INVALID_ARGUMENT;
-    if (num_tokens >= (int64_t(1) << 31) / num_q_heads) return UQ_ERR_UNSUPPORTED;   // vectors are numbered in 32 bits
+    if (num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
     p.q = q;
     p.k = nullptr;
     p.q_stride = q_stride;
@@ -556,7 +558,7 @@ uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const vo
         return UQ_ERR_INVALID_ARGUMENT;
     if (k != nullptr) {
         if (!rows_ok(k, k_stride, num_kv_heads, head_dim, in_dtype) || !aligned16(k_out)) return UQ_ERR_INVALID_ARGUMENT;
-        if (num_tokens >= (int64_t(1) << 31) / (int64_t(num_q_heads) + num_kv_heads)) return UQ_ERR_UNSUPPORTED;
+        if (num_tokens >= kMaxVectors / (int64_t(num_q_heads) + num_kv_heads) - 256) return UQ_ERR_UNSUPPORTED;
     }
     p.k = k;
     p.k_stride = k_stride;
@@ -582,7 +584,7 @@ uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc*
         return UQ_ERR_INVALID_ARGUMENT;
     s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     if (s != UQ_OK) return s;
-    if (num_tokens >= (int64_t(1) << 31) / (int64_t(num_q_heads) + desc->num_kv_heads) - 16) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens >= kMaxVectors / (int64_t(num_q_heads) + desc->num_kv_heads) - 256) return UQ_ERR_UNSUPPORTED;
     const uq::QuantizeParams c = slot_params(desc, k, v, num_tokens, kv_stride, page_table, num_seqs,
                                              max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     return from_hip(uq::launch_norm_rope(p, &c, desc->head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));
@@ -601,6 +603,7 @@ uq_status uq_read_kv(const uq_cache_desc* desc, const uint8_t* kv_codes, const u
     if (!aligned16(k_out) || !aligned16(v_out)) return UQ_ERR_INVALID_ARGUMENT;
     s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     if (s != UQ_OK) return s;
+    if (num_tokens >= kMaxVectors / desc->num_kv_heads - 256) return UQ_ERR_UNSUPPORTED;
     const uq::QuantizeParams c = slot_params(desc, nullptr, nullptr, num_tokens, 0, page_table, num_seqs,
                                              max_pages_per_seq, slot_mapping, const_cast<uint8_t*>(kv_codes),
                                              const_cast<uint8_t*>(kv_scales));
@@ -751,8 +754,9 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
         e.row_blocks = e.row_blocks > at_once ? e.row_blocks : at_once;
         e.splits *= 4;
     }
-    if (e.row_blocks * desc->num_kv_heads * (e.shared ? 1 : e.splits) > 0x7FFFFFFF) return UQ_ERR_UNSUPPORTED;
-    if (num_tokens * num_q_heads > (int64_t(1) << 34)) return UQ_ERR_UNSUPPORTED;   // blocks of the join
+    // blocks of the grid (256 threads each) and of the join (16 rows each)
+    if (e.row_blocks * desc->num_kv_heads * (e.shared ? 1 : e.splits) >= kMaxBlocks) return UQ_ERR_UNSUPPORTED;
+    if (e.splits > 1 && num_tokens * num_q_heads >= 16 * kMaxBlocks) return UQ_ERR_UNSUPPORTED;
     e.partials = e.splits > 1 ? size_t(e.splits) * size_t(num_tokens) * size_t(num_q_heads) *
                                     size_t(desc->head_dim + 2) * sizeof(float)
                               : 0;

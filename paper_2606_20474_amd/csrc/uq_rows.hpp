@@ -280,7 +280,6 @@ hipError_t launch_norm_rope(NormRopeParams p, const QuantizeParams* c, int head_
     const int64_t qb = (p.num_tokens * p.num_q_heads + 63) / 64;
     const int64_t kb = c != nullptr ? (kv_units(*c) + 3) / 4 : (p.num_tokens * p.num_kv_heads + 63) / 64;
     if (qb + kb == 0) return hipSuccess;
-    if (qb + kb > (int64_t(1) << 25)) return hipErrorInvalidValue;   // 2^31 vectors; the entry points refuse them
     p.q_blocks = unsigned(qb);
     const unsigned blocks = unsigned(qb + kb);
     const QuantizeParams none{};
@@ -299,7 +298,6 @@ hipError_t launch_norm_rope(NormRopeParams p, const QuantizeParams* c, int head_
 hipError_t launch_read_kv(const QuantizeParams& c, void* k_out, void* v_out, int dtype, hipStream_t stream) {
     const int64_t units = kv_units(c);
     if (units == 0) return hipSuccess;
-    if (units > 0x7FFFFFFF) return hipErrorInvalidValue;   // the kernel numbers them in 32 bits
     const dim3 grid{unsigned((units + 3) / 4)}, block{256u};
     if (c.head_dim == 64) hipLaunchKernelGGL(read_kv_kernel<2>, grid, block, 0, stream, c, k_out, v_out, dtype);
     else if (c.head_dim == 128) hipLaunchKernelGGL(read_kv_kernel<4>, grid, block, 0, stream, c, k_out, v_out, dtype);

@@ -153,3 +153,14 @@ def test_host_tensors_and_wrong_shapes_are_rejected():
     for call in calls:
         with pytest.raises(ValueError, match="on the GPU"):
             call()
+
+
+def test_more_blocks_than_a_grid_holds():
+    """A grid has fewer than 2^32 threads; larger calls are refused before the launch."""
+    one = spec(rot_dim=0)
+    assert rope(s=one, d=64, qs=64, hq=1, k=None, ko=None, hkv=0, T=1 << 30) == UNSUPPORTED
+    assert rope(s=one, d=64, qs=64, hq=1, ks=64, hkv=1, T=1 << 29) == UNSUPPORTED
+    assert write(T=1 << 28) == UNSUPPORTED
+    D = desc(head_dim=64, num_kv_heads=1)
+    assert read(D=D, T=1 << 30) == UNSUPPORTED
+    assert extend(D=desc(num_kv_heads=1024, head_dim=64), hq=1024, qs=65536, T=1 << 23, B=65535) == UNSUPPORTED
