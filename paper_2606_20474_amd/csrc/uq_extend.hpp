@@ -674,11 +674,15 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     }
     bool big_max = false;   // wave-uniform: a running maximum of magnitude 2^20 or more (see decode_kernel)
 
-    // The wave's rows against the tile in `slot`; `clear`: every row sees all of it.
+    // The wave's rows against the tile in `slot`; `clear`: every row sees all 32 tokens.
     // Masks, rescaling and large maxima are one branch, so that the rest is one
     // block of instructions, in which the exponentials of the second 16 tokens run
     // beside the products of the first.
-    auto compute = [&](int tok0, int slot, bool clear) {
+    constexpr bool kPick = TT > 64;
+    auto clear_of = [&](int from, int n) {
+        return from + n - 1 <= w_lo && (p.window == 0 || from > w_hi - p.window || from + n <= p.sinks);
+    };
+    auto compute = [&](int tok0, int slot) {
         const unsigned l = fresh_lane(), lh = l >> 5, lc = l & 31;
         const uint8_t* v_at = vt(slot) + lh * kVRow + 16 * lc + (kVOctet - 128) * (lc >> 3);
         const uint8_t* k_at = kt(slot) + (lc >> 4) * (8 * D) + (lh * 16 + (lc & 15)) * 16;
@@ -702,9 +706,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                     s[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qop[q][k], s[q], 4, 0, 0, ksc[k], 0, 127);
             }
         };
-        scores(0);
-#pragma unroll
-        for (int tb = 0; tb < TT / 32; ++tb) {
+        auto tokens = [&](int tb, bool clear) {
             auto load_v = [&](int mm, uint4 (&v)[CB]) {
 #pragma unroll
                 for (int c = 0; c < CB; ++c) v[c] = *reinterpret_cast<const uint4*>(v_at + ((2 * tb + mm) * CB + c) * 2 * kVRow);
@@ -797,6 +799,22 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
             values(va, p0);
             weights(1, p1);
             values(vb, p1);
+        };
+        const bool clear = clear_of(tok0, TT);
+        // of a tile that is not clear only the 32s that a row of the wave sees
+        int tb_from = 0, tb_end = TT / 32;
+        if (kPick && !clear) {
+            tb_end = (w_hi - tok0) / 32 + 1;
+            if (p.window > 0) {
+                const int from = w_lo - p.window + 1 - tok0;   // first token of the windows, in the tile
+                if (tok0 >= p.sinks) tb_from = from > 0 ? from / 32 : 0;
+                else if (from >= TT) tb_end = (p.sinks - tok0 + 31) / 32 < tb_end ? (p.sinks - tok0 + 31) / 32 : tb_end;
+            }
+        }
+        scores(0);
+#pragma unroll
+        for (int tb = 0; tb < TT / 32; ++tb) {
+            if (!kPick || (tb >= tb_from && tb < tb_end)) tokens(tb, kPick ? clear || clear_of(tok0 + 32 * tb, 32) : clear);
             if (tb + 1 < TT / 32) scores(tb + 1);
         }
     };
@@ -855,7 +873,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
         const int tok0 = token_of(t);
         // tiles past the wave's last row, or before its windows and after the sinks
         if (!busy || tok0 > w_hi || (p.window > 0 && tok0 + TT <= w_lo - p.window + 1 && tok0 >= p.sinks)) continue;
-        compute(tok0, slot, tok0 + TT - 1 <= w_lo && (p.window == 0 || tok0 > w_hi - p.window || tok0 + TT <= p.sinks));
+        compute(tok0, slot);
     }
 
     // ---- the row's sum over both halves, the accumulators divided by it and back to
