@@ -13,8 +13,8 @@
 //             queries as operand B (columns = rows of the block).  A lane then
 //             holds 16 tokens of one row, so the softmax needs no exchange
 //             between lanes but one (lanes l and l ^ 32 share a row).
-//   softmax   in the log2 domain, running maximum with a lazy rescale, sums per
-//             lane until the end.
+//   softmax   in the log2 domain, relative to a running reference with a lazy
+//             rescale, sums per lane until the end.
 //   values    O^T += V^T P^T on v_mfma_f32_32x32x16_f16.  The scores leave the
 //             QK instruction in the order in which P enters as operand B (the
 //             token of a k index is free as long as V's operand uses the same
@@ -36,12 +36,18 @@
 // waves' work on 64 rows of which 40 are used (vector 42 %, matrix 16 %, a third of
 // the time waiting with two waves per SIMD).
 //
-// FP16 holds P with 11 significant bits and a code times 2^E exactly for E in
-// [-23, 13].  So the values of each block of 32 channels are taken relative to an
-// exponent of their own, v 2^-e, and the accumulators hold O 2^-e: e is 8 below the
-// largest scale exponent when it is set (in the first tile), and set again, the
-// accumulators rescaled, when a tile's largest passes e + 13.  Values more than
-// 2^31 below the largest of their 32 channels that the block has seen are lost.
+// FP16 holds P with 11 significant bits from 2^-14 on, its range ending at 2^16, and the
+// sum counts weights that FP16 would lose.  So a row's weights are relative to a
+// reference that follows the scores both ways: it is set 7 below the largest score of
+// 32 tokens (whose weight is 2^7 then) when that score leaves [-5, 15] above it.  A
+// row's sum and accumulators are fp32 and hold what lies behind, up to 2^80 of it.
+//
+// A code times 2^E is exact in FP16 for E in [-23, 13].  So the values of each block of
+// 32 channels are taken relative to an exponent of their own, v 2^-e, and the
+// accumulators hold O 2^-e: e is 8 below the largest scale exponent when it is set (in
+// the first tile), and set again, the accumulators rescaled, when a tile's largest
+// passes e + 13.  Values more than 2^31 below the largest of their 32 channels that the
+// block has seen are lost.
 #pragma once
 
 #include "uq_device.hpp"
@@ -60,6 +66,13 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 // is 1 again.)
 constexpr float kLift = 5.08057e-4f;
 constexpr float kLower = 0.99964790f;
+
+// The reference of a row's weights, in powers of two: set kLead below the largest score
+// of 32 tokens, and again when that of others is not within kDown .. kUp above it.  Down
+// only while the row's sum is below 2^kDepth, by at most kDepth, so that the
+// accumulators (at most 2^16 times the sum) stay finite.
+constexpr float kLead = 7.0f, kUp = kLead + kLazyRescale, kDown = kLead - 12.0f;
+constexpr float kDepth = 40.0f, kDeep = 0x1p40f;
 
 constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
 
@@ -409,7 +422,7 @@ __device__ __forceinline__ void stage_queries(const ExtendParams& p, const Exten
     }
 }
 
-// Two parts of a row, running maxima m and sums l: the first becomes both, and the
+// Two parts of a row, references m and sums l: the first becomes both, and the
 // share of the second in it is returned.
 __device__ __forceinline__ float join_share(float& m, float& l, float m2, float l2) {
     const float top = __builtin_fmaxf(m, m2);
@@ -672,7 +685,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
 #pragma unroll
         for (int c = 0; c < CB; ++c) acc[c][q] = v16f(0.f);
     }
-    bool big_max = false;   // wave-uniform: a running maximum of magnitude 2^20 or more (see decode_kernel)
+    bool big_max = false;   // wave-uniform: a reference of magnitude 2^20 or more (see decode_kernel)
 
     // Tiles of 128 tokens (head size 64): of one that is partly hidden only the 32s with a
     // visible token are computed, and only those with a hidden one masked (window 1024:
@@ -721,12 +734,13 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                 for (int i = 3; i < 15; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[q][i]), s[q][i + 1]);
                 return __builtin_fmaxf(mx, s[q][15]);
             };
-            bool grows = !clear || big_max;
+            bool moves = !clear || big_max;
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
-                grows = __builtin_amdgcn_ballot_w64(max_of(q) * sl2 > m_run[q] + kLazyRescale) != 0 || grows;
+                moves = __builtin_amdgcn_ballot_w64(__builtin_fabsf(__builtin_fmaf(max_of(q), sl2, -0.5f * (kUp + kDown) - m_run[q])) >
+                                                    0.5f * (kUp - kDown)) != 0 || moves;
             float scale = sl2, shift[NQ];
-            if (__builtin_expect(grows, 0)) {
+            if (__builtin_expect(moves, 0)) {
                 big_max = false;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
@@ -747,12 +761,17 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                     float a = max_of(q), b = a;
                     swap32(a, b);
                     const float mloc = __builtin_fmaxf(a, b) * sl2;
-                    if (mloc > m_run[q] + kLazyRescale) {
-                        const float alpha = __builtin_amdgcn_exp2f(m_run[q] - mloc);
+                    // (both lanes of a row decide alike; down, unless the row sees none of the 32)
+                    float la = l_run[q], lb = l_run[q];
+                    swap32(la, lb);
+                    const bool down = mloc < m_run[q] + kDown && mloc > -__builtin_inff() && la + lb < kDeep;
+                    if (mloc > m_run[q] + kUp || down) {
+                        const float to = down ? __builtin_fmaxf(mloc - kLead, m_run[q] - kDepth) : mloc - kLead;
+                        const float alpha = __builtin_amdgcn_exp2f(m_run[q] - to);
                         l_run[q] *= alpha;
 #pragma unroll
                         for (int c = 0; c < CB; ++c) acc[c][q] *= alpha;
-                        m_run[q] = mloc;
+                        m_run[q] = to;
                     }
                     big_max = big_max || __builtin_amdgcn_ballot_w64(__builtin_fabsf(m_run[q]) >= 0x1p20f && m_run[q] != kNoMax) != 0;
                 }
@@ -760,7 +779,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
 #pragma unroll
             for (int q = 0; q < NQ; ++q) shift[q] = kLift - m_run[q];
             if (__builtin_expect(big_max, 0)) {
-                // the difference to the rounded product, as m_run was
+                // the difference to the rounded product, as m_run is one less kLead
 #pragma clang fp contract(off)
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
