@@ -813,8 +813,11 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     p.num_pages = desc->num_pages;
     p.context_lens = context_lens;
     p.max_context = max_context;
-    p.window = window;
-    p.sinks = window > 0 ? sinks : 0;
+    // (no more than the context: the same tokens are visible, and first - window, where first
+    // may be below 0, stays in 32 bits)
+    const int32_t reach = max_context > 1 ? max_context : 1;
+    p.window = window < reach ? window : reach;
+    p.sinks = window == 0 ? 0 : sinks < reach ? sinks : reach;
     p.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
     p.rotate_v = desc->rotate_v != 0;
     p.row_blocks = int32_t(e.row_blocks);
