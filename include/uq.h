@@ -736,7 +736,7 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  * num_tokens == 0 or batch == 0 is a no-op.
  * Errors: as uq_decode_attention, plus INVALID_ARGUMENT for a null
  * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for
- * num_tokens >= 2^24 or more blocks than a grid holds.
+ * num_tokens >= 2^24, max_context > 2^30 or more blocks than a grid holds.
  */
 size_t uq_extend_workspace_bytes(const uq_cache_desc *desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
                                  int32_t max_context, int32_t window, int32_t sinks);

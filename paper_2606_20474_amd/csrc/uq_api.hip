@@ -724,6 +724,7 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
     const int32_t group = num_q_heads / desc->num_kv_heads;
     if (group > kMaxGroup || batch > 65535 || desc->num_kv_heads > 65535) return UQ_ERR_UNSUPPORTED;
     if (num_tokens >= (int64_t(1) << 24)) return UQ_ERR_UNSUPPORTED;   // rows of a KV head are numbered in 28 bits
+    if (max_context > (1 << 30)) return UQ_ERR_UNSUPPORTED;   // tiles and pages ahead of the walk, and positions, stay in 32 bits
     const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
     // the waves split the tokens of the sequences with few rows where such sequences
