@@ -609,9 +609,11 @@ uq_status uq_decode_attention_noalloc(const uq_cache_desc *desc, const void *q, 
  * free ones run out: the pages it and the sequences before it need (those
  * refused for the first two reasons apart) exceed num_free_pages.  The caller
  * drops the first result[1] entries of free_pages.
- * No output may overlap an input other than page_table.  batch == 0 is valid.
- * Errors: INVALID_ARGUMENT for null pointers, negative batch, num_free_pages or
- * num_tokens, max_pages_per_seq < 1; UNSUPPORTED for batch > 4096, num_tokens
+ * No output may overlap an input or another output: cached_lens is an array of its
+ * own, not the context_lens of this call (the last step's may be, where the two
+ * alternate).  batch == 0 is valid.
+ * Errors: INVALID_ARGUMENT for null pointers, such overlaps, negative batch,
+ * num_free_pages or num_tokens, max_pages_per_seq < 1; UNSUPPORTED for batch > 4096, num_tokens
  * or num_free_pages >= 2^29, or max_pages_per_seq >= 2^27.
  */
 uq_status uq_plan_tokens(int32_t batch, const int32_t *cached_lens, const int32_t *new_lens,

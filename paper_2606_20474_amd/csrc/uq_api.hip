@@ -487,6 +487,12 @@ uq_status uq_quantize_kv(const uq_cache_desc* desc, const void* k, const void* v
     return from_hip(uq::launch_quantize_kv(p, int(in_dtype), static_cast<hipStream_t>(stream)));
 }
 
+// Two blocks of device memory share a byte.
+static bool overlaps(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes > 0 && b_bytes > 0 && x < y + b_bytes && y < x + a_bytes;
+}
+
 uq_status uq_plan_tokens(int32_t batch, const int32_t* cached_lens, const int32_t* new_lens,
                          const int32_t* free_pages, int32_t num_free_pages, int32_t* page_table,
                          int32_t max_pages_per_seq, int64_t num_tokens, int32_t* context_lens, int32_t* cu_seqlens,
@@ -500,6 +506,19 @@ uq_status uq_plan_tokens(int32_t batch, const int32_t* cached_lens, const int32_
     if (cu_seqlens == nullptr || result == nullptr || (num_free_pages > 0 && free_pages == nullptr))
         return UQ_ERR_INVALID_ARGUMENT;
     if (num_tokens > 0 && (seq_ids == nullptr || positions == nullptr || slots == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
+    // every block reads the lengths and the free list, and writes a share of the outputs
+    const size_t word = sizeof(int32_t), rows = size_t(num_tokens);
+    const struct { const void* at; size_t bytes; } ins[] = {{cached_lens, batch * word}, {new_lens, batch * word},
+                                                            {free_pages, num_free_pages * word}},
+        outs[] = {{page_table, size_t(batch) * max_pages_per_seq * word}, {context_lens, batch * word},
+                  {cu_seqlens, (batch + 1) * word}, {seq_ids, rows * word}, {positions, rows * word},
+                  {slots, rows * sizeof(int64_t)}, {result, 3 * word}};
+    for (const auto& o : outs) {
+        for (const auto& i : ins)
+            if (overlaps(o.at, o.bytes, i.at, i.bytes)) return UQ_ERR_INVALID_ARGUMENT;
+        for (const auto& other : outs)
+            if (&other != &o && overlaps(o.at, o.bytes, other.at, other.bytes)) return UQ_ERR_INVALID_ARGUMENT;
+    }
     const uq::PlanParams p{batch,        cached_lens,  new_lens,   free_pages, num_free_pages, page_table, max_pages_per_seq,
                            num_tokens,   context_lens, cu_seqlens, seq_ids,    positions,      slots,      result};
     return from_hip(uq::launch_plan_tokens(p, static_cast<hipStream_t>(stream)));

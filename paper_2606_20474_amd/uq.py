@@ -592,7 +592,9 @@ class TokenPlan:
 def plan_tokens(cached_lens, new_lens, free_pages, page_table, plan: TokenPlan, stream=None):
     """Pages, slots and positions of one step from its lengths: fills `plan`
     and the new entries of `page_table` (int32 [batch, max_pages_per_seq]),
-    taking pages from the front of `free_pages` (int32)."""
+    taking pages from the front of `free_pages` (int32).  `plan.context_lens`
+    of this call is no input of it: an engine that feeds the last step's
+    lengths keeps two plans or copies them (such a call is refused)."""
     _need(cached_lens, "cached_lens", _I32, (None,))
     B = cached_lens.shape[0]
     _need(new_lens, "new_lens", _I32, (B,))

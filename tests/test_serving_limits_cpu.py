@@ -35,3 +35,27 @@ def test_longest_context(window):
     assert extend(1 << 30) == INVALID
     if window == 0:
         assert uq.lib.uq_extend_workspace_bytes(ctypes.byref(D), 2, 2, 4, 1 << 30, 0, 0) > 0
+
+
+def plan(**kw):
+    """Two sequences over rows of 4 pages, 4 free pages, 8 token rows; every array has its own memory unless named."""
+    a = {n: 0x10000 * (i + 1) for i, n in enumerate(("cached", "new", "free", "table", "context", "cu", "seq", "pos",
+                                                     "slots", "result"))}
+    a.update(kw)
+    p = {n: at(x) for n, x in a.items()}
+    return uq.lib.uq_plan_tokens(2, p["cached"], p["new"], p["free"], 4, p["table"], 4, 8, p["context"], p["cu"], p["seq"],
+                                 p["pos"], p["slots"], p["result"], None)
+
+
+SIZES = dict(cached=8, new=8, free=16, table=32, context=8, cu=12, seq=32, pos=32, slots=64, result=12)
+
+
+@pytest.mark.parametrize("out", ["table", "context", "cu", "seq", "pos", "slots", "result"])
+@pytest.mark.parametrize("other", list(SIZES))
+def test_plan_outputs_stand_alone(out, other):
+    """An output is written by one block while others still read the inputs."""
+    if out == other:
+        return
+    for first, second in ((out, other), (other, out)):      # the same start, and the last bytes of either
+        assert plan(**{first: 0x200000, second: 0x200000}) == INVALID
+        assert plan(**{first: 0x200000, second: 0x200000 + SIZES[first] - 4}) == INVALID
