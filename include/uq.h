@@ -653,7 +653,8 @@ typedef struct uq_norm_rope_desc {
  * needs eps > 0 (else it is 0 * inf); squares and their sum stay in fp32
  * range.  head_dim: 64, 128 or 256.  num_tokens == 0 is a no-op.
  * Errors: INVALID_ARGUMENT for null or misaligned pointers, negative sizes,
- * num_q_heads < 1, a stride too small or misaligned, a bad eps or max_position;
+ * num_q_heads < 1, a stride too small or misaligned, overlaps of the rows other
+ * than those two, a bad eps or max_position;
  * UNSUPPORTED for other head_dim, rot_dim or dtypes, or 2^30 vectors (a token's
  * head of q or k) or more.
  */
@@ -671,7 +672,8 @@ uq_status uq_norm_rope(const uq_norm_rope_desc *spec, int32_t head_dim, const vo
  *   q             : as above, q_stride; k, v as above with kv_stride, all of
  *                   in_dtype.
  *   q_out         : [num_tokens][num_q_heads][head_dim] F32, BF16, F16 or
- *                   FP8_E4M3 (bytes), 16-byte aligned.  Padding tokens get
+ *                   FP8_E4M3 (bytes), 16-byte aligned; it may be q as above,
+ *                   and overlaps q, k and v no other way.  Padding tokens get
  *                   their queries too.
  *   page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes,
  *   kv_scales     : as in uq_quantize_kv.

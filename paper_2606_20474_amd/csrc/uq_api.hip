@@ -524,6 +524,29 @@ uq_status uq_plan_tokens(int32_t batch, const int32_t* cached_lens, const int32_
     return from_hip(uq::launch_plan_tokens(p, static_cast<hipStream_t>(stream)));
 }
 
+// Token rows of `heads` vectors, token t at element t * stride.
+struct TokenRows {
+    const void* at;
+    int64_t count, stride;
+    int64_t width;      // heads * head_dim
+    uq_dtype dtype;
+    size_t item() const { return dtype == UQ_F32 ? 4 : dtype == UQ_FP8_E4M3 ? 1 : 2; }
+};
+// Contiguous rows `out` share a byte with the rows `x`.
+static bool meets(const TokenRows& out, const TokenRows& x) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), r = reinterpret_cast<uintptr_t>(x.at);
+    const size_t bytes = size_t(out.count * out.width) * out.item();
+    const size_t row = size_t(x.width) * x.item(), stride = size_t(x.stride) * x.item();
+    const uintptr_t first = a < r + row ? 0 : (a - r - row) / stride + 1;   // the first row that ends behind out's start
+    return bytes > 0 && first < uintptr_t(x.count) && r + first * stride < a + bytes;
+}
+// The same against the rows `out` is made of: they may be written in place, as the lanes
+// that write a vector have read it, where the two are laid out alike.
+static bool meets_own(const TokenRows& out, const TokenRows& x) {
+    const bool in_place = out.at == x.at && out.dtype == x.dtype && (x.count == 1 || x.stride == x.width);
+    return !in_place && meets(out, x);
+}
+
 // The norm and rotation part of the parameter block; every argument check of
 // the spec, q and the output types.
 static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
@@ -579,6 +602,15 @@ uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const vo
         if (!rows_ok(k, k_stride, num_kv_heads, head_dim, in_dtype) || !aligned16(k_out)) return UQ_ERR_INVALID_ARGUMENT;
         if (num_tokens >= kMaxVectors / (int64_t(num_q_heads) + num_kv_heads) - 256) return UQ_ERR_UNSUPPORTED;
     }
+    const int64_t d = head_dim;
+    const TokenRows qi{q, num_tokens, q_stride, num_q_heads * d, in_dtype}, qo{q_out, num_tokens, 0, num_q_heads * d, out_dtype};
+    if (meets_own(qo, qi)) return UQ_ERR_INVALID_ARGUMENT;
+    if (k != nullptr) {
+        const TokenRows ki{k, num_tokens, k_stride, num_kv_heads * d, in_dtype}, ko{k_out, num_tokens, 0, num_kv_heads * d, out_dtype};
+        if (meets_own(ko, ki) || meets(ko, qi) || meets(qo, ki) ||
+            overlaps(q_out, size_t(num_tokens * qo.width) * qo.item(), k_out, size_t(num_tokens * ko.width) * ko.item()))
+            return UQ_ERR_INVALID_ARGUMENT;
+    }
     p.k = k;
     p.k_stride = k_stride;
     p.num_kv_heads = num_kv_heads;
@@ -604,6 +636,11 @@ uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc*
     s = check_slots(page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     if (s != UQ_OK) return s;
     if (num_tokens >= kMaxVectors / (int64_t(num_q_heads) + desc->num_kv_heads) - 256) return UQ_ERR_UNSUPPORTED;
+    const int64_t d = desc->head_dim, width = desc->num_kv_heads * d;
+    const TokenRows qo{q_out, num_tokens, 0, num_q_heads * d, q_out_dtype};
+    if (meets_own(qo, {q, num_tokens, q_stride, num_q_heads * d, in_dtype}) ||
+        meets(qo, {k, num_tokens, kv_stride, width, in_dtype}) || meets(qo, {v, num_tokens, kv_stride, width, in_dtype}))
+        return UQ_ERR_INVALID_ARGUMENT;
     const uq::QuantizeParams c = slot_params(desc, k, v, num_tokens, kv_stride, page_table, num_seqs,
                                              max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     return from_hip(uq::launch_norm_rope(p, &c, desc->head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));

@@ -59,3 +59,40 @@ def test_plan_outputs_stand_alone(out, other):
     for first, second in ((out, other), (other, out)):      # the same start, and the last bytes of either
         assert plan(**{first: 0x200000, second: 0x200000}) == INVALID
         assert plan(**{first: 0x200000, second: 0x200000 + SIZES[first] - 4}) == INVALID
+
+
+def spec():
+    return uq.uq_norm_rope_desc(None, None, 1e-6, None, None, 0, 0, 0)
+
+
+# one token row: 4 query heads and 2 KV heads of 128, BF16; 6 tokens
+T, Q, KV = 6, 4 * 128 * 2, 2 * 128 * 2
+BF16, F16, F32, FP8 = uq.UQ_BF16, uq.UQ_F16, uq.UQ_F32, uq.UQ_FP8_E4M3
+
+
+def rope(q, k, qo, ko, qs=512, ks=256, odt=BF16, dt=BF16, tokens=T):
+    s = spec()
+    return uq.lib.uq_norm_rope(ctypes.byref(s), 128, at(q), qs, 4, at(k), ks, 2, dt, tokens, at(qo), at(ko), odt, None)
+
+
+def write(q, k, v, qo, qs=512, ks=256, odt=FP8):
+    s, D, P = spec(), desc(), at(0x900000)
+    return uq.lib.uq_norm_rope_write(ctypes.byref(D), ctypes.byref(s), at(q), qs, 4, at(k), at(v), ks, BF16, T, at(qo), odt,
+                                     None, 0, 0, P, P, P, None)
+
+
+def test_row_outputs_stand_alone():
+    """A vector's lanes write its place after they have read it; another vector's input there may not be read yet."""
+    A, B, C, E = 0x100000, 0x200000, 0x300000, 0x400000
+    for kw in (dict(q=A, k=B, qo=A, ko=C, odt=F32), dict(q=A, k=B, qo=A, ko=C, odt=F16),      # another type
+               dict(q=A, k=B, qo=A, ko=C, qs=1024), dict(q=A, k=B, qo=A + 64, ko=C),          # other places of q
+               dict(q=A, k=B, qo=A + T * Q - 16, ko=C), dict(q=A, k=B, qo=A - T * Q + 16, ko=C),
+               dict(q=A, k=B, qo=C, ko=B, odt=F32), dict(q=A, k=B, qo=C, ko=B, ks=512),
+               dict(q=A, k=B, qo=B, ko=C), dict(q=A, k=B, qo=C, ko=A), dict(q=A, k=B, qo=C, ko=C),
+               dict(q=A, k=B, qo=C, ko=C + T * Q - 16), dict(q=A, k=B, qo=C + T * KV - 16, ko=C),
+               # rows of one buffer: the output in the middle of it
+               dict(q=A, k=A + Q, qo=A + 3 * (Q + 2 * KV), ko=C, qs=1024, ks=1024)):
+        assert rope(**kw) == INVALID, kw
+    for kw in (dict(qo=A), dict(qo=A, odt=F16), dict(qo=A, odt=BF16, qs=1024), dict(qo=A + 16), dict(qo=B), dict(qo=C),
+               dict(qo=C + T * KV - 16), dict(qo=A + T * Q - 16)):
+        assert write(**{**dict(q=A, k=B, v=C), **kw}) == INVALID, kw
