@@ -8,6 +8,7 @@ missing, importing this module fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -320,6 +321,16 @@ def _stream(stream=None):
     return _raw_stream(_current_device()) if stream is None else stream.cuda_stream
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on(stream):
+    """Where a call makes its tensors: on the stream its kernels run on, so
+    that zeroes are written before them and the memory of a workspace goes to
+    no other stream's tensors while they run."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
 _DT = {torch.float32: UQ_F32, torch.bfloat16: UQ_BF16, torch.float16: UQ_F16, torch.uint8: UQ_FP8_E4M3,
        torch.float8_e4m3fn: UQ_FP8_E4M3}
 
@@ -380,7 +391,8 @@ def prepare_query(desc: CacheDesc, q, out=None, stream=None):
         raise ValueError(f"q: rows of {HEAD_DIM} channels expected")
     rows = q.numel() // HEAD_DIM
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.uint8, device=q.device)
+        with _on(stream):
+            out = torch.empty(q.shape, dtype=torch.uint8, device=q.device)
     _need(out, "out", (torch.uint8, torch.float8_e4m3fn), min_numel=q.numel())
     d = desc.c_struct()
     _check(lib.uq_prepare_query(ctypes.byref(d), _ptr(q), _DT[q.dtype], rows, _ptr(out), _stream(stream)),
@@ -408,12 +420,15 @@ def quantize_error(x, c_values, rotate=True, pow2=True, sums=None, stream=None):
     ``sums`` float64 [n, 2] (sum of squared errors, sum of squares),
     accumulated into ``sums`` if given, else into a new zeroed tensor."""
     _need(x, "x", _ROWS, contiguous=False)
-    rows = x.reshape(-1, HEAD_DIM) if x.dim() != 2 else x
+    with _on(stream):
+        rows = x.reshape(-1, HEAD_DIM) if x.dim() != 2 else x
     if rows.shape[-1] != HEAD_DIM or rows.stride(-1) != 1:
         raise ValueError("rows of 128 contiguous channels expected")
-    c = c_values.to(device=x.device, dtype=torch.float32).contiguous()
+    with _on(stream):
+        c = c_values.to(device=x.device, dtype=torch.float32).contiguous()
     if sums is None:
-        sums = torch.zeros((c.numel(), 2), dtype=torch.float64, device=x.device)
+        with _on(stream):
+            sums = torch.zeros((c.numel(), 2), dtype=torch.float64, device=x.device)
     _need(sums, "sums", (torch.float64,), (c.numel(), 2))
     st = lib.uq_quantize_error(_ptr(rows), _DT[x.dtype], rows.shape[0], rows.stride(0), int(bool(rotate)),
                                int(bool(pow2)), c.numel(), _ptr(c), _ptr(sums), _stream(stream))
@@ -446,10 +461,12 @@ def decode_attention(desc: CacheDesc, q, codes, scales, page_table, context_lens
     if softmax_scale is None:
         softmax_scale = desc.head_dim ** -0.5
     if workspace is None:
-        workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
+        with _on(stream):
+            workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     qdt = _DT[q.dtype] if q_dtype is None else q_dtype
     st = lib.uq_decode_attention(ctypes.byref(d), _ptr(q), qdt, B, Hq, _ptr(codes), _ptr(scales), _ptr(page_table),
@@ -471,10 +488,12 @@ def decode_attention_scaled_pv(desc: CacheDesc, q, codes, scales, page_table, co
     if softmax_scale is None:
         softmax_scale = desc.head_dim ** -0.5
     if workspace is None:
-        workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
+        with _on(stream):
+            workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     qdt = _DT[q.dtype] if q_dtype is None else q_dtype
     st = lib.uq_decode_attention_scaled_pv(ctypes.byref(d), _ptr(q), qdt, B, Hq, _ptr(codes), _ptr(scales),
@@ -538,10 +557,12 @@ def decode_step(desc: CacheDesc, q, k_new, v_new, codes, scales, page_table, con
     if softmax_scale is None:
         softmax_scale = desc.head_dim ** -0.5
     if workspace is None:
-        workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
+        with _on(stream):
+            workspace = alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     qdt = _DT[q.dtype] if q_dtype is None else q_dtype
     fn = lib.uq_decode_step_partials if partials_only else lib.uq_decode_step
@@ -659,14 +680,16 @@ def norm_rope(spec: NormRope, q, k=None, q_out=None, k_out=None, out_dtype=None,
     T, Hq, d = q.shape
     out_dtype = out_dtype or (q.dtype if q_out is None else q_out.dtype)
     if q_out is None:
-        q_out = torch.empty((T, Hq, d), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            q_out = torch.empty((T, Hq, d), dtype=out_dtype, device=q.device)
     _need(q_out, "q_out", _ROWS, (T, Hq, d))
     k_stride, Hkv = 0, 0
     if k is not None:
         k_stride = _head_rows(k, "k", (q.dtype,), (T, None, d))
         Hkv = k.shape[1]
         if k_out is None:
-            k_out = torch.empty((T, Hkv, d), dtype=q_out.dtype, device=q.device)
+            with _on(stream):
+                k_out = torch.empty((T, Hkv, d), dtype=q_out.dtype, device=q.device)
         _need(k_out, "k_out", (q_out.dtype,), (T, Hkv, d))
     elif k_out is not None:
         raise ValueError("k_out: given without k")
@@ -692,7 +715,8 @@ def norm_rope_write(desc: CacheDesc, spec: NormRope, q, k, v, slot_mapping, code
     _need(slot_mapping, "slot_mapping", (torch.int64,), (T,))
     _pools(desc, codes, scales)
     if q_out is None:
-        q_out = torch.empty((T, Hq, d), dtype=q_out_dtype, device=q.device)
+        with _on(stream):
+            q_out = torch.empty((T, Hq, d), dtype=q_out_dtype, device=q.device)
     _need(q_out, "q_out", _QUERY, (T, Hq, d))
     s, c = spec.c_struct(T, d), desc.c_struct()
     st = lib.uq_norm_rope_write(ctypes.byref(c), ctypes.byref(s), _ptr(q), q_stride, Hq, _ptr(k), _ptr(v), kv_stride,
@@ -711,7 +735,8 @@ def read_kv(desc: CacheDesc, slot_mapping, codes, scales, page_table=None, max_p
     shape = (slot_mapping.shape[0], desc.num_kv_heads, desc.head_dim)
     _pools(desc, codes, scales)
     if k_out is None and v_out is None:
-        k_out, v_out = (torch.zeros(shape, dtype=out_dtype, device=codes.device) for _ in range(2))
+        with _on(stream):
+            k_out, v_out = (torch.zeros(shape, dtype=out_dtype, device=codes.device) for _ in range(2))
     for t, name in ((k_out, "k_out"), (v_out, "v_out")):
         if t is not None:
             _need(t, name, _ROWS, shape)
@@ -746,10 +771,12 @@ def extend_attention(desc: CacheDesc, q, cu_seqlens, codes, scales, page_table, 
     d = desc.c_struct()
     if workspace is None:
         n = lib.uq_extend_workspace_bytes(ctypes.byref(d), T, B, Hq, max_context, window, sinks)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.zeros((T, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.zeros((T, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
     _need(out, "out", _OUT, (T, Hq, desc.head_dim))
     st = lib.uq_extend_attention(ctypes.byref(d), _ptr(q), _DT[q.dtype], q_stride, T, _ptr(cu_seqlens), B, Hq,
                                  _ptr(codes), _ptr(scales), _ptr(page_table), page_table.shape[1], _ptr(context_lens),
@@ -780,10 +807,12 @@ def decode_window(desc: CacheDesc, q, codes, scales, page_table, context_lens, m
         softmax_scale = desc.head_dim ** -0.5
     if workspace is None:
         n = decode_window_workspace_bytes(desc, B, Hq, max_context, window, sinks, partition_tokens)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     qdt = _DT[q.dtype] if q_dtype is None else q_dtype
     st = lib.uq_decode_window(ctypes.byref(d), _ptr(q), qdt, _ptr(k_new), _ptr(v_new),
@@ -876,10 +905,12 @@ def ref_decode_attention(desc: RefCacheDesc, q, cache, page_table, context_lens,
     if softmax_scale is None:
         softmax_scale = HEAD_DIM ** -0.5
     if workspace is None:
-        workspace = ref_alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
+        with _on(stream):
+            workspace = ref_alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     st = lib.uq_ref_decode_attention(ctypes.byref(d), _ptr(q), _DT[q.dtype], B, Hq, _ptr(cache), _ptr(page_table),
                                      page_table.shape[1], _ptr(context_lens), max_context, softmax_scale,
@@ -927,10 +958,12 @@ def ref_decode_step(desc: RefCacheDesc, q, k_new, v_new, cache, page_table, cont
     if softmax_scale is None:
         softmax_scale = HEAD_DIM ** -0.5
     if workspace is None:
-        workspace = ref_alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
+        with _on(stream):
+            workspace = ref_alloc_workspace(desc, B, Hq, max_context, partition_tokens, q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
     d = desc.c_struct()
     fn = lib.uq_ref_decode_step_partials if partials_only else lib.uq_ref_decode_step
     st = fn(ctypes.byref(d), _ptr(q), _DT[q.dtype], _ptr(k_new), _ptr(v_new), _DT[k_new.dtype], B, Hq, _ptr(cache),
@@ -969,7 +1002,7 @@ def _prefix(prefix: SharedPrefix, B):
 
 
 def _cascade_common(q, k_new, v_new, max_context, num_kv_heads, prefix, softmax_scale, partition_tokens, workspace,
-                    out, out_dtype):
+                    out, out_dtype, stream):
     B, Hq = _q_out(q, out, HEAD_DIM)
     _prefix(prefix, B)
     if k_new is not None or v_new is not None:
@@ -978,10 +1011,12 @@ def _cascade_common(q, k_new, v_new, max_context, num_kv_heads, prefix, softmax_
         softmax_scale = HEAD_DIM ** -0.5
     if workspace is None:
         n = cascade_workspace_bytes(num_kv_heads, B, Hq, max_context, prefix, partition_tokens)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
     _need(workspace, "workspace", _U8)
     if out is None:
-        out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, Hq, HEAD_DIM), dtype=out_dtype, device=q.device)
     ndt = UQ_F32 if k_new is None else _DT[k_new.dtype]
     return B, Hq, softmax_scale, workspace, out, ndt
 
@@ -991,7 +1026,7 @@ def decode_cascade(desc: CacheDesc, q, codes, scales, page_table, context_lens, 
                    k_new=None, v_new=None, stream=None, partials_only=False):
     """Decode attention (or, with k_new/v_new, a decode step) with a shared prefix."""
     B, Hq, scale, workspace, out, ndt = _cascade_common(q, k_new, v_new, max_context, desc.num_kv_heads, prefix,
-                                                        softmax_scale, partition_tokens, workspace, out, out_dtype)
+                                                        softmax_scale, partition_tokens, workspace, out, out_dtype, stream)
     _pools(desc, codes, scales)
     _table(page_table, context_lens, B)
     d = desc.c_struct()
@@ -1023,7 +1058,7 @@ def ref_decode_cascade(desc: RefCacheDesc, q, cache, page_table, context_lens, m
                        softmax_scale=None, partition_tokens=0, workspace=None, out=None, out_dtype=torch.float32,
                        k_new=None, v_new=None, stream=None, partials_only=False):
     B, Hq, scale, workspace, out, ndt = _cascade_common(q, k_new, v_new, max_context, desc.num_kv_heads, prefix,
-                                                        softmax_scale, partition_tokens, workspace, out, out_dtype)
+                                                        softmax_scale, partition_tokens, workspace, out, out_dtype, stream)
     _cache(desc, cache)
     _table(page_table, context_lens, B)
     d = desc.c_struct()
@@ -1060,7 +1095,8 @@ def probe_stream_read(buf, sink=None, stream=None):
     returns the per-block checksum words (int32 [PROBE_STREAM_BLOCKS])."""
     _need(buf, "buf", _U8)
     if sink is None:
-        sink = torch.empty(PROBE_STREAM_BLOCKS, dtype=torch.int32, device=buf.device)
+        with _on(stream):
+            sink = torch.empty(PROBE_STREAM_BLOCKS, dtype=torch.int32, device=buf.device)
     _need(sink, "sink", (torch.int32,), min_numel=PROBE_STREAM_BLOCKS)
     _check(lib.uq_probe_stream_read(_ptr(buf), buf.numel(), _ptr(sink), _stream(stream)), "uq_probe_stream_read")
     return sink
@@ -1078,7 +1114,8 @@ def probe_page_gather(desc: CacheDesc, num_q_heads, codes, scales, page_table, c
     part = partition_tokens or default_partition(desc, B, num_q_heads, max_context)
     nwords = 4 * max(1, -(-max_context // part)) * desc.num_kv_heads * B
     if sink is None:
-        sink = torch.empty(nwords, dtype=torch.int32, device=codes.device)
+        with _on(stream):
+            sink = torch.empty(nwords, dtype=torch.int32, device=codes.device)
     _need(sink, "sink", (torch.int32,), min_numel=nwords)
     d = desc.c_struct()
     st = lib.uq_probe_page_gather(ctypes.byref(d), B, num_q_heads, _ptr(codes), _ptr(scales), _ptr(page_table),
@@ -1100,14 +1137,16 @@ def probe_page_gather_cascade(desc: CacheDesc, num_q_heads, codes, scales, page_
     _prefix(prefix, B)
     if workspace is None:
         n = cascade_workspace_bytes(desc.num_kv_heads, B, num_q_heads, max_context, prefix, partition_tokens)
-        workspace = torch.empty(n, dtype=torch.uint8, device=codes.device)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=codes.device)
     _need(workspace, "workspace", _U8)
     part = partition_tokens or default_partition(desc, B, num_q_heads, max_context)
     G = num_q_heads // desc.num_kv_heads
     blocks = (max(1, -(-max_context // part)) * desc.num_kv_heads * B
               + desc.num_kv_heads * -(-B * G // 16) * max(1, -(-prefix.num_tokens // 32)))
     if sink is None:
-        sink = torch.empty(4 * blocks, dtype=torch.int32, device=codes.device)
+        with _on(stream):
+            sink = torch.empty(4 * blocks, dtype=torch.int32, device=codes.device)
     _need(sink, "sink", (torch.int32,), min_numel=1)
     d = desc.c_struct()
     sp = prefix.c_struct()
@@ -1128,7 +1167,8 @@ def probe_mfma(kind, a, b, scale_a=None, scale_b=None, stream=None):
     if kind != PROBE_MFMA_BF16:
         _need(scale_a, "scale_a", _U8, (n, 64))
         _need(scale_b, "scale_b", _U8, (n, 64))
-    d = torch.empty((n, 64, 4), dtype=torch.float32, device=a.device)
+    with _on(stream):
+        d = torch.empty((n, 64, 4), dtype=torch.float32, device=a.device)
     _check(lib.uq_probe_mfma(kind, _ptr(a), _ptr(b), _ptr(scale_a), _ptr(scale_b), n, _ptr(d), _stream(stream)),
            "uq_probe_mfma")
     return d
