@@ -722,7 +722,11 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  *   sinks         : first tokens that stay visible; used with a window only.
  *   workspace     : >= uq_extend_workspace_bytes(...), 16-byte aligned (may be
  *                   NULL when that is 0); no initial contents required.  Calls
- *                   that share one must not run concurrently.
+ *                   that share one must not run concurrently.  The size is that
+ *                   of these very arguments: fewer tokens or sequences, or a
+ *                   shorter context, can need more, as a call is split where its
+ *                   rows do not fill the GPU.  UQ_EXTEND_WORKSPACE_BOUND(head_dim)
+ *                   is enough for every call.
  *   out           : [num_tokens][num_q_heads][head_dim] F32 or BF16,
  *                   contiguous, 16-byte aligned.  A query that sees nothing (a
  *                   position below 0: more queries than context) gives 0.
@@ -742,6 +746,9 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for
  * num_tokens >= 2^24, max_context > 2^30 or more blocks than a grid holds.
  */
+/* At most 1024 blocks' rows (256 each, 128 at head_dim 256) have partials. */
+#define UQ_EXTEND_WORKSPACE_BOUND(head_dim) \
+    (((size_t)1 << ((head_dim) == 256 ? 17 : 18)) * ((size_t)(head_dim) + 2) * sizeof(float))
 size_t uq_extend_workspace_bytes(const uq_cache_desc *desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
                                  int32_t max_context, int32_t window, int32_t sinks);
 uq_status uq_extend_attention(const uq_cache_desc *desc, const void *q, uq_dtype q_dtype, int64_t q_stride,

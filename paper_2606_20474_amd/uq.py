@@ -750,7 +750,15 @@ def read_kv(desc: CacheDesc, slot_mapping, codes, scales, page_table=None, max_p
     return k_out, v_out
 
 
+def extend_workspace_bound(head_dim=HEAD_DIM):
+    """``UQ_EXTEND_WORKSPACE_BOUND``: a workspace of this many bytes is enough
+    for every extend_attention call, whatever its batch."""
+    return (1 << (17 if head_dim == 256 else 18)) * (head_dim + 2) * 4
+
+
 def extend_workspace_bytes(desc: CacheDesc, num_tokens, batch, num_q_heads, max_context, window=0, sinks=0):
+    """Bytes that extend_attention needs for these very arguments; a smaller
+    step can need more (extend_workspace_bound is enough for all)."""
     d = desc.c_struct()
     return int(lib.uq_extend_workspace_bytes(ctypes.byref(d), num_tokens, batch, num_q_heads, max_context, window, sinks))
 

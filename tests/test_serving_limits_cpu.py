@@ -96,3 +96,38 @@ def test_row_outputs_stand_alone():
     for kw in (dict(qo=A), dict(qo=A, odt=F16), dict(qo=A, odt=BF16, qs=1024), dict(qo=A + 16), dict(qo=B), dict(qo=C),
                dict(qo=C + T * KV - 16), dict(qo=A + T * Q - 16)):
         assert write(**{**dict(q=A, k=B, v=C), **kw}) == INVALID, kw
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_one_workspace_for_every_step(d):
+    """The bound holds over batches, heads and contexts, and is within 4 times the largest need met here."""
+    bound = uq.extend_workspace_bound(d)
+    largest, grows_down = 0, False
+    for hkv, group in ((1, 1), (1, 16), (2, 5), (4, 8), (8, 8), (8, 16), (3, 12), (128, 1), (600, 1)):
+        D = desc(head_dim=d, num_kv_heads=hkv)
+        for batch in (1, 2, 3, 16, 63, 64, 65, 300, 5000):
+            last = 0
+            for tokens in sorted({1, 2, 5, batch, 2 * batch, 5 * batch, 64 * batch // group + 1, 64, 128, 333, 512, 1024, 2048,
+                                  8191, 8192, 100000, 1 << 23}):
+                for context in (0, 16, 600, 5000, 131072, 1 << 30):
+                    for window in (0, 300, 40000):
+                        need = uq.lib.uq_extend_workspace_bytes(ctypes.byref(D), tokens, batch, hkv * group, context, window, 4)
+                        assert need <= bound, (hkv, group, batch, tokens, context, window)
+                        largest = max(largest, need)
+                grows_down = grows_down or need < last
+                last = need
+    assert grows_down and largest * 4 >= bound
+
+
+def test_the_header_states_the_same_bound(tmp_path):
+    import os
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc") or shutil.which("cc")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "bound.c"
+    src.write_text('#include "uq.h"\n#include <stdio.h>\nint main(void) { printf("%zu %zu %zu\\n", '
+                   "UQ_EXTEND_WORKSPACE_BOUND(64), UQ_EXTEND_WORKSPACE_BOUND(128), UQ_EXTEND_WORKSPACE_BOUND(256)); return 0; }\n")
+    subprocess.run([cc, "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "bound")], check=True)
+    got = subprocess.run([str(tmp_path / "bound")], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(x) for x in got] == [uq.extend_workspace_bound(d) for d in (64, 128, 256)]
