@@ -732,12 +732,16 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  *                   position below 0: more queries than context) gives 0.
  *                   Rows behind cu_seqlens[batch] are left as they were.
  * QK^T is that of uq_decode_attention (FP8 query, FP4 keys); the softmax
- * runs in fp32; its weights enter PV cut to 11 significant bits (relative error
- * up to 2^-10 each, its mean made up for; uq_decode_attention carries 16 bits).
- * A weight more than 2^9 below the largest of the 32 tokens it is computed with
- * is off by up to 2^-19 of that one, and one more than 2^54 below the row's sum may
- * count as 0.  Values more than 2^31 below the largest one of their token range's 32
- * channels may count as 0 (uq_decode_attention keeps both).
+ * runs in fp32.  Its weights enter PV cut to 11 significant bits (relative error
+ * up to 2^-10 each, its mean made up for; uq_decode_attention carries 16 bits),
+ * or with an error of 2^-31 of the row's largest weight where that is more.
+ * Where a row's heavy tokens have small values (its average so far is below an
+ * eighth of the largest value scale its walk began with, in some 32 channels),
+ * the light ones carry the output: there the second bound is 2^-15 of the
+ * largest weight of the 32 tokens it is computed with, down to 2^-54 of the
+ * row's sum; from the first peak on, or within 2048 tokens of one of many.
+ * Values more than 2^31 below the largest one of their 32 channels so far may
+ * count as 0 (not in uq_decode_attention).
  * A long context with few queries is split over blocks and joined by a second
  * launch; the bits of a row depend on num_tokens, batch, max_context and the
  * other sequences' lengths then.

@@ -38,9 +38,9 @@
 //
 // FP16 holds P with 11 significant bits from 2^-14 on, its range ending at 2^16, and the
 // sum counts weights that FP16 would lose.  So a row's weights are relative to a
-// reference that follows the scores both ways: it is set 7 below the largest score of
-// 32 tokens (whose weight is 2^7 then) when that score leaves [-5, 15] above it.  A
-// row's sum and accumulators are fp32 and hold what lies behind, up to 2^80 of it.
+// reference 7 or more below its largest score, whose weight is 2^7 to 2^15 then, and
+// where the heavy tokens' values are small the reference follows the scores down: the row's
+// sum and accumulators are fp32 and hold what lies behind, up to 2^80 of it.
 //
 // A code times 2^E is exact in FP16 for E in [-23, 13].  So the values of each block of
 // 32 channels are taken relative to an exponent of their own, v 2^-e, and the
@@ -67,12 +67,22 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 constexpr float kLift = 5.08057e-4f;
 constexpr float kLower = 0.99964790f;
 
-// The reference of a row's weights, in powers of two: set kLead below the largest score
-// of 32 tokens, and again when that of others is not within kDown .. kUp above it.  Down
-// only while the row's sum is below 2^kDepth, by at most kDepth, so that the
-// accumulators (at most 2^16 times the sum) stay finite.
-constexpr float kLead = 7.0f, kUp = kLead + kLazyRescale, kDown = kLead - 12.0f;
+// The reference of a row's weights, in powers of two.  It moves up when a score of 32
+// tokens is more than kUp above it, to kLead below that score.  It moves down to the
+// largest of the 32 when that is more than kDown below it and the row's average so far is
+// less than kSmall in some 32 channels, where the largest scale is 2^8 or more: the heavy
+// tokens' values are small then, and light ones count.  Down by at most kDepth and only
+// while the row's sum is below 2^kDepth, so that the accumulators (at most 2^16 times the
+// sum) stay finite.
+constexpr float kLead = 7.0f, kUp = kLead + kLazyRescale, kDown = -9.0f;
+constexpr float kSmall = 32.0f;
 constexpr float kDepth = 40.0f, kDeep = 0x1p40f;
+// A wave looks for low scores while it has credit: 1 for each 32 tokens, at most
+// kCredit, less kCostMoved for each 32 with a lane below kDown where a row moved down and
+// kCostIdle where none did.  (Scores of a standard deviation of 4, 6 and 12 in powers of
+// two, 8192 new tokens of 64 heads: 867, 857 and 855 us, 840, 824 and 840 without looking,
+// 930, 1016 and 1060 when looking at every 32 and whatever the values.)
+constexpr int kCredit = 64, kCostMoved = 8, kCostIdle = 64;
 
 constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
 
@@ -687,6 +697,8 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     }
     bool big_max = false;   // wave-uniform: a reference of magnitude 2^20 or more (see decode_kernel)
 
+    int credit = kCredit;   // wave-uniform
+
     // Tiles of 128 tokens (head size 64): of one that is partly hidden only the 32s with a
     // visible token are computed, and only those with a hidden one masked (window 1024:
     // 220 us, 262 without; 128: 60, 84; no window: the same).  With tiles of 64 windows gain 3
@@ -734,11 +746,48 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                 for (int i = 3; i < 15; i += 2) mx = __builtin_fmaxf(__builtin_fmaxf(mx, s[q][i]), s[q][i + 1]);
                 return __builtin_fmaxf(mx, s[q][15]);
             };
+            auto move = [&](int q, float to) {
+                const float alpha = __builtin_amdgcn_exp2f(m_run[q] - to);
+                l_run[q] *= alpha;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[c][q] *= alpha;
+                m_run[q] = to;
+            };
+            // The references of rows with low scores, moved down; true if one was.  (Both lanes
+            // of a row decide alike; one that sees none of the 32 stays.)
+            auto follow_down = [&]() {
+                bool any = false;
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    float a = max_of(q), b = a, la = l_run[q], lb = la, least = __builtin_inff();
+                    swap32(a, b);
+                    swap32(la, lb);
+                    const float mloc = __builtin_fmaxf(a, b) * sl2, sum = la + lb;
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) {
+                        float oa = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) oa = __builtin_fmaxf(oa, __builtin_fabsf(acc[c][q][i]));
+                        float ob = oa;
+                        swap32(oa, ob);
+                        least = __builtin_fminf(least, __builtin_fmaxf(oa, ob));
+                    }
+                    const bool down = mloc < m_run[q] + kDown && mloc > -__builtin_inff() && sum < kDeep && least < sum * kSmall;
+                    if (down) move(q, __builtin_fmaxf(mloc, m_run[q] - kDepth));
+                    any = any || __builtin_amdgcn_ballot_w64(down) != 0;
+                }
+                return any;
+            };
+            // half the width of the scores' range: kDown .. kUp, or without credit all below kUp
+            // (2^20: a score that low adds nothing)
+            const bool follow = credit > 0;
+            const float reach = follow ? 0.5f * (kUp - kDown) : 0x1p20f;
+            credit = credit < kCredit ? credit + 1 : credit;
             bool moves = !clear || big_max;
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
-                moves = __builtin_amdgcn_ballot_w64(__builtin_fabsf(__builtin_fmaf(max_of(q), sl2, -0.5f * (kUp + kDown) - m_run[q])) >
-                                                    0.5f * (kUp - kDown)) != 0 || moves;
+                moves = __builtin_amdgcn_ballot_w64(__builtin_fabsf(__builtin_fmaf(max_of(q), sl2, (reach - kUp) - m_run[q])) > reach) != 0 ||
+                        moves;
             float scale = sl2, shift[NQ];
             if (__builtin_expect(moves, 0)) {
                 big_max = false;
@@ -761,19 +810,17 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                     float a = max_of(q), b = a;
                     swap32(a, b);
                     const float mloc = __builtin_fmaxf(a, b) * sl2;
-                    // (both lanes of a row decide alike; down, unless the row sees none of the 32)
-                    float la = l_run[q], lb = l_run[q];
-                    swap32(la, lb);
-                    const bool down = mloc < m_run[q] + kDown && mloc > -__builtin_inff() && la + lb < kDeep;
-                    if (mloc > m_run[q] + kUp || down) {
-                        const float to = down ? __builtin_fmaxf(mloc - kLead, m_run[q] - kDepth) : mloc - kLead;
-                        const float alpha = __builtin_amdgcn_exp2f(m_run[q] - to);
-                        l_run[q] *= alpha;
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) acc[c][q] *= alpha;
-                        m_run[q] = to;
-                    }
+                    if (mloc > m_run[q] + kUp) move(q, mloc - kLead);
                     big_max = big_max || __builtin_amdgcn_ballot_w64(__builtin_fabsf(m_run[q]) >= 0x1p20f && m_run[q] != kNoMax) != 0;
+                }
+                if (follow) {
+                    bool low = false;
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q) {
+                        const float a = max_of(q);
+                        low = low || __builtin_amdgcn_ballot_w64(a * sl2 < m_run[q] + kDown && a > -__builtin_inff()) != 0;
+                    }
+                    if (low) credit -= follow_down() ? kCostMoved : kCostIdle;
                 }
             }
 #pragma unroll
