@@ -672,9 +672,10 @@ uq_status uq_norm_rope(const uq_norm_rope_desc *spec, int32_t head_dim, const vo
  *   q             : as above, q_stride; k, v as above with kv_stride, all of
  *                   in_dtype.
  *   q_out         : [num_tokens][num_q_heads][head_dim] F32, BF16, F16 or
- *                   FP8_E4M3 (bytes), 16-byte aligned; it may be q as above,
- *                   and overlaps q, k and v no other way.  Padding tokens get
- *                   their queries too.
+ *                   FP8_E4M3 (bytes, for uq_extend_attention; the decode calls
+ *                   take them at head_dim 128 only, rows at 64 and 256),
+ *                   16-byte aligned; it may be q as above, and overlaps q, k
+ *                   and v no other way.  Padding tokens get their queries too.
  *   page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes,
  *   kv_scales     : as in uq_quantize_kv.
  * Errors: those of uq_norm_rope and uq_quantize_kv.
@@ -742,9 +743,13 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  * row's sum; from the first peak on, or within 2048 tokens of one of many.
  * Values more than 2^31 below the largest one of their 32 channels so far may
  * count as 0 (not in uq_decode_attention).
- * A long context with few queries is split over blocks and joined by a second
- * launch; the bits of a row depend on num_tokens, batch, max_context and the
- * other sequences' lengths then.
+ * Long contexts are split over blocks and joined by a second launch where the
+ * call's rows do not fill the GPU; the bits of a row depend on num_tokens, batch,
+ * max_context and the other sequences' lengths then.  That goes by the whole
+ * call: a sequence with few queries and a long context beside chunks that fill
+ * the GPU is not split, and takes as long as one block takes to walk it (calls of
+ * their own, or uq_decode_attention for single tokens, are split).  A row's last
+ * bits also depend on the rows next to it.
  * num_tokens == 0 or batch == 0 is a no-op.
  * Errors: as uq_decode_attention, plus INVALID_ARGUMENT for a null
  * cu_seqlens, negative sizes, window or sinks, or a bad q_stride; UNSUPPORTED for
@@ -775,7 +780,7 @@ uq_status uq_extend_attention(const uq_cache_desc *desc, const void *q, uq_dtype
  *                   pages; 0 for the default.
  *   workspace     : >= uq_decode_window_workspace_bytes(...).
  * Every other argument, the output and the errors are those of uq_decode_step
- * (the step: head_dim 128), plus INVALID_ARGUMENT for a bad window or sinks or only one of
+ * (the step and FP8 queries: head_dim 128), plus INVALID_ARGUMENT for a bad window or sinks or only one of
  * k_new, v_new.
  */
 size_t uq_decode_window_workspace_bytes(const uq_cache_desc *desc, int32_t batch, int32_t num_q_heads,

@@ -784,8 +784,10 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
     const int64_t rows = num_tokens * group, m = uq::extend_block_rows(desc->head_dim);
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
     // the waves split the tokens of the sequences with few rows where such sequences
-    // are likely the most: few rows on average (the same batch, 40 rows each: 130 us,
-    // 207 us where the waves split the rows, most of them idle)
+    // are likely the most: few rows on average (16 sequences of 5 tokens over 8k to 24k, 40
+    // rows each: 122 us a pass, 204 where the waves split the rows, most of them idle).
+    // Both rules, this and the splits, go by the whole batch: a few single tokens beside
+    // chunks that fill the GPU are walked like the chunks, each by one block.
     e.alone_rows = rows <= seqs * uq::extend_alone_rows(desc->head_dim) ? uq::extend_alone_rows(desc->head_dim) : 0;
     e.row_blocks = rows / m + seqs;
     int64_t blocks = (rows + m - 1) / m;   // of a batch of full sequences; at least one each
@@ -796,15 +798,14 @@ static uq_status extend_shape(const uq_cache_desc* desc, int64_t num_tokens, int
         walk = most < walk ? most : walk;
     }
     const int64_t tiles = (walk + 63) / 64;
-    // two blocks per CU (16 sequences of 5 tokens over 8k to 24k, 128 row blocks: 132
-    // us; 4, 8 and 16 per CU 141, 159 and 212 us)
+    // two blocks per CU (the same batch, 128 row blocks, equal numbers of splits: 137 us;
+    // 4, 8 and 16 per CU 146, 169 and 231)
     int64_t splits = blocks > 0 ? (2 * uq::kNumCus + blocks - 1) / blocks : 1;
     splits = splits < tiles / 4 ? splits : tiles / 4;
     e.splits = int32_t(splits < 1 ? 1 : splits);
     // few rows of sequences with different contexts: shares of one length rather than
-    // as many for each (16 sequences of 5 tokens over 8k to 24k: 117 us, 130 with equal
-    // numbers), in as many blocks as run at once; a sequence may have 4 times the
-    // mean number
+    // as many for each (the same batch: 122 us, 137 with equal numbers), in as many
+    // blocks as run at once; a sequence may have 4 times the mean number
     e.shared = e.splits > 1 && e.alone_rows > 0 && window == 0 && batch > 1 && batch <= 64;
     if (e.shared) {
         const int64_t at_once = 2 * uq::kNumCus / desc->num_kv_heads;
@@ -881,7 +882,7 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     p.splits = e.splits;
     p.alone_rows = e.alone_rows;
     // blocks that do not all run at once, of sequences with different contexts (12
-    // chunks behind contexts of up to 32k tokens, 2576 blocks: 2356 us, 2797 in the
+    // chunks behind contexts of up to 32k tokens, 2576 blocks: 2287 us a pass, 2638 in the
     // sequences' order; the order is kept where every block has a window's length)
     p.longest_first = window == 0 && !e.shared && batch > 1 && batch <= 64 && e.row_blocks * p.num_kv_heads > 2 * uq::kNumCus;
     p.part_acc = static_cast<float*>(workspace);

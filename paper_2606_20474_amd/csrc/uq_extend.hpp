@@ -29,12 +29,13 @@
 // (extend_shape in uq_api.hip has the rules and both sides' times).
 //
 // What bounds it: the issue of the softmax's and the decode's vector instructions
-// beside the matrix instructions.  8192 new tokens of 64 heads over 4, d = 128: 0.80
-// to 0.90 ms, 1.2 to 1.4 PFLOP/s of the 1.1e12 that causality leaves; the matrix
-// cores are busy 47 % of the time and vector instructions issue 71 % of it.  5 tokens of 64 heads over
-// 8 in 16 sequences of 8k to 24k: 117 us, 2.2 TB/s of codes and scales, the four
-// waves' work on 64 rows of which 40 are used (vector 42 %, matrix 16 %, a third of
-// the time waiting with two waves per SIMD).
+// beside the matrix instructions.  8192 new tokens of 64 heads over 4, d = 128: 0.82 ms a
+// pass among others (0.92 on a GPU that idled before), 1.35 PFLOP/s for the 1.1e12 flops
+// that causality leaves; the matrix cores are busy 46 % of the time and vector
+// instructions issue 72 % of it.  5 tokens of 64 heads over 8 in 16 sequences of 8k to
+// 24k: 117 us a pass, 2.2 TB/s of codes and scales, the four waves' work on 64 rows of
+// which 40 are used (vector 52 %, matrix 18 %, 37 % of the waves' time waiting with two
+// waves per SIMD).
 //
 // FP16 holds P with 11 significant bits from 2^-14 on, its range ending at 2^16, and the
 // sum counts weights that FP16 would lose.  So a row's weights are relative to a
@@ -697,12 +698,13 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     }
     bool big_max = false;   // wave-uniform: a reference of magnitude 2^20 or more (see decode_kernel)
 
-    int credit = kCredit;   // wave-uniform
+    int credit = kCredit;   // for looking down, wave-uniform
 
     // Tiles of 128 tokens (head size 64): of one that is partly hidden only the 32s with a
-    // visible token are computed, and only those with a hidden one masked (window 1024:
-    // 220 us, 262 without; 128: 60, 84; no window: the same).  With tiles of 64 windows gain 3
-    // to 8 % of it, and long prompts lose 1 %: not there.
+    // visible token are computed, and only those with a hidden one masked (two prompts of
+    // 4099, 64 heads over 8, window 1024: 198 us a pass, 245 without; 128: 83, 135; no
+    // window: the same).  With tiles of 64 (head size 128) windows gain, 307 us against 321
+    // and 135 against 157, and chunks behind long contexts lose, 2314 against 2292: not there.
     constexpr bool kPick = TT > 64;
     auto clear_of = [&](int from, int n) {
         return from + n - 1 <= w_lo && (p.window == 0 || from > w_hi - p.window || from + n <= p.sinks);

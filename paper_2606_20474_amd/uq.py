@@ -704,7 +704,8 @@ def norm_rope_write(desc: CacheDesc, spec: NormRope, q, k, v, slot_mapping, code
                     q_out_dtype=torch.uint8, page_table=None, max_pages_per_seq=0, stream=None):
     """norm_rope with the cache behind it: k and v [T, Hkv, d] go into the
     pools at `slot_mapping`; returns the queries, prepared FP8 bytes
-    (uint8, the default) or rows."""
+    (uint8, the default) or rows of `q_out_dtype`.  extend_attention takes
+    the bytes at every head size, the decode calls at 128 only."""
     num_seqs, mpps = _write_table(page_table, max_pages_per_seq)
     d = desc.head_dim
     q_stride = _head_rows(q, "q", _ROWS, (None, None, d))
