@@ -740,7 +740,8 @@ uq_status uq_read_kv(const uq_cache_desc *desc, const uint8_t *kv_codes, const u
  * eighth of the largest value scale its walk began with, in some 32 channels),
  * the light ones carry the output: there the second bound is 2^-15 of the
  * largest weight of the 32 tokens it is computed with, down to 2^-54 of the
- * row's sum; from the first peak on, or within 2048 tokens of one of many.
+ * row's sum; at once after a first such token, within 2048 to 8192 tokens where
+ * they follow each other or other rows have light tokens that do not count.
  * Values more than 2^31 below the largest one of their 32 channels so far may
  * count as 0 (not in uq_decode_attention).
  * Long contexts are split over blocks and joined by a second launch where the

@@ -783,12 +783,12 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
             // half the width of the scores' range: kDown .. kUp, or without credit all below kUp
             // (2^20: a score that low adds nothing)
             const bool follow = credit > 0;
-            const float reach = follow ? 0.5f * (kUp - kDown) : 0x1p20f;
+            const float width = follow ? 0.5f * (kUp - kDown) : 0x1p20f;
             credit = credit < kCredit ? credit + 1 : credit;
             bool moves = !clear || big_max;
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
-                moves = __builtin_amdgcn_ballot_w64(__builtin_fabsf(__builtin_fmaf(max_of(q), sl2, (reach - kUp) - m_run[q])) > reach) != 0 ||
+                moves = __builtin_amdgcn_ballot_w64(__builtin_fabsf(__builtin_fmaf(max_of(q), sl2, (width - kUp) - m_run[q])) > width) != 0 ||
                         moves;
             float scale = sl2, shift[NQ];
             if (__builtin_expect(moves, 0)) {
