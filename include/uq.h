@@ -686,6 +686,38 @@ uq_status uq_norm_rope_write(const uq_cache_desc *desc, const uq_norm_rope_desc 
                              const int32_t *page_table, int32_t num_seqs, int32_t max_pages_per_seq,
                              const int64_t *slot_mapping, uint8_t *kv_codes, uint8_t *kv_scales, void *stream);
 
+/* Positions with several axes (time, height and width of an image's or a
+ * video's tokens): every pair of rotated channels turns by the position of
+ * one of them. */
+typedef struct uq_rope_axes {
+    int32_t num_axes;           /* 1 .. 4 */
+    int64_t position_stride;    /* spec.positions is [num_axes][position_stride], >= num_tokens */
+    const uint8_t *pair_axes;   /* HOST array [rot_dim / 2], read during the call: the axis of each pair, below num_axes;
+                                   pair j is channels j and j + rot_dim / 2, or (interleaved) 2 j and 2 j + 1 */
+} uq_rope_axes;
+
+/*
+ * uq_norm_rope_axes, uq_norm_rope_axes_write -- uq_norm_rope and
+ * uq_norm_rope_write where pair j of token t turns by row
+ * positions[pair_axes[j]][t] of cos_sin, its columns j and rot_dim / 2 + j.
+ * Axes that are equal give the bits of those calls.  Each axis's positions
+ * are clamped to [0, max_position).  Any map of pairs to axes is taken;
+ * one that is constant over aligned 8 pairs, or 4, loads angles in wide words.
+ * Errors: those of the calls, plus INVALID_ARGUMENT for a NULL axes or
+ * pair_axes, num_axes outside 1 .. 4, an axis out of range, a
+ * position_stride below num_tokens, or rot_dim == 0.
+ */
+uq_status uq_norm_rope_axes(const uq_norm_rope_desc *spec, const uq_rope_axes *axes, int32_t head_dim, const void *q,
+                            int64_t q_stride, int32_t num_q_heads, const void *k, int64_t k_stride,
+                            int32_t num_kv_heads, uq_dtype in_dtype, int64_t num_tokens, void *q_out, void *k_out,
+                            uq_dtype out_dtype, void *stream);
+uq_status uq_norm_rope_axes_write(const uq_cache_desc *desc, const uq_norm_rope_desc *spec, const uq_rope_axes *axes,
+                                  const void *q, int64_t q_stride, int32_t num_q_heads, const void *k, const void *v,
+                                  int64_t kv_stride, uq_dtype in_dtype, int64_t num_tokens, void *q_out,
+                                  uq_dtype q_out_dtype, const int32_t *page_table, int32_t num_seqs,
+                                  int32_t max_pages_per_seq, const int64_t *slot_mapping, uint8_t *kv_codes,
+                                  uint8_t *kv_scales, void *stream);
+
 /*
  * uq_read_kv -- stored tokens as rows, the inverse of uq_quantize_kv: the
  * values the codes and scales stand for, K rotated back, V with rotate_v, in
@@ -767,6 +799,140 @@ uq_status uq_extend_attention(const uq_cache_desc *desc, const void *q, uq_dtype
                               int32_t max_pages_per_seq, const int32_t *context_lens, int32_t max_context,
                               int32_t window, int32_t sinks, float softmax_scale, void *workspace,
                               size_t workspace_bytes, void *out, uq_dtype out_dtype, void *stream);
+
+/*
+ * uq_cross_attention -- attention of ragged queries to tokens without order:
+ * every query of sequence b sees all context_lens[b] tokens of it, as those of
+ * a decoder that attends to an encoder's states (uq_quantize_kv has written
+ * them).  Query and context lengths are independent; a context of 0 gives 0.
+ * For one query per sequence uq_decode_attention is the same and faster.
+ * Arguments, precision, the split and the errors are those of
+ * uq_extend_attention without a window; workspace >=
+ * uq_cross_workspace_bytes(...), and UQ_EXTEND_WORKSPACE_BOUND(head_dim) is
+ * enough for every call.
+ */
+size_t uq_cross_workspace_bytes(const uq_cache_desc *desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
+                                int32_t max_context);
+uq_status uq_cross_attention(const uq_cache_desc *desc, const void *q, uq_dtype q_dtype, int64_t q_stride,
+                             int64_t num_tokens, const int32_t *cu_seqlens, int32_t batch, int32_t num_q_heads,
+                             const uint8_t *kv_codes, const uint8_t *kv_scales, const int32_t *page_table,
+                             int32_t max_pages_per_seq, const int32_t *context_lens, int32_t max_context,
+                             float softmax_scale, void *workspace, size_t workspace_bytes, void *out,
+                             uq_dtype out_dtype, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Eviction.
+ *
+ * A cache that may not grow beyond a budget keeps, of every sequence and KV
+ * head, the tokens that attention has used most: uq_token_weights adds what a
+ * step's queries gave each token to its weight, uq_select_tokens picks the
+ * tokens that stay, uq_compact_kv moves them to the front of their pages and
+ * gives the pages behind them back.  KV heads keep different tokens (each
+ * has tiles of its own in a page) but equally many, so page tables and
+ * lengths stay one per sequence; decode and extend attention read the
+ * result as any cache.  A token's index is not its position any more: the
+ * next tokens' positions are the caller's (uq_norm_rope takes them apart from
+ * the slots), and a sliding window counts cached tokens.
+ *
+ * Weights are fp32 [batch][num_kv_heads][weights_width]: entry t belongs to
+ * token t of the sequence's context.  They start at 0; uq_compact_kv moves them
+ * with their tokens and clears the entries behind, so that new tokens start
+ * at 0 again.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * uq_token_weights -- for every token t of sequence b and KV head h
+ *   weights[b][h][t] += sum over the queries i and the head's query heads j of
+ *                       softmax over the tokens query i sees of
+ *                       (softmax_scale q8_ij . k_.), at t,
+ * q8 and k as in uq_decode_attention (FP8 query, FP4 keys), all else in fp32.
+ *   q, q_dtype, q_stride, cu_seqlens, num_tokens, kv_codes, kv_scales,
+ *   page_table, context_lens, max_context : as in uq_extend_attention, called
+ *                   after the step's keys are written.
+ *   last          : only the last `last` queries of each sequence count; 0: all.
+ *   causal        : 1: query i of m sees the tokens up to its position n - m
+ *                   + i, as in uq_extend_attention; 0: all n.
+ *   weights       : as above, weights_width >= max_context; entries at and
+ *                   behind a context's length, and the rows of sequences
+ *                   without queries, are left as they were.
+ *   workspace     : >= uq_token_weights_workspace_bytes(...), 16-byte aligned, no
+ *                   initial contents required; the size does not fall when an argument
+ *                   grows (q_dtype and num_kv_heads apart; `last` from 0 on counts as
+ *                   the largest).  Calls that share one must not run concurrently.
+ * Every sum has one order: the same call gives the same bits.
+ * num_tokens, batch or max_context of 0 is a no-op.
+ * Errors: those of uq_extend_attention, plus INVALID_ARGUMENT for a NULL
+ * weights or workspace, a weights_width below max_context, a negative last, or
+ * weights or a workspace that overlap an input or each other;
+ * UNSUPPORTED for 2^30 pieces of work or more (a wave's, of 512 tokens or 128
+ * rows), or 2^30 query vectors that are not FP8.
+ */
+size_t uq_token_weights_workspace_bytes(const uq_cache_desc *desc, uq_dtype q_dtype, int64_t num_tokens, int32_t batch,
+                                        int32_t num_q_heads, int32_t max_context, int32_t last);
+uq_status uq_token_weights(const uq_cache_desc *desc, const void *q, uq_dtype q_dtype, int64_t q_stride,
+                           int64_t num_tokens, const int32_t *cu_seqlens, int32_t batch, int32_t num_q_heads,
+                           const uint8_t *kv_codes, const uint8_t *kv_scales, const int32_t *page_table,
+                           int32_t max_pages_per_seq, const int32_t *context_lens, int32_t max_context, int32_t last,
+                           int32_t causal, float softmax_scale, float *weights, int64_t weights_width, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * uq_select_tokens -- the tokens of every sequence and KV head that stay.  A
+ * context of n = min(context_lens[b], max_context) <= budget tokens stays
+ * whole; of a longer one the first `sinks`, the last `recent` and, of those
+ * between, the budget - sinks - recent of the largest weight, of equal ones
+ * those of the lowest index (-0 equals 0; a NaN is below every number).
+ *   weights       : as above (may be NULL when max_context <= budget).
+ *   kept          : int32 [batch][num_kv_heads][budget]: the indices that
+ *                   stay, ascending, -1 behind the last.
+ *   kept_lens     : int32 [batch]: how many, min(n, budget): the context
+ *                   lengths after uq_compact_kv.
+ *   workspace     : >= uq_select_tokens_workspace_bytes(...), 16-byte aligned (may be NULL
+ *                   when that is 0).
+ * batch == 0 is a no-op.
+ * Errors: INVALID_ARGUMENT for null pointers, negative sizes, num_kv_heads or
+ * budget < 1, sinks + recent > budget, weights_width < max_context, outputs that
+ * overlap an input or each other (kept_lens is not the context_lens of the call);
+ * UNSUPPORTED for batch or num_kv_heads > 65535, 2^22 (sequence, KV head)
+ * pairs, or sizes above 2^30; WORKSPACE_TOO_SMALL.
+ */
+size_t uq_select_tokens_workspace_bytes(int32_t batch, int32_t num_kv_heads, int32_t max_context, int32_t budget);
+uq_status uq_select_tokens(const float *weights, int64_t weights_width, int32_t batch, int32_t num_kv_heads,
+                           const int32_t *context_lens, int32_t max_context, int32_t budget, int32_t sinks,
+                           int32_t recent, int32_t *kept, int32_t *kept_lens, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/*
+ * uq_compact_kv -- token i of sequence b and KV head h becomes token
+ * kept[b][h][i], i < kept_lens[b]: codes and scale bytes, as they are, in place
+ * through page_table.  Tokens with kept[b][h][i] == i are not written, so pages
+ * at the front that keep all their tokens may be shared with other sequences;
+ * the others must not be pages that another sequence of the call has.
+ *   kept          : int32 [batch][num_kv_heads][budget], as uq_select_tokens gives it: in
+ *                   each row the first kept_lens[b] entries ascend strictly (so that
+ *                   kept[b][h][i] >= i).
+ *   context_lens  : int32 [batch], the lengths before; they are not changed (kept_lens
+ *                   are the new ones).
+ *   weights       : NULL, or as above: moved with the tokens, and the entries from
+ *                   kept_lens[b] to context_lens[b] (at most weights_width) set to 0.
+ *   freed_pages, freed_count : both NULL, or int32 [batch * max_pages_per_seq] and
+ *                   int32 [1]: the page ids of the page-table entries from
+ *                   ceil(kept_lens[b] / 16) to ceil(context_lens[b] / 16), sequence
+ *                   after sequence, and how many.  The table itself is not changed.
+ *   workspace     : >= uq_compact_kv_workspace_bytes(...), 16-byte aligned (may be NULL
+ *                   when that is 0); no initial contents required.
+ * Errors: INVALID_ARGUMENT for null or misaligned pointers, only one of
+ * freed_pages and freed_count, negative sizes, num_kv_heads, budget or
+ * max_pages_per_seq < 1, pools, weights or freed arrays that overlap an input or
+ * each other; UNSUPPORTED as in uq_select_tokens, and for
+ * max_pages_per_seq >= 2^27; WORKSPACE_TOO_SMALL.
+ */
+size_t uq_compact_kv_workspace_bytes(const uq_cache_desc *desc, int32_t batch, int32_t budget);
+uq_status uq_compact_kv(const uq_cache_desc *desc, const int32_t *kept, int32_t budget, const int32_t *kept_lens,
+                        const int32_t *context_lens, int32_t batch, uint8_t *kv_codes, uint8_t *kv_scales,
+                        const int32_t *page_table, int32_t max_pages_per_seq, float *weights, int64_t weights_width,
+                        int32_t *freed_pages, int32_t *freed_count, void *workspace, size_t workspace_bytes,
+                        void *stream);
 
 /*
  * uq_decode_window -- uq_decode_attention (k_new == v_new == NULL) or

@@ -2,6 +2,7 @@
 // validation on the host, launch configuration, workspace sizing.
 #include <atomic>
 #include <cstring>
+#include <initializer_list>
 #include <math.h>
 #include <mutex>
 #include <stdint.h>
@@ -549,9 +550,9 @@ static bool meets_own(const TokenRows& out, const TokenRows& x) {
 
 // The norm and rotation part of the parameter block; every argument check of
 // the spec, q and the output types.
-static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
-                                 int32_t num_q_heads, uq_dtype in_dtype, int64_t num_tokens, void* q_out,
-                                 uq_dtype out_dtype, uq::NormRopeParams& p) {
+static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, const uq_rope_axes* axes, int32_t head_dim, const void* q,
+                                 int64_t q_stride, int32_t num_q_heads, uq_dtype in_dtype, int64_t num_tokens,
+                                 void* q_out, uq_dtype out_dtype, uq::NormRopeParams& p) {
     if (spec == nullptr || num_tokens < 0 || num_q_heads < 1 || spec->rot_dim < 0) return UQ_ERR_INVALID_ARGUMENT;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return UQ_ERR_UNSUPPORTED;
     if (!row_dtype(in_dtype)) return UQ_ERR_UNSUPPORTED;
@@ -565,6 +566,23 @@ static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim
     if (num_tokens > 0 && (!rows_ok(q, q_stride, num_q_heads, head_dim, in_dtype) || q_out == nullptr || !aligned16(q_out)))
         return UQ_ERR_INVALID_ARGUMENT;
     if (num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
+    p.num_axes = 0;
+    p.axis_stride = 0;
+    p.axis_unit = 8;
+    for (uint32_t& w : p.axis_of) w = 0;
+    if (axes != nullptr) {
+        if (rot == 0 || axes->num_axes < 1 || axes->num_axes > 4 || axes->pair_axes == nullptr ||
+            axes->position_stride < num_tokens)
+            return UQ_ERR_INVALID_ARGUMENT;
+        p.num_axes = axes->num_axes;
+        p.axis_stride = axes->position_stride;
+        for (int32_t i = 0; i < rot / 2; ++i) {
+            const uint32_t a = axes->pair_axes[i];
+            if (a >= uint32_t(axes->num_axes)) return UQ_ERR_INVALID_ARGUMENT;
+            p.axis_of[i / 16] |= a << (2 * (i % 16));
+            while (a != axes->pair_axes[i & ~(p.axis_unit - 1)]) p.axis_unit = p.axis_unit == 8 ? 4 : 1;
+        }
+    }
     p.q = q;
     p.k = nullptr;
     p.q_stride = q_stride;
@@ -587,12 +605,12 @@ static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, int32_t head_dim
     return UQ_OK;
 }
 
-uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
-                       int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
-                       uq_dtype in_dtype, int64_t num_tokens, void* q_out, void* k_out, uq_dtype out_dtype,
-                       void* stream) {
+static uq_status norm_rope(const uq_norm_rope_desc* spec, const uq_rope_axes* axes, int32_t head_dim, const void* q,
+                           int64_t q_stride, int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
+                           uq_dtype in_dtype, int64_t num_tokens, void* q_out, void* k_out, uq_dtype out_dtype,
+                           void* stream) {
     uq::NormRopeParams p;
-    uq_status s = norm_rope_setup(spec, head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, out_dtype, p);
+    uq_status s = norm_rope_setup(spec, axes, head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, out_dtype, p);
     if (s != UQ_OK) return s;
     if (!row_dtype(out_dtype)) return UQ_ERR_UNSUPPORTED;
     if (num_tokens == 0) return num_kv_heads < 0 ? UQ_ERR_INVALID_ARGUMENT : UQ_OK;
@@ -618,15 +636,16 @@ uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const vo
     return from_hip(uq::launch_norm_rope(p, nullptr, head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));
 }
 
-uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc* spec, const void* q,
-                             int64_t q_stride, int32_t num_q_heads, const void* k, const void* v, int64_t kv_stride,
-                             uq_dtype in_dtype, int64_t num_tokens, void* q_out, uq_dtype q_out_dtype,
-                             const int32_t* page_table, int32_t num_seqs, int32_t max_pages_per_seq,
-                             const int64_t* slot_mapping, uint8_t* kv_codes, uint8_t* kv_scales, void* stream) {
+static uq_status norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc* spec, const uq_rope_axes* axes,
+                                 const void* q, int64_t q_stride, int32_t num_q_heads, const void* k, const void* v,
+                                 int64_t kv_stride, uq_dtype in_dtype, int64_t num_tokens, void* q_out,
+                                 uq_dtype q_out_dtype, const int32_t* page_table, int32_t num_seqs,
+                                 int32_t max_pages_per_seq, const int64_t* slot_mapping, uint8_t* kv_codes,
+                                 uint8_t* kv_scales, void* stream) {
     uq_status s = check_desc(desc);
     if (s != UQ_OK) return s;
     uq::NormRopeParams p;
-    s = norm_rope_setup(spec, desc->head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, q_out_dtype, p);
+    s = norm_rope_setup(spec, axes, desc->head_dim, q, q_stride, num_q_heads, in_dtype, num_tokens, q_out, q_out_dtype, p);
     if (s != UQ_OK) return s;
     if (!row_dtype(q_out_dtype) && q_out_dtype != UQ_FP8_E4M3) return UQ_ERR_UNSUPPORTED;
     if (num_tokens == 0) return UQ_OK;
@@ -644,6 +663,43 @@ uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc*
     const uq::QuantizeParams c = slot_params(desc, k, v, num_tokens, kv_stride, page_table, num_seqs,
                                              max_pages_per_seq, slot_mapping, kv_codes, kv_scales);
     return from_hip(uq::launch_norm_rope(p, &c, desc->head_dim, int(in_dtype), static_cast<hipStream_t>(stream)));
+}
+
+uq_status uq_norm_rope(const uq_norm_rope_desc* spec, int32_t head_dim, const void* q, int64_t q_stride,
+                       int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
+                       uq_dtype in_dtype, int64_t num_tokens, void* q_out, void* k_out, uq_dtype out_dtype,
+                       void* stream) {
+    return norm_rope(spec, nullptr, head_dim, q, q_stride, num_q_heads, k, k_stride, num_kv_heads, in_dtype, num_tokens,
+                     q_out, k_out, out_dtype, stream);
+}
+
+uq_status uq_norm_rope_axes(const uq_norm_rope_desc* spec, const uq_rope_axes* axes, int32_t head_dim, const void* q,
+                            int64_t q_stride, int32_t num_q_heads, const void* k, int64_t k_stride,
+                            int32_t num_kv_heads, uq_dtype in_dtype, int64_t num_tokens, void* q_out, void* k_out,
+                            uq_dtype out_dtype, void* stream) {
+    if (axes == nullptr) return UQ_ERR_INVALID_ARGUMENT;
+    return norm_rope(spec, axes, head_dim, q, q_stride, num_q_heads, k, k_stride, num_kv_heads, in_dtype, num_tokens,
+                     q_out, k_out, out_dtype, stream);
+}
+
+uq_status uq_norm_rope_write(const uq_cache_desc* desc, const uq_norm_rope_desc* spec, const void* q,
+                             int64_t q_stride, int32_t num_q_heads, const void* k, const void* v, int64_t kv_stride,
+                             uq_dtype in_dtype, int64_t num_tokens, void* q_out, uq_dtype q_out_dtype,
+                             const int32_t* page_table, int32_t num_seqs, int32_t max_pages_per_seq,
+                             const int64_t* slot_mapping, uint8_t* kv_codes, uint8_t* kv_scales, void* stream) {
+    return norm_rope_write(desc, spec, nullptr, q, q_stride, num_q_heads, k, v, kv_stride, in_dtype, num_tokens, q_out,
+                           q_out_dtype, page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales, stream);
+}
+
+uq_status uq_norm_rope_axes_write(const uq_cache_desc* desc, const uq_norm_rope_desc* spec, const uq_rope_axes* axes,
+                                  const void* q, int64_t q_stride, int32_t num_q_heads, const void* k, const void* v,
+                                  int64_t kv_stride, uq_dtype in_dtype, int64_t num_tokens, void* q_out,
+                                  uq_dtype q_out_dtype, const int32_t* page_table, int32_t num_seqs,
+                                  int32_t max_pages_per_seq, const int64_t* slot_mapping, uint8_t* kv_codes,
+                                  uint8_t* kv_scales, void* stream) {
+    if (axes == nullptr) return UQ_ERR_INVALID_ARGUMENT;
+    return norm_rope_write(desc, spec, axes, q, q_stride, num_q_heads, k, v, kv_stride, in_dtype, num_tokens, q_out,
+                           q_out_dtype, page_table, num_seqs, max_pages_per_seq, slot_mapping, kv_codes, kv_scales, stream);
 }
 
 uq_status uq_read_kv(const uq_cache_desc* desc, const uint8_t* kv_codes, const uint8_t* kv_scales,
@@ -828,12 +884,12 @@ size_t uq_extend_workspace_bytes(const uq_cache_desc* desc, int64_t num_tokens, 
     return extend_shape(desc, num_tokens, batch, num_q_heads, max_context, window, sinks, e) == UQ_OK ? e.workspace : 0;
 }
 
-uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride,
-                              int64_t num_tokens, const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads,
-                              const uint8_t* kv_codes, const uint8_t* kv_scales, const int32_t* page_table,
-                              int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context,
-                              int32_t window, int32_t sinks, float softmax_scale, void* workspace,
-                              size_t workspace_bytes, void* out, uq_dtype out_dtype, void* stream) {
+static uq_status extend(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride, int64_t num_tokens,
+                        const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads, const uint8_t* kv_codes,
+                        const uint8_t* kv_scales, const int32_t* page_table, int32_t max_pages_per_seq,
+                        const int32_t* context_lens, int32_t max_context, int32_t window, int32_t sinks, bool cross,
+                        float softmax_scale, void* workspace, size_t workspace_bytes, void* out, uq_dtype out_dtype,
+                        void* stream) {
     ExtendShape e;
     uq_status s = extend_shape(desc, num_tokens, batch, num_q_heads, max_context, window, sinks, e);
     if (s != UQ_OK) return s;
@@ -876,6 +932,7 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     const int32_t reach = max_context > 1 ? max_context : 1;
     p.window = window < reach ? window : reach;
     p.sinks = window == 0 ? 0 : sinks < reach ? sinks : reach;
+    p.cross = cross;
     p.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
     p.rotate_v = desc->rotate_v != 0;
     p.row_blocks = int32_t(e.row_blocks);
@@ -891,6 +948,280 @@ uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype
     p.out = out;
     p.out_dtype = out_dtype == UQ_F32 ? 0 : 1;
     return from_hip(uq::launch_extend(p, static_cast<hipStream_t>(stream)));
+}
+
+uq_status uq_extend_attention(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride,
+                              int64_t num_tokens, const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads,
+                              const uint8_t* kv_codes, const uint8_t* kv_scales, const int32_t* page_table,
+                              int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context,
+                              int32_t window, int32_t sinks, float softmax_scale, void* workspace,
+                              size_t workspace_bytes, void* out, uq_dtype out_dtype, void* stream) {
+    return extend(desc, q, q_dtype, q_stride, num_tokens, cu_seqlens, batch, num_q_heads, kv_codes, kv_scales, page_table,
+                  max_pages_per_seq, context_lens, max_context, window, sinks, false, softmax_scale, workspace,
+                  workspace_bytes, out, out_dtype, stream);
+}
+
+size_t uq_cross_workspace_bytes(const uq_cache_desc* desc, int64_t num_tokens, int32_t batch, int32_t num_q_heads,
+                                int32_t max_context) {
+    return uq_extend_workspace_bytes(desc, num_tokens, batch, num_q_heads, max_context, 0, 0);
+}
+
+uq_status uq_cross_attention(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride,
+                             int64_t num_tokens, const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads,
+                             const uint8_t* kv_codes, const uint8_t* kv_scales, const int32_t* page_table,
+                             int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context,
+                             float softmax_scale, void* workspace, size_t workspace_bytes, void* out,
+                             uq_dtype out_dtype, void* stream) {
+    return extend(desc, q, q_dtype, q_stride, num_tokens, cu_seqlens, batch, num_q_heads, kv_codes, kv_scales, page_table,
+                  max_pages_per_seq, context_lens, max_context, 0, 0, true, softmax_scale, workspace, workspace_bytes, out,
+                  out_dtype, stream);
+}
+
+// Memory a call reads or writes.  Blocks that run beside each other read the inputs
+// while others write: an output shares no byte with an input or another output.
+struct Span {
+    const void* at;
+    size_t bytes;
+};
+static bool outputs_meet(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+    auto meet = [](const Span& a, const Span& b) {
+        return a.at != nullptr && b.at != nullptr && overlaps(a.at, a.bytes, b.at, b.bytes);
+    };
+    for (const Span& o : outs) {
+        for (const Span& i : ins)
+            if (meet(o, i)) return true;
+        for (const Span& other : outs)
+            if (&other != &o && meet(o, other)) return true;
+    }
+    return false;
+}
+static Span codes_span(const uq_cache_desc* d, const uint8_t* at) {
+    return {at, size_t(d->num_pages) * size_t(d->num_kv_heads) * 16 * size_t(d->head_dim)};
+}
+static Span scales_span(const uq_cache_desc* d, const uint8_t* at) {
+    return {at, size_t(d->num_pages) * size_t(d->num_kv_heads) * size_t(d->head_dim)};
+}
+
+// How a call of uq_token_weights is cut.  A wave of the first kernel holds
+// 16 row_units rows and walks `chunk` tokens, one of the second holds key_units units of
+// keys (16 tokens; 32 at head size 64) and walks row_split rows.
+struct WeightsShape {
+    int64_t rows_per_head;
+    bool by_seq;
+    int32_t row_units, chunk, chunks, key_units, row_split, splits;
+    int32_t norm_blocks, sum_blocks;
+    size_t query, rows;    // bytes of the prepared queries and of the rows' references and sums
+    size_t workspace;
+};
+// Partial results of split rows or contexts: the splits below keep to it.
+constexpr size_t kWeightsParts = size_t(16) << 20;
+constexpr int64_t kWeightsWaves = 4096;    // four per SIMD
+
+static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int64_t num_tokens, int32_t batch,
+                               int32_t num_q_heads, int32_t max_context, int32_t last, WeightsShape& e) {
+    uq_status s = check_desc(desc);
+    if (s != UQ_OK) return s;
+    if (num_tokens < 0 || batch < 0 || num_q_heads < 1 || max_context < 0 || last < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (num_q_heads % desc->num_kv_heads != 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (!row_dtype(q_dtype) && q_dtype != UQ_FP8_E4M3) return UQ_ERR_UNSUPPORTED;
+    const int64_t group = num_q_heads / desc->num_kv_heads, heads = desc->num_kv_heads;
+    if (group > kMaxGroup || batch > 65535 || heads > 65535) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens >= (int64_t(1) << 24)) return UQ_ERR_UNSUPPORTED;   // rows of a KV head are numbered in 28 bits
+    if (max_context > (1 << 30)) return UQ_ERR_UNSUPPORTED;
+    if (q_dtype != UQ_FP8_E4M3 && num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
+    const int64_t seqs = num_tokens < batch ? num_tokens : batch;
+    e.by_seq = last > 0 && int64_t(batch) * last < num_tokens;
+    const int64_t queries = e.by_seq ? int64_t(batch) * last : num_tokens;
+    e.rows_per_head = queries * group;
+    // 16 rows per wave where a sequence has no more, up to 128 (64 at head size 256, whose
+    // operands are twice as large)
+    const int64_t each = seqs > 0 ? (e.rows_per_head + seqs - 1) / seqs : 1;
+    const int32_t most = desc->head_dim == 256 ? 4 : 8;
+    e.row_units = 1;
+    while (e.row_units < most && 16 * e.row_units < each) e.row_units *= 2;
+    const int64_t row_blocks = (e.rows_per_head / (16 * e.row_units) + seqs) * heads;
+    // the longest chunks, from 512 tokens on, that leave a wave for every place
+    const int64_t bound = max_context > 1 ? max_context : 1;
+    e.chunk = 1 << 30;
+    while (e.chunk > 512 && row_blocks * ((bound + e.chunk - 1) / e.chunk) < kWeightsWaves) e.chunk /= 2;
+    const int64_t rows = e.rows_per_head * heads;
+    while (e.chunk < (1 << 30) && bound > e.chunk && size_t(rows) * size_t((bound + e.chunk - 1) / e.chunk) * 8 > kWeightsParts) e.chunk *= 2;
+    e.chunks = int32_t((bound + e.chunk - 1) / e.chunk);
+    const int64_t norm_waves = row_blocks * e.chunks;
+    // keys: 128 tokens per wave where that leaves enough waves, else 2 units
+    const int32_t unit = desc->head_dim == 64 ? 32 : 16, wide = desc->head_dim == 128 ? 8 : 4;
+    auto groups = [&](int32_t units) { return int64_t(batch) * heads * ((bound + units * unit - 1) / (units * unit)); };
+    e.key_units = groups(wide) >= kWeightsWaves ? wide : 2;
+    // rows split where the keys are too few
+    const int64_t longest = (e.by_seq || (last > 0 && last < num_tokens) ? int64_t(last) : num_tokens) * group;
+    int64_t splits = groups(e.key_units) > 0 ? kWeightsWaves / groups(e.key_units) : 1;
+    splits = splits < longest / 256 ? splits : longest / 256;
+    const size_t part = size_t(batch) * size_t(heads) * size_t(bound) * sizeof(float);
+    while (splits > 1 && part * size_t(splits) > kWeightsParts) --splits;
+    splits = splits > 1 ? splits : 1;
+    e.row_split = int32_t(((longest + splits - 1) / splits + 15) / 16 * 16);
+    if (e.row_split < 16) e.row_split = 16;
+    e.splits = int32_t(longest > 0 ? (longest + e.row_split - 1) / e.row_split : 1);
+    const int64_t sum_waves = groups(e.key_units) * e.splits;
+    // items are numbered in 31 bits
+    if (norm_waves >= (int64_t(1) << 30) || sum_waves >= (int64_t(1) << 30)) return UQ_ERR_UNSUPPORTED;
+    const int64_t at_once = 32 * int64_t(uq::kNumCus);   // blocks of 4 waves; a wave goes on to further items
+    e.norm_blocks = int32_t(norm_waves / 4 + 1 < at_once ? norm_waves / 4 + 1 : at_once);
+    e.sum_blocks = int32_t(sum_waves / 4 + 1 < at_once ? sum_waves / 4 + 1 : at_once);
+    e.query = q_dtype == UQ_FP8_E4M3 ? 0 : align16(size_t(num_tokens) * size_t(num_q_heads) * size_t(desc->head_dim));
+    e.rows = align16((size_t(rows) + 16) * sizeof(float));
+    e.workspace = e.query + 2 * e.rows + kWeightsParts;
+    return UQ_OK;
+}
+
+size_t uq_token_weights_workspace_bytes(const uq_cache_desc* desc, uq_dtype q_dtype, int64_t num_tokens, int32_t batch,
+                                        int32_t num_q_heads, int32_t max_context, int32_t last) {
+    WeightsShape e;
+    return weights_shape(desc, q_dtype, num_tokens, batch, num_q_heads, max_context, last, e) == UQ_OK ? e.workspace : 0;
+}
+
+uq_status uq_token_weights(const uq_cache_desc* desc, const void* q, uq_dtype q_dtype, int64_t q_stride,
+                           int64_t num_tokens, const int32_t* cu_seqlens, int32_t batch, int32_t num_q_heads,
+                           const uint8_t* kv_codes, const uint8_t* kv_scales, const int32_t* page_table,
+                           int32_t max_pages_per_seq, const int32_t* context_lens, int32_t max_context, int32_t last,
+                           int32_t causal, float softmax_scale, float* weights, int64_t weights_width, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    WeightsShape e;
+    uq_status s = weights_shape(desc, q_dtype, num_tokens, batch, num_q_heads, max_context, last, e);
+    if (s != UQ_OK) return s;
+    if (!(isfinite(softmax_scale) && softmax_scale > 0.0f)) return UQ_ERR_INVALID_ARGUMENT;
+    if (weights_width < max_context) return UQ_ERR_INVALID_ARGUMENT;
+    if (num_tokens == 0 || batch == 0 || max_context == 0) return UQ_OK;
+    if (q == nullptr || cu_seqlens == nullptr || kv_codes == nullptr || kv_scales == nullptr || page_table == nullptr ||
+        context_lens == nullptr || weights == nullptr || workspace == nullptr)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (max_pages_per_seq < 1 || int64_t(max_context) > int64_t(max_pages_per_seq) * kPageSize)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (!aligned16(q) || !aligned16(kv_codes) || !aligned16(kv_scales) || !aligned16(workspace)) return UQ_ERR_INVALID_ARGUMENT;
+    const int64_t vec = q_dtype == UQ_F32 ? 4 : q_dtype == UQ_FP8_E4M3 ? 16 : 8;   // elements of 16 bytes
+    if (q_stride < int64_t(num_q_heads) * desc->head_dim || q_stride % vec != 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < e.workspace) return UQ_ERR_WORKSPACE_TOO_SMALL;
+    const size_t item = q_dtype == UQ_F32 ? 4 : q_dtype == UQ_FP8_E4M3 ? 1 : 2, word = sizeof(int32_t);
+    const std::initializer_list<Span> outs = {{weights, size_t(batch) * size_t(desc->num_kv_heads) * size_t(weights_width) * word}, {workspace, e.workspace}},
+                                      ins = {{q, (size_t(num_tokens - 1) * size_t(q_stride) + size_t(num_q_heads) * size_t(desc->head_dim)) * item},
+                        {cu_seqlens, (size_t(batch) + 1) * word}, {context_lens, size_t(batch) * word},
+                        {page_table, size_t(batch) * size_t(max_pages_per_seq) * word}, codes_span(desc, kv_codes), scales_span(desc, kv_scales)};
+    if (outputs_meet(outs, ins)) return UQ_ERR_INVALID_ARGUMENT;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    if (e.query > 0) {
+        // rows: rotated and cast as uq_norm_rope_write does without a norm and rotation
+        uq::NormRopeParams r;
+        const uq_norm_rope_desc none = {nullptr, nullptr, 0.0f, nullptr, nullptr, 0, 0, 0};
+        s = norm_rope_setup(&none, nullptr, desc->head_dim, q, q_stride, num_q_heads, q_dtype, num_tokens, ws, UQ_FP8_E4M3, r);
+        if (s != UQ_OK) return s;
+        r.num_kv_heads = 0;
+        const hipError_t h = uq::launch_norm_rope(r, nullptr, desc->head_dim, int(q_dtype), static_cast<hipStream_t>(stream));
+        if (h != hipSuccess) return from_hip(h);
+    }
+    uq::WeightsParams p;
+    p.q = e.query > 0 ? ws : static_cast<const uint8_t*>(q);
+    p.q_stride = e.query > 0 ? int64_t(num_q_heads) * desc->head_dim : q_stride;
+    p.num_tokens = int32_t(num_tokens);
+    p.cu_seqlens = cu_seqlens;
+    p.batch = batch;
+    p.num_kv_heads = desc->num_kv_heads;
+    p.group = num_q_heads / desc->num_kv_heads;
+    p.group_magic = uint32_t((uint64_t(1) << 32) / uint64_t(p.group)) + 1;
+    p.head_dim = desc->head_dim;
+    p.codes = kv_codes;
+    p.scales = kv_scales;
+    p.page_table = page_table;
+    p.max_pages_per_seq = max_pages_per_seq;
+    p.num_pages = desc->num_pages;
+    p.context_lens = context_lens;
+    p.max_context = max_context;
+    p.last = last;
+    p.causal = causal != 0;
+    p.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
+    p.weights = weights;
+    p.width = weights_width;
+    p.by_seq = e.by_seq;
+    p.rows_per_head = e.rows_per_head;
+    p.row_units = e.row_units;
+    p.chunk = e.chunk;
+    p.chunks = e.chunks;
+    p.key_units = e.key_units;
+    p.row_split = e.row_split;
+    p.splits = e.splits;
+    p.norm_blocks = e.norm_blocks;
+    p.sum_blocks = e.sum_blocks;
+    p.ref = reinterpret_cast<float*>(ws + e.query);
+    p.inv = reinterpret_cast<float*>(ws + e.query + e.rows);
+    p.parts = reinterpret_cast<float*>(ws + e.query + 2 * e.rows);
+    return from_hip(uq::launch_token_weights(p, static_cast<hipStream_t>(stream)));
+}
+
+// Sizes that uq_select_tokens and uq_compact_kv share.
+static uq_status check_kept(int32_t batch, int32_t num_kv_heads, int32_t budget) {
+    if (batch < 0 || num_kv_heads < 1 || budget < 1) return UQ_ERR_INVALID_ARGUMENT;
+    if (batch > 65535 || num_kv_heads > 65535 || int64_t(batch) * num_kv_heads >= kMaxBlocks / 4 || budget > (1 << 30))
+        return UQ_ERR_UNSUPPORTED;
+    return UQ_OK;
+}
+
+size_t uq_select_tokens_workspace_bytes(int32_t batch, int32_t num_kv_heads, int32_t max_context, int32_t budget) {
+    (void)batch, (void)num_kv_heads, (void)max_context, (void)budget;
+    return 0;
+}
+
+uq_status uq_select_tokens(const float* weights, int64_t weights_width, int32_t batch, int32_t num_kv_heads,
+                           const int32_t* context_lens, int32_t max_context, int32_t budget, int32_t sinks,
+                           int32_t recent, int32_t* kept, int32_t* kept_lens, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+    uq_status s = check_kept(batch, num_kv_heads, budget);
+    if (s != UQ_OK) return s;
+    if (max_context < 0 || sinks < 0 || recent < 0 || int64_t(sinks) + recent > budget || weights_width < max_context)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (max_context > (1 << 30)) return UQ_ERR_UNSUPPORTED;
+    if (batch == 0) return UQ_OK;
+    if ((weights == nullptr && max_context > budget) || context_lens == nullptr || kept == nullptr || kept_lens == nullptr)
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < uq_select_tokens_workspace_bytes(batch, num_kv_heads, max_context, budget)) return UQ_ERR_WORKSPACE_TOO_SMALL;
+    (void)workspace;
+    const size_t word = sizeof(int32_t), rows = size_t(batch) * size_t(num_kv_heads);
+    const std::initializer_list<Span> outs = {{kept, rows * size_t(budget) * word}, {kept_lens, size_t(batch) * word}},
+                                      ins = {{weights, rows * size_t(weights_width) * word}, {context_lens, size_t(batch) * word}};
+    if (outputs_meet(outs, ins)) return UQ_ERR_INVALID_ARGUMENT;
+    const uq::SelectParams p{weights, weights_width, batch, num_kv_heads, context_lens, max_context, budget, sinks, recent, kept, kept_lens};
+    return from_hip(uq::launch_select_tokens(p, static_cast<hipStream_t>(stream)));
+}
+
+size_t uq_compact_kv_workspace_bytes(const uq_cache_desc* desc, int32_t batch, int32_t budget) {
+    (void)desc, (void)batch, (void)budget;
+    return 0;
+}
+
+uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t budget, const int32_t* kept_lens,
+                        const int32_t* context_lens, int32_t batch, uint8_t* kv_codes, uint8_t* kv_scales,
+                        const int32_t* page_table, int32_t max_pages_per_seq, float* weights, int64_t weights_width,
+                        int32_t* freed_pages, int32_t* freed_count, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    uq_status s = check_desc(desc);
+    if (s == UQ_OK) s = check_kept(batch, desc->num_kv_heads, budget);
+    if (s != UQ_OK) return s;
+    if (max_pages_per_seq < 1 || weights_width < 0 || (freed_pages == nullptr) != (freed_count == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
+    if (max_pages_per_seq >= (1 << 27)) return UQ_ERR_UNSUPPORTED;
+    if (batch > 0 && (kept == nullptr || kept_lens == nullptr || context_lens == nullptr || kv_codes == nullptr ||
+                      kv_scales == nullptr || page_table == nullptr))
+        return UQ_ERR_INVALID_ARGUMENT;
+    if (!aligned16(kv_codes) || !aligned16(kv_scales)) return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < uq_compact_kv_workspace_bytes(desc, batch, budget)) return UQ_ERR_WORKSPACE_TOO_SMALL;
+    (void)workspace;
+    const size_t word = sizeof(int32_t), rows = size_t(batch) * size_t(desc->num_kv_heads), seqs = size_t(batch);
+    const std::initializer_list<Span> outs = {codes_span(desc, kv_codes), scales_span(desc, kv_scales), {weights, rows * size_t(weights_width) * word},
+                         {freed_pages, seqs * size_t(max_pages_per_seq) * word}, {freed_count, word}},
+                                      ins = {{kept, rows * size_t(budget) * word}, {kept_lens, seqs * word}, {context_lens, seqs * word},
+                        {page_table, seqs * size_t(max_pages_per_seq) * word}};
+    if (outputs_meet(outs, ins)) return UQ_ERR_INVALID_ARGUMENT;
+    if (batch == 0 && freed_count == nullptr) return UQ_OK;
+    const uq::CompactParams p{kv_codes, kv_scales, desc->num_pages, desc->head_dim, desc->num_kv_heads, batch, kept, budget, kept_lens,
+                              context_lens, page_table, max_pages_per_seq, weights, weights_width, freed_pages, freed_count};
+    return from_hip(uq::launch_compact_kv(p, static_cast<hipStream_t>(stream)));
 }
 
 // The tokens a window's walk can have at most: the sinks' pages, and the

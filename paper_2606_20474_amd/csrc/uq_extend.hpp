@@ -90,6 +90,9 @@ constexpr int kNoBase = -512;   // no exponent yet: every scale is above it
 // Tokens per tile: one 16-byte unit of K and one of V for each of 256 threads.
 template <int D> constexpr int extend_tile() { return 8192 / D; }
 
+// CROSS, below: the queries have no order and see their whole context
+// (uq_cross_attention); every row then stands at the last token.
+
 // Where a block's rows stand and which tiles they see.
 struct ExtendRows {
     int b;              // sequence
@@ -182,7 +185,7 @@ __device__ __forceinline__ bool extend_find(const ExtendParams& p, int at, Exten
 // of different sequences differ by the whole context, and a long one that starts
 // last leaves the others' CUs idle.  above(j): blocks that end at or past the j-th
 // 32nd; `at` falls into the largest j with more than `at` of them.
-template <int M>
+template <int M, bool CROSS>
 __device__ __forceinline__ bool extend_find_longest(const ExtendParams& p, int at, ExtendRows& r) {
     const int lane = threadIdx.x & 63;
     int first = 0, count = 0, n = 0;
@@ -208,6 +211,7 @@ __device__ __forceinline__ bool extend_find_longest(const ExtendParams& p, int a
     const int width = __builtin_amdgcn_readfirstlane(top) / 32 + 1;
     auto above = [&](int j) {
         const int64_t from = int64_t(j) * width;
+        if (CROSS) return j == 0 || from < n ? blocks : 0;
         if (j == 0 || from <= start) return blocks;
         return from >= n ? 0 : blocks - int((from - start) * p.group / M);
     };
@@ -236,11 +240,11 @@ __device__ __forceinline__ bool extend_find_longest(const ExtendParams& p, int a
 }
 
 // Block `at` where every row block has p.splits of them.
-template <int M>
+template <int M, bool CROSS>
 __device__ __forceinline__ bool extend_find_split(const ExtendParams& p, int at, ExtendRows& r) {
     r.split = at % p.splits;
     r.share = 0;
-    return p.longest_first ? extend_find_longest<M>(p, at / p.splits, r) : extend_find<M>(p, at / p.splits, r);
+    return p.longest_first ? extend_find_longest<M, CROSS>(p, at / p.splits, r) : extend_find<M>(p, at / p.splits, r);
 }
 
 // Row block and split `at` of a batch (at most 64 sequences, one per lane, no
@@ -303,8 +307,12 @@ __device__ __forceinline__ bool extend_find_share(const ExtendParams& p, int at,
 }
 
 // Positions of a row block's first and last row.
-template <int M>
+template <int M, bool CROSS>
 __device__ __forceinline__ void extend_span(const ExtendParams& p, const ExtendRows& r, int& lo, int& hi) {
+    if constexpr (CROSS) {
+        lo = hi = r.n_ctx - 1;
+        return;
+    }
     const int last = r.row0 + M < r.count * p.group ? r.row0 + M - 1 : r.count * p.group - 1;
     lo = r.n_ctx - r.count + r.row0 / p.group;
     hi = r.n_ctx - r.count + last / p.group;
@@ -470,7 +478,7 @@ template <int D, int W, bool ALONE> struct ExtendShape {
 // K and of V: loaded into registers while the tile before is computed (the page ids
 // one tile earlier still), stored to LDS after it, K as it is and V decoded.  Two
 // buffers and one barrier per tile; a wave alone needs one buffer and none.
-template <int D, int NQ, int W, bool ALONE>
+template <int D, int NQ, int W, bool ALONE, bool CROSS>
 __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r, int hk, uint8_t* smem) {
     using Shape = ExtendShape<D, W, ALONE>;
     constexpr int TT = Shape::TT, CB = Shape::CB, kVRow = Shape::kVRow, kVOctet = Shape::kVOctet;
@@ -507,7 +515,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     };
 
     int lo, hi;
-    extend_span<M>(p, r, lo, hi);
+    extend_span<M, CROSS>(p, r, lo, hi);
     extend_tiles<TT>(p, lo, hi, r);
     int first_tile = 0, last_tile = r.tiles;
     bool whole = true;
@@ -550,7 +558,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
     // the wave's first and last position (a wave without rows only moves tiles)
     const bool busy = w_row0 < rows;
     const int w_last = w_row0 + 32 * NQ < rows ? w_row0 + 32 * NQ - 1 : rows - 1;
-    const int w_lo = r.n_ctx - r.count + w_row0 / p.group, w_hi = r.n_ctx - r.count + w_last / p.group;
+    const int w_lo = CROSS ? hi : r.n_ctx - r.count + w_row0 / p.group, w_hi = CROSS ? hi : r.n_ctx - r.count + w_last / p.group;
 
     const int32_t* pt_row = p.page_table + int64_t(r.b) * p.max_pages_per_seq;
     const int n_pages = (hi + kPage) / kPage;   // pages up to the last that holds a visible token
@@ -799,7 +807,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
                         // element i: token 8 (i / 4) + 4 half + i % 4 of the 32; it is seen when 0 <=
                         // position - token < window, or among the first tokens
                         const int tok = tok0 + 32 * tb + 4 * int(lh), row = w_row0 + 32 * q + int(lc);
-                        const int pos = row < rows ? r.n_ctx - r.count + div_group(p, row) : -1;
+                        const int pos = row >= rows ? -1 : CROSS ? r.n_ctx - 1 : r.n_ctx - r.count + div_group(p, row);
                         const unsigned reach = p.window > 0 ? unsigned(p.window) : 0x80000000u;
                         const int sinks = pos + 1 < p.sinks ? pos + 1 : p.sinks;
 #pragma unroll
@@ -1048,7 +1056,7 @@ __device__ __forceinline__ void extend_walk(const ExtendParams& p, ExtendRows r,
 // MIXED: sequences with up to p.alone_rows rows of a KV head are walked by waves that
 // split the tokens.  (Both walks in one kernel cost the other some registers, so it
 // is a kernel of its own.)
-template <int D, int NQ, int W, bool MIXED>
+template <int D, int NQ, int W, bool MIXED, bool CROSS>
 __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
     constexpr int kTogetherLds = ExtendShape<D, W, false>::kLds, kAloneLds = MIXED ? ExtendShape<D, W, true>::kLds : 0;
     __shared__ __attribute__((aligned(16))) uint8_t smem[kTogetherLds > kAloneLds ? kTogetherLds : kAloneLds];
@@ -1061,22 +1069,22 @@ __global__ void __launch_bounds__(64 * W, 2) extend_kernel(ExtendParams p) {
             const bool found = extend_find_share<M, extend_tile<D>(), ExtendShape<D, W, true>::TT>(p, rest, r);
             if (blockIdx.x == 0 && threadIdx.x == 0) *p.share = r.share;   // for the join
             if (!found) return;
-        } else if (!extend_find_split<M>(p, rest, r)) {
+        } else if (!extend_find_split<M, CROSS>(p, rest, r)) {
             return;
         }
         if (r.count * p.group <= p.alone_rows) {
-            extend_walk<D, 2, W, true>(p, r, hk, smem);
+            extend_walk<D, 2, W, true, CROSS>(p, r, hk, smem);
             return;
         }
-    } else if (!extend_find_split<M>(p, rest, r)) {
+    } else if (!extend_find_split<M, CROSS>(p, rest, r)) {
         return;
     }
-    extend_walk<D, NQ, W, false>(p, r, hk, smem);
+    extend_walk<D, NQ, W, false, CROSS>(p, r, hk, smem);
 }
 
 // Joins the partials of every (token, query head): 16 lanes per row, N channels
 // each.
-template <int D, int M>
+template <int D, int M, bool CROSS>
 __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     constexpr int N = D / 16;
     const int L = threadIdx.x & 15;
@@ -1098,7 +1106,7 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     r.n_ctx = extend_context(p, lo);
     r.row0 = ((t - r.first) * p.group + hq % p.group) / M * M;
     int plo, phi;
-    extend_span<M>(p, r, plo, phi);
+    extend_span<M, CROSS>(p, r, plo, phi);
     constexpr int TT = extend_tile<D>(), TA = ExtendShape<D, 4, true>::TT;
     const int share = p.share != nullptr ? *p.share : 0;
     int per;
@@ -1145,18 +1153,18 @@ __global__ void __launch_bounds__(256) extend_merge_kernel(ExtendParams p) {
     }
 }
 
-template <int D, int NQ, int W>
+template <int D, int NQ, int W, bool CROSS>
 static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) {
     const dim3 grid{unsigned(int64_t(p.row_blocks) * p.num_kv_heads * (p.share != nullptr ? 1 : p.splits))}, block{64u * W};
     if (p.alone_rows > 0) {
-        if constexpr (D <= 128) launch_kernel(extend_kernel<D, NQ, W, true>, grid, block, stream, p);
+        if constexpr (D <= 128) launch_kernel(extend_kernel<D, NQ, W, true, CROSS>, grid, block, stream, p);
         else return hipErrorInvalidValue;   // (not asked for)
     } else {
-        launch_kernel(extend_kernel<D, NQ, W, false>, grid, block, stream, p);
+        launch_kernel(extend_kernel<D, NQ, W, false, CROSS>, grid, block, stream, p);
     }
     if (p.splits > 1) {
         const int64_t rows = int64_t(p.num_tokens) * p.num_q_heads;
-        hipLaunchKernelGGL((extend_merge_kernel<D, 32 * NQ * W>), dim3(unsigned((rows + 15) / 16)), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((extend_merge_kernel<D, 32 * NQ * W, CROSS>), dim3(unsigned((rows + 15) / 16)), dim3(256), 0, stream, p);
     }
     return hipGetLastError();
 }
@@ -1164,10 +1172,15 @@ static hipError_t launch_extend_with(const ExtendParams& p, hipStream_t stream) 
 int extend_block_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 int extend_alone_rows(int head_dim) { return head_dim == 256 ? 0 : 64; }
 
+template <bool CROSS>
+static hipError_t launch_extend_as(const ExtendParams& p, hipStream_t stream) {
+    if (p.head_dim == 64) return launch_extend_with<64, 2, 4, CROSS>(p, stream);
+    if (p.head_dim == 128) return launch_extend_with<128, 2, 4, CROSS>(p, stream);
+    return launch_extend_with<256, 1, 4, CROSS>(p, stream);
+}
+
 hipError_t launch_extend(const ExtendParams& p, hipStream_t stream) {
-    if (p.head_dim == 64) return launch_extend_with<64, 2, 4>(p, stream);
-    if (p.head_dim == 128) return launch_extend_with<128, 2, 4>(p, stream);
-    return launch_extend_with<256, 1, 4>(p, stream);
+    return p.cross ? launch_extend_as<true>(p, stream) : launch_extend_as<false>(p, stream);
 }
 
 }  // namespace uq

@@ -189,6 +189,7 @@ struct ExtendParams {
     int32_t max_context;
     int32_t window;            // 0: causal over the whole context
     int32_t sinks;
+    int32_t cross;             // every query sees the whole context (window 0)
     float scale_log2;          // softmax_scale * log2(e)
     int32_t rotate_v;
     int32_t row_blocks;        // bound of the batch's row blocks per KV head (with share: blocks per KV head)
@@ -208,6 +209,80 @@ int extend_block_rows(int head_dim);
 // leave a CU one block).
 int extend_alone_rows(int head_dim);
 hipError_t launch_extend(const ExtendParams& p, hipStream_t stream);
+
+// uq_token_weights (uq_weights.hpp)
+struct WeightsParams {
+    const uint8_t* q;          // prepared FP8 rows [T][Hq][d], token stride q_stride
+    int64_t q_stride;
+    int32_t num_tokens;
+    const int32_t* cu_seqlens;
+    int32_t batch;
+    int32_t num_kv_heads;
+    int32_t group;
+    uint32_t group_magic;      // as in ExtendParams
+    int32_t head_dim;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const int32_t* page_table;
+    int32_t max_pages_per_seq;
+    int64_t num_pages;
+    const int32_t* context_lens;
+    int32_t max_context;
+    int32_t last;              // queries of a sequence that count, its last ones (0: all)
+    int32_t causal;
+    float scale_log2;
+    float* weights;            // [batch][Hkv][width]
+    int64_t width;
+    int32_t by_seq;            // rows are numbered by sequence, `last` queries each (else by token row)
+    int64_t rows_per_head;     // of that numbering
+    int32_t row_units;         // 16-row units a wave of the norms holds
+    int32_t chunk;             // tokens a wave of the norms walks
+    int32_t chunks;            // of the longest context
+    int32_t key_units;         // key units a wave of the sums holds
+    int32_t row_split;         // rows a wave of the sums walks, a multiple of 16
+    int32_t splits;            // of a sequence with the most rows
+    int32_t norm_blocks;
+    int32_t sum_blocks;
+    float* ref;                // [Hkv][rows_per_head] reference and 1 / sum of every row
+    float* inv;
+    float* parts;              // [chunks][Hkv][rows_per_head][2], then [splits][batch][Hkv][max_context]
+};
+hipError_t launch_token_weights(const WeightsParams& p, hipStream_t stream);
+
+struct SelectParams {
+    const float* weights;      // [batch][heads][width]
+    int64_t width;
+    int32_t batch;
+    int32_t heads;
+    const int32_t* context_lens;
+    int32_t max_context;
+    int32_t budget;
+    int32_t sinks;
+    int32_t recent;
+    int32_t* kept;             // [batch][heads][budget]
+    int32_t* kept_lens;        // [batch]
+};
+hipError_t launch_select_tokens(const SelectParams& p, hipStream_t stream);
+
+struct CompactParams {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t num_pages;
+    int32_t head_dim;
+    int32_t heads;
+    int32_t batch;
+    const int32_t* kept;       // [batch][heads][budget]
+    int32_t budget;
+    const int32_t* kept_lens;
+    const int32_t* context_lens;
+    const int32_t* page_table;
+    int32_t max_pages_per_seq;
+    float* weights;            // [batch][heads][width] or nullptr
+    int64_t width;
+    int32_t* freed_pages;      // nullptr: not wanted
+    int32_t* freed_count;
+};
+hipError_t launch_compact_kv(const CompactParams& p, hipStream_t stream);
 
 struct PlanParams {
     int32_t batch;
@@ -246,6 +321,12 @@ struct NormRopeParams {
     void* k_out;               // without a cache
     int32_t out_dtype;         // 0 f32, 1 bf16, 2 f16, 3 fp8 (queries, with a cache)
     uint32_t q_blocks;         // blocks of the queries (set by the launcher)
+    // positions with several axes (0: one position per token): axis a of token t at
+    // positions[a * axis_stride + t], and 2 bits per pair that name its axis
+    int32_t num_axes;
+    int64_t axis_stride;
+    int32_t axis_unit;         // aligned pairs that share an axis: 8, 4, or 1 (no rule)
+    uint32_t axis_of[8];
 };
 
 hipError_t launch_quantize_kv(const QuantizeParams& p, int dtype, hipStream_t stream);

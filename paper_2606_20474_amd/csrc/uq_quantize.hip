@@ -522,5 +522,7 @@ hipError_t launch_prepare_query(const void* q, int dtype, int64_t rows, uint8_t*
 
 }  // namespace uq
 
+#include "uq_evict.hpp"
 #include "uq_plan.hpp"
 #include "uq_rows.hpp"
+#include "uq_weights.hpp"

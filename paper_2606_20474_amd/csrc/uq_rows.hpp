@@ -43,15 +43,85 @@ __device__ __forceinline__ void rotate_pair(float& a, float& b, float c, float s
     a = ya;
 }
 
+// The angles of a token: N consecutive pairs from `pair` on.  A token with one
+// position: one row of the table, rot / 2 cosines, then the sines.
+struct RowAngles {
+    const float* cs;
+    int half;
+    __device__ __forceinline__ uint32_t map(int, bool, int) const { return 0; }
+    template <int N> __device__ __forceinline__ void load(int pair, uint32_t, float (&c)[N], float (&s)[N]) const {
+        if constexpr (N == 8) {
+            load_x8<0>(cs, pair, c);
+            load_x8<0>(cs, half + pair, s);
+        } else {
+            load_x4<0>(cs, pair, c);
+            load_x4<0>(cs, half + pair, s);
+        }
+    }
+};
+
+// A token with a position on every axis: a row of the table for each, and 2 bits per
+// pair that say which.  Where 8 or 4 aligned pairs share an axis (p.axis_unit) they are
+// loaded together.
+struct AxisAngles {
+    const NormRopeParams& p;
+    int64_t at[4];   // the axes' rows
+    __device__ __forceinline__ AxisAngles(const NormRopeParams& q, int64_t t) : p(q) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            int pos = q.positions[(a < q.num_axes ? a : 0) * q.axis_stride + t];
+            pos = pos < 0 ? 0 : pos < q.max_position ? pos : q.max_position - 1;
+            at[a] = int64_t(pos) * q.rot;
+        }
+    }
+    // the axes of 16 pairs from 16 w (or, with `next`, 16 w + 16) on, shifted
+    __device__ __forceinline__ uint32_t map(int w, bool next, int shift) const {
+        return (next ? p.axis_of[w + 1] : p.axis_of[w]) >> shift;
+    }
+    __device__ __forceinline__ const float* row(uint32_t axis) const {
+        const int64_t lo = axis & 1u ? at[1] : at[0], hi = axis & 1u ? at[3] : at[2];
+        return p.cos_sin + (axis & 2u ? hi : lo);
+    }
+    template <int N> __device__ __forceinline__ void load(int pair, uint32_t axes, float (&c)[N], float (&s)[N]) const {
+        const int half = p.rot / 2;
+        if (N == 8 && p.axis_unit == 8) {
+            const float* r = row(axes);
+            if constexpr (N == 8) {
+                load_x8<0>(r, pair, c);
+                load_x8<0>(r, half + pair, s);
+            }
+        } else if (p.axis_unit >= 4) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                const float* r = row(axes >> (2 * k));
+                float x[4], y[4];
+                load_x4<0>(r, pair + k, x);
+                load_x4<0>(r, half + pair + k, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    c[k + i] = x[i];
+                    s[k + i] = y[i];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float* r = row(axes >> (2 * i));
+                c[i] = r[pair + i];
+                s[i] = r[half + pair + i];
+            }
+        }
+    }
+};
+
 // Pairs (c, c + 32 H), c < 32 H: both in this lane.
-template <int NG, int H>
-__device__ __forceinline__ void rope_in_lane(float (&x)[NG][8], const float* cs, int L) {
+template <int NG, int H, class ANGLES>
+__device__ __forceinline__ void rope_in_lane(float (&x)[NG][8], const ANGLES& ang, int L) {
     if constexpr (2 * H <= NG) {
 #pragma unroll
         for (int j = 0; j < H; ++j) {
             float c[8], s[8];
-            load_x8<0>(cs, 32 * j + 8 * L, c);
-            load_x8<0>(cs, 32 * H + 32 * j + 8 * L, s);
+            ang.load(32 * j + 8 * L, ang.map(2 * j, (L & 2) != 0, 16 * (L & 1)), c, s);
 #pragma unroll
             for (int i = 0; i < 8; ++i) rotate_pair(x[j][i], x[j + H][i], c[i], s[i]);
         }
@@ -60,11 +130,10 @@ __device__ __forceinline__ void rope_in_lane(float (&x)[NG][8], const float* cs,
 
 // Pairs (c, c + 8 S), c < 8 S, S 1 or 2: lanes L and L ^ S of the quad, in
 // x[0]; with S = 1 only lanes 0 and 1 take part.  The whole quad executes this.
-template <int S, int NG>
-__device__ __forceinline__ void rope_across(float (&x)[NG][8], const float* cs, int L) {
+template <int S, int NG, class ANGLES>
+__device__ __forceinline__ void rope_across(float (&x)[NG][8], const ANGLES& ang, int L) {
     float c[8], s[8];
-    load_x8<0>(cs, 8 * (L & (S - 1)), c);
-    load_x8<0>(cs, 8 * S + 8 * (L & (S - 1)), s);
+    ang.load(8 * (L & (S - 1)), ang.map(0, false, 16 * (L & (S - 1))), c, s);
     const bool upper = (L & S) != 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -75,29 +144,27 @@ __device__ __forceinline__ void rope_across(float (&x)[NG][8], const float* cs, 
     }
 }
 
-// cs: the position's row of the table, rot / 2 cosines, then the sines.
-template <int NG>
-__device__ __forceinline__ void rope_quad(float (&x)[NG][8], const float* cs, int rot, bool interleaved, int L) {
+template <int NG, class ANGLES>
+__device__ __forceinline__ void rope_quad(float (&x)[NG][8], const ANGLES& ang, int rot, bool interleaved, int L) {
     if (interleaved) {
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
             const int c0 = 32 * j + 8 * L;   // this lane's 8 channels, 4 pairs (rot is a multiple of 8)
             if (c0 < rot) {
                 float c[4], s[4];
-                load_x4<0>(cs, c0 / 2, c);
-                load_x4<0>(cs, rot / 2 + c0 / 2, s);
+                ang.load(c0 / 2, ang.map(j, false, 8 * L), c, s);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) rotate_pair(x[j][2 * i], x[j][2 * i + 1], c[i], s[i]);
             }
         }
         return;
     }
-    if (rot == 64) rope_in_lane<NG, 1>(x, cs, L);
-    else if (rot == 128) rope_in_lane<NG, 2>(x, cs, L);
-    else if (rot == 192) rope_in_lane<NG, 3>(x, cs, L);
-    else if (rot == 256) rope_in_lane<NG, 4>(x, cs, L);
-    else if (rot == 32) rope_across<2, NG>(x, cs, L);
-    else if (rot == 16) rope_across<1, NG>(x, cs, L);
+    if (rot == 64) rope_in_lane<NG, 1>(x, ang, L);
+    else if (rot == 128) rope_in_lane<NG, 2>(x, ang, L);
+    else if (rot == 192) rope_in_lane<NG, 3>(x, ang, L);
+    else if (rot == 256) rope_in_lane<NG, 4>(x, ang, L);
+    else if (rot == 32) rope_across<2, NG>(x, ang, L);
+    else if (rot == 16) rope_across<1, NG>(x, ang, L);
 }
 
 // Eight fp32 values as elements e .. e + 7 of a buffer of dtype DT (0 f32, 1
@@ -125,14 +192,16 @@ __device__ __forceinline__ void store_x8(void* base, int64_t elem, int dt, const
 }
 
 // Norm and rotation of the vector a quad holds (token t, weight w or nullptr).
-template <int NG>
+template <int NG, bool AXES>
 __device__ __forceinline__ void norm_rope_quad(float (&x)[NG][8], const NormRopeParams& p, int64_t t, const float* w,
                                                int L) {
     if (w != nullptr) norm_quad<NG>(x, w, p.eps, L);
-    if (p.rot > 0) {
+    if constexpr (AXES) {
+        rope_quad<NG>(x, AxisAngles(p, t), p.rot, p.interleaved != 0, L);
+    } else if (p.rot > 0) {
         int pos = p.positions[t];
         pos = pos < 0 ? 0 : pos < p.max_position ? pos : p.max_position - 1;
-        rope_quad<NG>(x, p.cos_sin + int64_t(pos) * p.rot, p.rot, p.interleaved != 0, L);
+        rope_quad<NG>(x, RowAngles{p.cos_sin + int64_t(pos) * p.rot, p.rot / 2}, p.rot, p.interleaved != 0, L);
     }
 }
 
@@ -151,7 +220,7 @@ __device__ __forceinline__ void norm_rope_quad(float (&x)[NG][8], const NormRope
 // after K is done with them (130 us with both at once; five waves' worth of spills
 // are none); several heads per quad, the weights and angles loaded once for all,
 // gave 126 us.
-template <int DT, int NG, bool WRITE>
+template <int DT, int NG, bool WRITE, bool AXES>
 __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRopeParams p, QuantizeParams c) {
     constexpr int D = 32 * NG;
     const int L = threadIdx.x & 3;
@@ -166,7 +235,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         const int64_t row = int64_t(t) * (isk ? p.k_stride : p.q_stride) + int64_t(h) * D + 8 * L;
 #pragma unroll
         for (int j = 0; j < NG; ++j) load_x8<DT>(isk ? p.k : p.q, row + 32 * j, x[j]);
-        norm_rope_quad<NG>(x, p, t, isk ? p.k_weight : p.q_weight, L);
+        norm_rope_quad<NG, AXES>(x, p, t, isk ? p.k_weight : p.q_weight, L);
         const int64_t out = int64_t(vec) * D + 8 * L;
         if (p.out_dtype == 3) {
             wht_quad<NG>(x, L);
@@ -194,7 +263,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         int off;
         const bool valid = page_of_slot(c, slot, page, off);
         if (!valid) return;
-        norm_rope_quad<NG>(x, p, t, p.k_weight, L);
+        norm_rope_quad<NG, AXES>(x, p, t, p.k_weight, L);
         const int64_t ph = page * c.num_kv_heads + h;
         uint8_t* kc = c.codes + ph * (16 * D);
         uint8_t* ks = c.scales + ph * D;
@@ -202,7 +271,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         quantize_xq<NG>(x, L, c.c, true, w, b, [&](float (&y)[NG][8]) {
 #pragma unroll
             for (int j = 0; j < NG; ++j) load_x8<DT>(c.k, row + 32 * j, y[j]);
-            norm_rope_quad<NG>(y, p, t, p.k_weight, L);
+            norm_rope_quad<NG, AXES>(y, p, t, p.k_weight, L);
         });
         store_k_quad<NG>(kc, ks, off, L, w, b);
 #pragma unroll
@@ -267,13 +336,20 @@ __global__ void __launch_bounds__(256) read_kv_kernel(QuantizeParams c, void* k_
 
 static int64_t kv_units(const QuantizeParams& c) { return (c.num_tokens + 15) / 16 * c.num_kv_heads; }
 
-template <int NG, bool WRITE>
+template <int NG, bool WRITE, bool AXES>
 static void launch_norm_rope_ng(const NormRopeParams& p, const QuantizeParams& c, int dtype, unsigned blocks,
                                 hipStream_t stream) {
     const dim3 grid{blocks}, block{256u};
-    if (dtype == 0) hipLaunchKernelGGL((norm_rope_kernel<0, NG, WRITE>), grid, block, 0, stream, p, c);
-    else if (dtype == 1) hipLaunchKernelGGL((norm_rope_kernel<1, NG, WRITE>), grid, block, 0, stream, p, c);
-    else hipLaunchKernelGGL((norm_rope_kernel<2, NG, WRITE>), grid, block, 0, stream, p, c);
+    if (dtype == 0) hipLaunchKernelGGL((norm_rope_kernel<0, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
+    else if (dtype == 1) hipLaunchKernelGGL((norm_rope_kernel<1, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
+    else hipLaunchKernelGGL((norm_rope_kernel<2, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
+}
+template <bool WRITE, bool AXES>
+static void launch_norm_rope_as(const NormRopeParams& p, const QuantizeParams& c, int head_dim, int dtype, unsigned blocks,
+                                hipStream_t stream) {
+    if (head_dim == 64) launch_norm_rope_ng<2, WRITE, AXES>(p, c, dtype, blocks, stream);
+    else if (head_dim == 128) launch_norm_rope_ng<4, WRITE, AXES>(p, c, dtype, blocks, stream);
+    else launch_norm_rope_ng<8, WRITE, AXES>(p, c, dtype, blocks, stream);
 }
 
 hipError_t launch_norm_rope(NormRopeParams p, const QuantizeParams* c, int head_dim, int dtype, hipStream_t stream) {
@@ -284,13 +360,11 @@ hipError_t launch_norm_rope(NormRopeParams p, const QuantizeParams* c, int head_
     const unsigned blocks = unsigned(qb + kb);
     const QuantizeParams none{};
     if (c != nullptr) {
-        if (head_dim == 64) launch_norm_rope_ng<2, true>(p, *c, dtype, blocks, stream);
-        else if (head_dim == 128) launch_norm_rope_ng<4, true>(p, *c, dtype, blocks, stream);
-        else launch_norm_rope_ng<8, true>(p, *c, dtype, blocks, stream);
+        if (p.num_axes > 0) launch_norm_rope_as<true, true>(p, *c, head_dim, dtype, blocks, stream);
+        else launch_norm_rope_as<true, false>(p, *c, head_dim, dtype, blocks, stream);
     } else {
-        if (head_dim == 64) launch_norm_rope_ng<2, false>(p, none, dtype, blocks, stream);
-        else if (head_dim == 128) launch_norm_rope_ng<4, false>(p, none, dtype, blocks, stream);
-        else launch_norm_rope_ng<8, false>(p, none, dtype, blocks, stream);
+        if (p.num_axes > 0) launch_norm_rope_as<false, true>(p, none, head_dim, dtype, blocks, stream);
+        else launch_norm_rope_as<false, false>(p, none, head_dim, dtype, blocks, stream);
     }
     return hipGetLastError();
 }

@@ -44,6 +44,9 @@ EXPORTS = (
     "uq_decode_attention_noalloc", "uq_decode_attention_scaled_pv", "uq_probe_stream_read", "uq_probe_page_gather",
     "uq_probe_page_gather_cascade", "uq_probe_mfma", "uq_plan_tokens", "uq_norm_rope", "uq_norm_rope_write", "uq_read_kv",
     "uq_extend_workspace_bytes", "uq_extend_attention", "uq_decode_window_workspace_bytes", "uq_decode_window",
+    "uq_norm_rope_axes", "uq_norm_rope_axes_write", "uq_cross_workspace_bytes", "uq_cross_attention",
+    "uq_token_weights_workspace_bytes", "uq_token_weights", "uq_select_tokens_workspace_bytes", "uq_select_tokens",
+    "uq_compact_kv_workspace_bytes", "uq_compact_kv",
 )
 
 UQ_REF_FP8_E4M3, UQ_REF_BF16, UQ_REF_TQ4 = 1, 2, 3
@@ -99,6 +102,14 @@ class uq_norm_rope_desc(ctypes.Structure):
         ("max_position", ctypes.c_int32),
         ("rot_dim", ctypes.c_int32),
         ("interleaved", ctypes.c_int32),
+    ]
+
+
+class uq_rope_axes(ctypes.Structure):
+    _fields_ = [
+        ("num_axes", ctypes.c_int32),
+        ("position_stride", ctypes.c_int64),
+        ("pair_axes", ctypes.c_char_p),
     ]
 
 
@@ -197,6 +208,28 @@ def _load():
     L.uq_decode_window.argtypes = [D, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, f32, i32, vp,
                                    sz, vp, i32, vp]
     L.uq_decode_window.restype = i32
+    A = ctypes.POINTER(uq_rope_axes)
+    L.uq_norm_rope_axes.argtypes = [N, A] + L.uq_norm_rope.argtypes[1:]
+    L.uq_norm_rope_axes.restype = i32
+    L.uq_norm_rope_axes_write.argtypes = [D, N, A] + L.uq_norm_rope_write.argtypes[2:]
+    L.uq_norm_rope_axes_write.restype = i32
+    L.uq_cross_workspace_bytes.argtypes = [D, i64, i32, i32, i32]
+    L.uq_cross_workspace_bytes.restype = sz
+    L.uq_cross_attention.argtypes = [D, vp, i32, i64, i64, vp, i32, i32, vp, vp, vp, i32, vp, i32, f32, vp, sz, vp, i32, vp]
+    L.uq_cross_attention.restype = i32
+    L.uq_token_weights_workspace_bytes.argtypes = [D, i32, i64, i32, i32, i32, i32]
+    L.uq_token_weights_workspace_bytes.restype = sz
+    L.uq_token_weights.argtypes = [D, vp, i32, i64, i64, vp, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, f32, vp, i64,
+                                   vp, sz, vp]
+    L.uq_token_weights.restype = i32
+    L.uq_select_tokens_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.uq_select_tokens_workspace_bytes.restype = sz
+    L.uq_select_tokens.argtypes = [vp, i64, i32, i32, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    L.uq_select_tokens.restype = i32
+    L.uq_compact_kv_workspace_bytes.argtypes = [D, i32, i32]
+    L.uq_compact_kv_workspace_bytes.restype = sz
+    L.uq_compact_kv.argtypes = [D, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, i64, vp, vp, vp, sz, vp]
+    L.uq_compact_kv.restype = i32
     return L
 
 
@@ -640,26 +673,52 @@ def plan_tokens(cached_lens, new_lens, free_pages, page_table, plan: TokenPlan, 
 class NormRope:
     """Mirror of ``uq_norm_rope_desc``: `positions` int32 [T], `cos_sin`
     float32 [max_position, rot_dim] (cosines, then sines; None: no rotation),
-    weights float32 [head_dim] or None (no norm)."""
+    weights float32 [head_dim] or None (no norm).  With `pair_axes`, the axis
+    of each of the rot_dim / 2 pairs (``pair_axes_of``), `positions` is [axes, T]
+    (``uq_rope_axes``)."""
     positions: torch.Tensor = None
     cos_sin: torch.Tensor = None
     q_weight: torch.Tensor = None
     k_weight: torch.Tensor = None
     eps: float = 1e-6
     interleaved: bool = False
+    pair_axes: object = None
 
     def c_struct(self, num_tokens, head_dim):
         rot = 0
         if self.cos_sin is not None:
             _need(self.cos_sin, "cos_sin", (torch.float32,), (None, None))
-            _need(self.positions, "positions", _I32, (num_tokens,))
+            _need(self.positions, "positions", _I32, (num_tokens,) if self.pair_axes is None else (None, num_tokens))
             rot = self.cos_sin.shape[1]
+        elif self.pair_axes is not None:
+            raise ValueError("pair_axes: given without cos_sin")
         for w, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
             if w is not None:
                 _need(w, name, (torch.float32,), (head_dim,))
         return uq_norm_rope_desc(_ptr(self.q_weight), _ptr(self.k_weight), self.eps,
                                  _ptr(self.positions) if rot else None, _ptr(self.cos_sin),
                                  self.cos_sin.shape[0] if rot else 0, rot, int(bool(self.interleaved)))
+
+    def axes_struct(self):
+        """The ``uq_rope_axes`` of the spec, or None."""
+        if self.pair_axes is None:
+            return None
+        axes = bytes(self.pair_axes)
+        if len(axes) != self.cos_sin.shape[1] // 2:
+            raise ValueError(f"pair_axes: {len(axes)} axes, expected {self.cos_sin.shape[1] // 2}, one per rotated pair")
+        return uq_rope_axes(self.positions.shape[0], self.positions.shape[1], axes)
+
+
+def pair_axes_of(sections, in_turns=False):
+    """The axis of every rotated pair from the number of pairs of each axis: one
+    section after another, or `in_turns` axis a >= 1 at every pair a, a + n, a + 2 n ..
+    of n axes until its section is used up and axis 0 at all others."""
+    n, total = len(sections), sum(sections)
+    if not in_turns:
+        return tuple(a for a, size in enumerate(sections) for _ in range(size))
+    if any(a + n * (size - 1) >= total for a, size in enumerate(sections) if a and size):
+        raise ValueError(f"sections: {tuple(sections)} do not fit {total} pairs in turns")
+    return tuple(j % n if j // n < sections[j % n] else 0 for j in range(total))
 
 
 def _head_rows(t, name, dtypes, shape):
@@ -693,10 +752,13 @@ def norm_rope(spec: NormRope, q, k=None, q_out=None, k_out=None, out_dtype=None,
         _need(k_out, "k_out", (q_out.dtype,), (T, Hkv, d))
     elif k_out is not None:
         raise ValueError("k_out: given without k")
-    s = spec.c_struct(T, d)
-    st = lib.uq_norm_rope(ctypes.byref(s), d, _ptr(q), q_stride, Hq, _ptr(k), k_stride, Hkv, _DT[q.dtype], T,
-                          _ptr(q_out), _ptr(k_out), _DT[q_out.dtype], _stream(stream))
-    _check(st, "uq_norm_rope")
+    s, a = spec.c_struct(T, d), spec.axes_struct()
+    rest = (d, _ptr(q), q_stride, Hq, _ptr(k), k_stride, Hkv, _DT[q.dtype], T, _ptr(q_out), _ptr(k_out), _DT[q_out.dtype],
+            _stream(stream))
+    if a is None:
+        _check(lib.uq_norm_rope(ctypes.byref(s), *rest), "uq_norm_rope")
+    else:
+        _check(lib.uq_norm_rope_axes(ctypes.byref(s), ctypes.byref(a), *rest), "uq_norm_rope_axes")
     return q_out, k_out
 
 
@@ -719,11 +781,14 @@ def norm_rope_write(desc: CacheDesc, spec: NormRope, q, k, v, slot_mapping, code
         with _on(stream):
             q_out = torch.empty((T, Hq, d), dtype=q_out_dtype, device=q.device)
     _need(q_out, "q_out", _QUERY, (T, Hq, d))
-    s, c = spec.c_struct(T, d), desc.c_struct()
-    st = lib.uq_norm_rope_write(ctypes.byref(c), ctypes.byref(s), _ptr(q), q_stride, Hq, _ptr(k), _ptr(v), kv_stride,
-                                _DT[q.dtype], T, _ptr(q_out), _DT[q_out.dtype], _ptr(page_table), num_seqs, mpps,
-                                _ptr(slot_mapping), _ptr(codes), _ptr(scales), _stream(stream))
-    _check(st, "uq_norm_rope_write")
+    s, c, a = spec.c_struct(T, d), desc.c_struct(), spec.axes_struct()
+    rest = (_ptr(q), q_stride, Hq, _ptr(k), _ptr(v), kv_stride, _DT[q.dtype], T, _ptr(q_out), _DT[q_out.dtype],
+            _ptr(page_table), num_seqs, mpps, _ptr(slot_mapping), _ptr(codes), _ptr(scales), _stream(stream))
+    if a is None:
+        _check(lib.uq_norm_rope_write(ctypes.byref(c), ctypes.byref(s), *rest), "uq_norm_rope_write")
+    else:
+        _check(lib.uq_norm_rope_axes_write(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), *rest),
+               "uq_norm_rope_axes_write")
     return q_out
 
 
@@ -793,6 +858,150 @@ def extend_attention(desc: CacheDesc, q, cu_seqlens, codes, scales, page_table, 
                                  _ptr(out), _DT[out.dtype], _stream(stream))
     _check(st, "uq_extend_attention")
     return out
+
+
+def cross_workspace_bytes(desc: CacheDesc, num_tokens, batch, num_q_heads, max_context):
+    """Bytes that cross_attention needs for these very arguments
+    (extend_workspace_bound is enough for every call)."""
+    d = desc.c_struct()
+    return int(lib.uq_cross_workspace_bytes(ctypes.byref(d), num_tokens, batch, num_q_heads, max_context))
+
+
+def cross_attention(desc: CacheDesc, q, cu_seqlens, codes, scales, page_table, context_lens, max_context,
+                    softmax_scale=None, workspace=None, out=None, out_dtype=torch.bfloat16, stream=None):
+    """Attention of the rows q [T, Hq, d] (or prepared FP8 bytes) to all cached
+    tokens of their sequence, such as an encoder's states -> out [T, Hq, d].
+    cu_seqlens int32 [batch + 1]; query and context lengths are independent."""
+    q_stride = _head_rows(q, "q", _QUERY, (None, None, desc.head_dim))
+    T, Hq = q.shape[0], q.shape[1]
+    _need(cu_seqlens, "cu_seqlens", _I32, (None,))
+    B = cu_seqlens.shape[0] - 1
+    _pools(desc, codes, scales)
+    _table(page_table, context_lens, B)
+    if softmax_scale is None:
+        softmax_scale = desc.head_dim ** -0.5
+    d = desc.c_struct()
+    if workspace is None:
+        n = lib.uq_cross_workspace_bytes(ctypes.byref(d), T, B, Hq, max_context)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", _U8)
+    if out is None:
+        with _on(stream):
+            out = torch.zeros((T, Hq, desc.head_dim), dtype=out_dtype, device=q.device)
+    _need(out, "out", _OUT, (T, Hq, desc.head_dim))
+    st = lib.uq_cross_attention(ctypes.byref(d), _ptr(q), _DT[q.dtype], q_stride, T, _ptr(cu_seqlens), B, Hq,
+                                _ptr(codes), _ptr(scales), _ptr(page_table), page_table.shape[1], _ptr(context_lens),
+                                max_context, softmax_scale, _ptr(workspace), workspace.numel(), _ptr(out),
+                                _DT[out.dtype], _stream(stream))
+    _check(st, "uq_cross_attention")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Eviction by accumulated attention weight
+
+
+def token_weights_workspace_bytes(desc: CacheDesc, num_tokens, batch, num_q_heads, max_context, last=0,
+                                  q_dtype=torch.uint8):
+    d = desc.c_struct()
+    return int(lib.uq_token_weights_workspace_bytes(ctypes.byref(d), _DT[q_dtype], num_tokens, batch, num_q_heads,
+                                                    max_context, last))
+
+
+def token_weights(desc: CacheDesc, q, cu_seqlens, codes, scales, page_table, context_lens, max_context, weights, last=0,
+                  causal=True, softmax_scale=None, workspace=None, stream=None):
+    """Adds to weights (float32 [batch, Hkv, width >= max_context]) the attention
+    weight that the step's queries q [T, Hq, d] (prepared FP8 bytes, or rows) give
+    every cached token, summed over the queries and the KV head's query heads;
+    returns weights.  `last`: only each sequence's last queries."""
+    q_stride = _head_rows(q, "q", _QUERY, (None, None, desc.head_dim))
+    T, Hq = q.shape[0], q.shape[1]
+    _need(cu_seqlens, "cu_seqlens", _I32, (None,))
+    B = cu_seqlens.shape[0] - 1
+    _pools(desc, codes, scales)
+    _table(page_table, context_lens, B)
+    _need(weights, "weights", (torch.float32,), (B, desc.num_kv_heads, None))
+    if softmax_scale is None:
+        softmax_scale = desc.head_dim ** -0.5
+    d = desc.c_struct()
+    if workspace is None:
+        n = lib.uq_token_weights_workspace_bytes(ctypes.byref(d), _DT[q.dtype], T, B, Hq, max_context, last)
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", _U8)
+    st = lib.uq_token_weights(ctypes.byref(d), _ptr(q), _DT[q.dtype], q_stride, T, _ptr(cu_seqlens), B, Hq,
+                              _ptr(codes), _ptr(scales), _ptr(page_table), page_table.shape[1], _ptr(context_lens),
+                              max_context, last, int(bool(causal)), softmax_scale, _ptr(weights), weights.shape[2],
+                              _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "uq_token_weights")
+    return weights
+
+
+def select_workspace_bytes(batch, num_kv_heads, max_context, budget):
+    return int(lib.uq_select_tokens_workspace_bytes(batch, num_kv_heads, max_context, budget))
+
+
+def select_tokens(weights, context_lens, max_context, budget, sinks=0, recent=0, kept=None, kept_lens=None,
+                  workspace=None, stream=None):
+    """The tokens of every sequence and KV head that stay within `budget`: the
+    first `sinks`, the last `recent`, and those of the largest weight between
+    -> (kept int32 [batch, Hkv, budget], ascending, -1 behind the last;
+    kept_lens int32 [batch])."""
+    _need(weights, "weights", (torch.float32,), (None, None, None))
+    B, H, width = weights.shape
+    _need(context_lens, "context_lens", _I32, (B,))
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(select_workspace_bytes(B, H, max_context, budget), dtype=torch.uint8,
+                                    device=weights.device)
+    _need(workspace, "workspace", _U8)
+    if kept is None:
+        with _on(stream):
+            kept = torch.empty((B, H, max(budget, 0)), dtype=torch.int32, device=weights.device)
+    if kept_lens is None:
+        with _on(stream):
+            kept_lens = torch.empty(B, dtype=torch.int32, device=weights.device)
+    _need(kept, "kept", _I32, (B, H, budget))
+    _need(kept_lens, "kept_lens", _I32, (B,))
+    st = lib.uq_select_tokens(_ptr(weights), width, B, H, _ptr(context_lens), max_context, budget, sinks, recent,
+                              _ptr(kept), _ptr(kept_lens), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "uq_select_tokens")
+    return kept, kept_lens
+
+
+def compact_workspace_bytes(desc: CacheDesc, batch, budget):
+    d = desc.c_struct()
+    return int(lib.uq_compact_kv_workspace_bytes(ctypes.byref(d), batch, budget))
+
+
+def compact_kv(desc: CacheDesc, kept, kept_lens, context_lens, codes, scales, page_table, weights=None,
+               freed_pages=None, freed_count=None, workspace=None, stream=None):
+    """Moves the kept tokens (select_tokens) to the front of their sequences'
+    pages, with their weights; kept_lens are the new context lengths.
+    freed_pages int32 [>= batch * max_pages_per_seq] and freed_count int32 [1]
+    get the ids of the pages behind them."""
+    _need(kept, "kept", _I32, (None, desc.num_kv_heads, None))
+    B, H, budget = kept.shape
+    _need(kept_lens, "kept_lens", _I32, (B,))
+    _table(page_table, context_lens, B)
+    _pools(desc, codes, scales)
+    if weights is not None:
+        _need(weights, "weights", (torch.float32,), (B, H, None))
+    if freed_pages is not None:
+        _need(freed_pages, "freed_pages", _I32, (None,), min_numel=B * page_table.shape[1])
+    if freed_count is not None:
+        _need(freed_count, "freed_count", _I32, (1,))
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(compact_workspace_bytes(desc, B, budget), dtype=torch.uint8, device=codes.device)
+    _need(workspace, "workspace", _U8)
+    d = desc.c_struct()
+    st = lib.uq_compact_kv(ctypes.byref(d), _ptr(kept), budget, _ptr(kept_lens), _ptr(context_lens), B, _ptr(codes),
+                           _ptr(scales), _ptr(page_table), page_table.shape[1], _ptr(weights),
+                           0 if weights is None else weights.shape[2], _ptr(freed_pages), _ptr(freed_count),
+                           _ptr(workspace), workspace.numel(), _stream(stream))
+    _check(st, "uq_compact_kv")
 
 
 def decode_window_workspace_bytes(desc: CacheDesc, batch, num_q_heads, max_context, window, sinks=0,
