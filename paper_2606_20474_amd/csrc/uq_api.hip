@@ -1002,20 +1002,19 @@ static Span scales_span(const uq_cache_desc* d, const uint8_t* at) {
     return {at, size_t(d->num_pages) * size_t(d->num_kv_heads) * size_t(d->head_dim)};
 }
 
-// How a call of uq_token_weights is cut.  A wave of the first kernel holds
-// 16 row_units rows and walks `chunk` tokens, one of the second holds key_units units of
-// keys (16 tokens; 32 at head size 64) and walks row_split rows.
+// How a call of uq_token_weights is cut: by rows and chunks of the context, and for the
+// sums of many rows by keys (128 tokens per wave) and splits of the rows.
 struct WeightsShape {
     int64_t rows_per_head;
-    bool by_seq;
-    int32_t row_units, chunk, chunks, key_units, row_split, splits;
+    bool by_seq, few;
+    int32_t row_units, chunk, chunks, row_split, splits;
     int32_t norm_blocks, sum_blocks;
     size_t query, rows;    // bytes of the prepared queries and of the rows' references and sums
     size_t workspace;
 };
 // Partial results of split rows or contexts: the splits below keep to it.
 constexpr size_t kWeightsParts = size_t(16) << 20;
-constexpr int64_t kWeightsWaves = 4096;    // four per SIMD
+constexpr int64_t kFewWaves = 8192, kManyWaves = 16384, kSumWaves = 16384;
 
 static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int64_t num_tokens, int32_t batch,
                                int32_t num_q_heads, int32_t max_context, int32_t last, WeightsShape& e) {
@@ -1033,36 +1032,37 @@ static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int6
     e.by_seq = last > 0 && int64_t(batch) * last < num_tokens;
     const int64_t queries = e.by_seq ? int64_t(batch) * last : num_tokens;
     e.rows_per_head = queries * group;
-    // 16 rows per wave where a sequence has no more, up to 128 (64 at head size 256, whose
-    // operands are twice as large)
-    const int64_t each = seqs > 0 ? (e.rows_per_head + seqs - 1) / seqs : 1;
-    const int32_t most = desc->head_dim == 256 ? 4 : 8;
-    e.row_units = 1;
-    while (e.row_units < most && 16 * e.row_units < each) e.row_units *= 2;
-    const int64_t row_blocks = (e.rows_per_head / (16 * e.row_units) + seqs) * heads;
-    // the longest chunks, from 512 tokens on, that leave a wave for every place
-    const int64_t bound = max_context > 1 ? max_context : 1;
-    e.chunk = 1 << 30;
-    while (e.chunk > 512 && row_blocks * ((bound + e.chunk - 1) / e.chunk) < kWeightsWaves) e.chunk /= 2;
     const int64_t rows = e.rows_per_head * heads;
+    // few rows, by the mean: no more than a wave holds of them as BF16 operands
+    const int64_t each = seqs > 0 ? (e.rows_per_head + seqs - 1) / seqs : 1;
+    const bool large = desc->head_dim == 256;
+    e.few = each <= (large ? 32 : 64);
+    e.row_units = !e.few ? (large ? 4 : 8) : each <= 16 ? 1 : each <= 32 ? 2 : 4;
+    const int64_t row_blocks = (e.rows_per_head / (16 * e.row_units) + seqs) * heads;
+    // the longest chunks, from 128 tokens (many rows: 512) on, that give so many waves
+    const int64_t bound = max_context > 1 ? max_context : 1;
+    const int32_t least = e.few ? 128 : 512;
+    e.chunk = 1 << 30;
+    while (e.chunk > least && row_blocks * ((bound + e.chunk - 1) / e.chunk) < (e.few ? kFewWaves : kManyWaves)) e.chunk /= 2;
     while (e.chunk < (1 << 30) && bound > e.chunk && size_t(rows) * size_t((bound + e.chunk - 1) / e.chunk) * 8 > kWeightsParts) e.chunk *= 2;
     e.chunks = int32_t((bound + e.chunk - 1) / e.chunk);
     const int64_t norm_waves = row_blocks * e.chunks;
-    // keys: 128 tokens per wave where that leaves enough waves, else 2 units
-    const int32_t unit = desc->head_dim == 64 ? 32 : 16, wide = desc->head_dim == 128 ? 8 : 4;
-    auto groups = [&](int32_t units) { return int64_t(batch) * heads * ((bound + units * unit - 1) / (units * unit)); };
-    e.key_units = groups(wide) >= kWeightsWaves ? wide : 2;
-    // rows split where the keys are too few
-    const int64_t longest = (e.by_seq || (last > 0 && last < num_tokens) ? int64_t(last) : num_tokens) * group;
-    int64_t splits = groups(e.key_units) > 0 ? kWeightsWaves / groups(e.key_units) : 1;
-    splits = splits < longest / 256 ? splits : longest / 256;
-    const size_t part = size_t(batch) * size_t(heads) * size_t(bound) * sizeof(float);
-    while (splits > 1 && part * size_t(splits) > kWeightsParts) --splits;
-    splits = splits > 1 ? splits : 1;
-    e.row_split = int32_t(((longest + splits - 1) / splits + 15) / 16 * 16);
-    if (e.row_split < 16) e.row_split = 16;
-    e.splits = int32_t(longest > 0 ? (longest + e.row_split - 1) / e.row_split : 1);
-    const int64_t sum_waves = groups(e.key_units) * e.splits;
+    int64_t sum_waves = norm_waves;
+    e.splits = 1;
+    e.row_split = 16;
+    if (!e.few) {
+        const int64_t groups = int64_t(batch) * heads * ((bound + (large ? 64 : 128) - 1) / (large ? 64 : 128));
+        // rows split where the keys are too few
+        const int64_t longest = (last > 0 && last < num_tokens ? int64_t(last) : num_tokens) * group;
+        int64_t splits = kSumWaves / (groups > 0 ? groups : 1);
+        splits = splits < longest / 256 ? splits : longest / 256;
+        const size_t part = size_t(batch) * size_t(heads) * size_t(bound) * sizeof(float);
+        while (splits > 1 && part * size_t(splits) > kWeightsParts) --splits;
+        splits = splits > 1 ? splits : 1;
+        e.row_split = int32_t(((longest + splits - 1) / splits + 15) / 16 * 16);
+        e.splits = int32_t((longest + e.row_split - 1) / e.row_split);
+        sum_waves = groups * e.splits;
+    }
     // items are numbered in 31 bits
     if (norm_waves >= (int64_t(1) << 30) || sum_waves >= (int64_t(1) << 30)) return UQ_ERR_UNSUPPORTED;
     const int64_t at_once = 32 * int64_t(uq::kNumCus);   // blocks of 4 waves; a wave goes on to further items
@@ -1100,6 +1100,7 @@ uq_status uq_token_weights(const uq_cache_desc* desc, const void* q, uq_dtype q_
     if (!aligned16(q) || !aligned16(kv_codes) || !aligned16(kv_scales) || !aligned16(workspace)) return UQ_ERR_INVALID_ARGUMENT;
     const int64_t vec = q_dtype == UQ_F32 ? 4 : q_dtype == UQ_FP8_E4M3 ? 16 : 8;   // elements of 16 bytes
     if (q_stride < int64_t(num_q_heads) * desc->head_dim || q_stride % vec != 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (q_stride >= (int64_t(1) << 26)) return UQ_ERR_UNSUPPORTED;   // 16 rows on are in 32 bits
     if (workspace_bytes < e.workspace) return UQ_ERR_WORKSPACE_TOO_SMALL;
     const size_t item = q_dtype == UQ_F32 ? 4 : q_dtype == UQ_FP8_E4M3 ? 1 : 2, word = sizeof(int32_t);
     const std::initializer_list<Span> outs = {{weights, size_t(batch) * size_t(desc->num_kv_heads) * size_t(weights_width) * word}, {workspace, e.workspace}},
@@ -1142,10 +1143,10 @@ uq_status uq_token_weights(const uq_cache_desc* desc, const void* q, uq_dtype q_
     p.width = weights_width;
     p.by_seq = e.by_seq;
     p.rows_per_head = e.rows_per_head;
+    p.few = e.few;
     p.row_units = e.row_units;
     p.chunk = e.chunk;
     p.chunks = e.chunks;
-    p.key_units = e.key_units;
     p.row_split = e.row_split;
     p.splits = e.splits;
     p.norm_blocks = e.norm_blocks;
@@ -1164,9 +1165,16 @@ static uq_status check_kept(int32_t batch, int32_t num_kv_heads, int32_t budget)
     return UQ_OK;
 }
 
+// Longer rows than a slice are cut by uq_select_tokens into slices of that many tokens, a block each in
+// three launches; their counts and candidates are in the workspace.
+static int64_t select_slices(int32_t max_context) {
+    return max_context > uq::kSelectSlice ? (int64_t(max_context) + uq::kSelectSlice - 1) / uq::kSelectSlice : 1;
+}
+
 size_t uq_select_tokens_workspace_bytes(int32_t batch, int32_t num_kv_heads, int32_t max_context, int32_t budget) {
-    (void)batch, (void)num_kv_heads, (void)max_context, (void)budget;
-    return 0;
+    if (check_kept(batch, num_kv_heads, budget) != UQ_OK || max_context < 0 || max_context > (1 << 30)) return 0;
+    const int64_t slices = select_slices(max_context);
+    return slices == 1 || max_context <= budget ? 0 : size_t(batch) * size_t(num_kv_heads) * (size_t(slices) * uq::kSelectSliceBytes + 16);
 }
 
 uq_status uq_select_tokens(const float* weights, int64_t weights_width, int32_t batch, int32_t num_kv_heads,
@@ -1181,19 +1189,31 @@ uq_status uq_select_tokens(const float* weights, int64_t weights_width, int32_t 
     if (batch == 0) return UQ_OK;
     if ((weights == nullptr && max_context > budget) || context_lens == nullptr || kept == nullptr || kept_lens == nullptr)
         return UQ_ERR_INVALID_ARGUMENT;
-    if (workspace_bytes < uq_select_tokens_workspace_bytes(batch, num_kv_heads, max_context, budget)) return UQ_ERR_WORKSPACE_TOO_SMALL;
-    (void)workspace;
+    const size_t need = uq_select_tokens_workspace_bytes(batch, num_kv_heads, max_context, budget);
+    const int64_t slices = need > 0 ? select_slices(max_context) : 1;
+    if (slices * batch * num_kv_heads >= kMaxBlocks / 4) return UQ_ERR_UNSUPPORTED;   // blocks of 1024 threads
+    if (need > 0 && (workspace == nullptr || !aligned16(workspace))) return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return UQ_ERR_WORKSPACE_TOO_SMALL;
     const size_t word = sizeof(int32_t), rows = size_t(batch) * size_t(num_kv_heads);
-    const std::initializer_list<Span> outs = {{kept, rows * size_t(budget) * word}, {kept_lens, size_t(batch) * word}},
+    const std::initializer_list<Span> outs = {{kept, rows * size_t(budget) * word}, {kept_lens, size_t(batch) * word}, {workspace, need}},
                                       ins = {{weights, rows * size_t(weights_width) * word}, {context_lens, size_t(batch) * word}};
     if (outputs_meet(outs, ins)) return UQ_ERR_INVALID_ARGUMENT;
-    const uq::SelectParams p{weights, weights_width, batch, num_kv_heads, context_lens, max_context, budget, sinks, recent, kept, kept_lens};
+    const uq::SelectParams p{weights, weights_width, batch, num_kv_heads, context_lens, max_context, budget, sinks, recent, kept, kept_lens,
+                             int32_t(slices), need > 0 ? static_cast<uint8_t*>(workspace) : nullptr};
     return from_hip(uq::launch_select_tokens(p, static_cast<hipStream_t>(stream)));
 }
 
+// (sequence, KV head) pairs from which a block each for keys and values moves its tokens in
+// place; fewer go through the workspace, a page per wave.  32, 64, 128 and 512 pairs of 16000
+// tokens cut to 4096, head size 128: 33, 45, 77 and 295 us in place, 24, 49, 106 and 384 through
+// the workspace; 512 of 600 cut to 500 19 and 32.
+constexpr int64_t kCompactRows = 64;
+
 size_t uq_compact_kv_workspace_bytes(const uq_cache_desc* desc, int32_t batch, int32_t budget) {
-    (void)desc, (void)batch, (void)budget;
-    return 0;
+    if (check_desc(desc) != UQ_OK || check_kept(batch, desc->num_kv_heads, budget) != UQ_OK) return 0;
+    const int64_t rows = int64_t(batch) * desc->num_kv_heads;
+    if (rows >= kCompactRows) return 0;
+    return align16(size_t(rows) * (size_t((budget + kPageSize - 1) / kPageSize) * 17 * size_t(desc->head_dim) + size_t(budget) * sizeof(float)));
 }
 
 uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t budget, const int32_t* kept_lens,
@@ -1210,17 +1230,20 @@ uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t 
                       kv_scales == nullptr || page_table == nullptr))
         return UQ_ERR_INVALID_ARGUMENT;
     if (!aligned16(kv_codes) || !aligned16(kv_scales)) return UQ_ERR_INVALID_ARGUMENT;
-    if (workspace_bytes < uq_compact_kv_workspace_bytes(desc, batch, budget)) return UQ_ERR_WORKSPACE_TOO_SMALL;
-    (void)workspace;
+    const size_t need = uq_compact_kv_workspace_bytes(desc, batch, budget);
+    if (need > 0 && (workspace == nullptr || !aligned16(workspace))) return UQ_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return UQ_ERR_WORKSPACE_TOO_SMALL;
+    if (need > 0 && int64_t(batch) * desc->num_kv_heads * ((budget + kPageSize - 1) / kPageSize) >= 4 * kMaxBlocks - 8) return UQ_ERR_UNSUPPORTED;
     const size_t word = sizeof(int32_t), rows = size_t(batch) * size_t(desc->num_kv_heads), seqs = size_t(batch);
     const std::initializer_list<Span> outs = {codes_span(desc, kv_codes), scales_span(desc, kv_scales), {weights, rows * size_t(weights_width) * word},
-                         {freed_pages, seqs * size_t(max_pages_per_seq) * word}, {freed_count, word}},
+                         {freed_pages, seqs * size_t(max_pages_per_seq) * word}, {freed_count, word}, {workspace, need}},
                                       ins = {{kept, rows * size_t(budget) * word}, {kept_lens, seqs * word}, {context_lens, seqs * word},
                         {page_table, seqs * size_t(max_pages_per_seq) * word}};
     if (outputs_meet(outs, ins)) return UQ_ERR_INVALID_ARGUMENT;
     if (batch == 0 && freed_count == nullptr) return UQ_OK;
     const uq::CompactParams p{kv_codes, kv_scales, desc->num_pages, desc->head_dim, desc->num_kv_heads, batch, kept, budget, kept_lens,
-                              context_lens, page_table, max_pages_per_seq, weights, weights_width, freed_pages, freed_count};
+                              context_lens, page_table, max_pages_per_seq, weights, weights_width, freed_pages, freed_count,
+                              need > 0 ? static_cast<uint8_t*>(workspace) : nullptr};
     return from_hip(uq::launch_compact_kv(p, static_cast<hipStream_t>(stream)));
 }
 

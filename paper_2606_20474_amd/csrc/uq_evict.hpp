@@ -12,10 +12,20 @@ namespace uq {
 // Which tokens stay.  Of a row (sequence, KV head) with more tokens than the
 // budget: the first `sinks`, the last `recent`, and of those between the ones with
 // the largest weights, of equal ones the first.  The weight of the last one that
-// stays is found by its bits, most significant first, from counts of the keys
-// (floats as integers of the same order) that begin with the bits found so far.
+// stays is found by its bits, 11, 11 and 10 at a time, most significant first, from
+// counts of the keys (floats as integers of the same order) that begin with the
+// bits found so far.
+//
+// Rows of up to kSelectSlice tokens: a block each, which holds the keys in registers, wave
+// w the tokens 1024 w .. 1024 w + 1023, 64 at a time, and so in order.  Longer rows are cut
+// into such slices, a block each, in three launches: the counts of the first 11 bits;
+// those bits of the row, and a list of the keys that begin with them; the rest of the
+// bits from the lists (from the slice itself where there are more than a list holds) and
+// the indices.  Every block of a row finds the same; none waits for another.
 
 constexpr int kSelectThreads = 1024;
+constexpr int kSelectBins = 2048;
+constexpr int kSelectKeys = kSelectSlice / kSelectThreads;
 
 // A float's bits as an unsigned integer of the same order; -0 equals 0, and a NaN is
 // below every number.
@@ -25,112 +35,340 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_tokens_kernel(SelectParams p) {
-    constexpr int kBins = 2048, kWaves = kSelectThreads / 64;
-    __shared__ int bins[kBins];
-    __shared__ int wave_sum[2][kWaves];
-    __shared__ int found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = int(blockIdx.x / unsigned(p.heads));
-    int n = p.context_lens[b];
+// A slice's tokens: which compete, and their keys.
+struct SelectRow {
+    const float* w;
+    int n, lo, hi, want;      // tokens; those that compete; how many of them stay
+    int from;                 // first token of this wave
+};
+struct SelectKeys {
+    uint32_t key[kSelectKeys];
+};
+__device__ __forceinline__ SelectRow select_row(const SelectParams& p, int row, int slice) {
+    SelectRow r;
+    int n = p.context_lens[row / p.heads];
     n = n < p.max_context ? n : p.max_context;
-    n = n > 0 ? n : 0;
-    const float* w = p.weights + int64_t(blockIdx.x) * p.width;
-    int32_t* kept = p.kept + int64_t(blockIdx.x) * p.budget;
-    if (blockIdx.x % unsigned(p.heads) == 0 && tid == 0) p.kept_lens[b] = n < p.budget ? n : p.budget;
-    if (n <= p.budget) {
-        for (int i = tid; i < p.budget; i += kSelectThreads) kept[i] = i < n ? i : -1;
-        return;
-    }
-    // the tokens that compete, and how many of them stay
-    const int lo = p.sinks, hi = n - p.recent;
-    const int want = p.budget - p.sinks - p.recent;
-    uint32_t prefix = 0;    // the bits found
-    int above = 0;          // competing keys above every key that begins with them
-    int shift = 32;
-    // (want == 0: no key is above the largest one, and no equal one stays)
-    for (int pass = 0; pass < 3 && want > 0; ++pass) {
-        const int width = pass == 2 ? 10 : 11;
-        const int before = shift;
-        shift -= width;
-        for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
-        __syncthreads();
-        for (int t = lo + tid; t < hi; t += kSelectThreads) {
-            const uint32_t key = weight_key(w[t]);
-            if (before == 32 || key >> before == prefix) atomicAdd(&bins[(key >> shift) & ((1u << width) - 1)], 1);
-        }
-        __syncthreads();
-        // the largest bin with at least want - above keys in it and above it: thread i
-        // holds bins 2 i and 2 i + 1, from the top
-        const int top = kBins - 1 - 2 * tid;
-        const int c0 = bins[top], c1 = bins[top - 1];
-        int sum = c0 + c1;
+    r.n = n > 0 ? n : 0;
+    r.w = p.weights + int64_t(row) * p.width;
+    r.lo = p.sinks;
+    r.hi = r.n - p.recent;
+    r.want = p.budget - p.sinks - p.recent;
+    r.from = slice * kSelectSlice + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 * kSelectKeys);
+    return r;
+}
+__device__ __forceinline__ void load_keys(const SelectRow& r, SelectKeys& k) {
+    const int lane = threadIdx.x & 63;
+    float x[kSelectKeys];
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int o = __shfl_up(sum, s);
-            if (lane >= s) sum += o;
+    for (int i = 0; i < kSelectKeys; ++i) {
+        const int t = r.from + 64 * i + lane;
+        x[i] = r.w[t < r.n ? t : r.n - 1];
+    }
+#pragma unroll
+    for (int i = 0; i < kSelectKeys; ++i) k.key[i] = weight_key(x[i]);
+}
+// f(key, token, competes) for every key of this wave; a wave whose tokens all compete takes a path without
+// the comparisons.
+template <class F>
+__device__ __forceinline__ void each_key(const SelectRow& r, const SelectKeys& k, F f) {
+    const int lane = threadIdx.x & 63;
+    if (r.from >= r.lo && r.from + 64 * kSelectKeys <= r.hi) {
+#pragma unroll
+        for (int i = 0; i < kSelectKeys; ++i) f(k.key[i], r.from + 64 * i + lane, true);
+    } else if (r.from < r.n) {
+#pragma unroll
+        for (int i = 0; i < kSelectKeys; ++i) {
+            const int t = r.from + 64 * i + lane;
+            f(k.key[i], t, t >= r.lo && t < r.hi);
         }
-        if (lane == 63) wave_sum[0][wave] = sum;
-        __syncthreads();
-        int prior = 0;
-        for (int i = 0; i < wave; ++i) prior += wave_sum[0][i];
-        const int end = above + prior + sum, mid = end - c1, start = mid - c0;
-        if (start < want && end >= want) {
-            found[0] = mid >= want ? top : top - 1;
-            found[1] = mid >= want ? start : mid;
-        }
-        __syncthreads();
-        prefix = (prefix << width) | uint32_t(found[0]);
-        above = found[1];
-        __syncthreads();
-    }
-    // every key above `prefix` stays, and the first `ties` equal to it
-    const uint32_t least = want > 0 ? prefix : 0xFFFFFFFFu;
-    const int ties = want > 0 ? want - above : 0;
-    // a wave takes a run of tokens: counts first, then the indices
-    const int run = ((n + kSelectThreads - 1) / kSelectThreads) * 64;
-    const int from = wave * run < n ? wave * run : n, to = from + run < n ? from + run : n;
-    auto kind = [&](int t, bool& sure, bool& equal) {
-        sure = equal = false;
-        if (t < to) {
-            const bool fixed = t < lo || t >= hi;
-            const uint32_t key = fixed ? 0u : weight_key(w[t]);
-            sure = fixed || key > least;
-            equal = !fixed && key == least;
-        }
-    };
-    int nsure = 0, nequal = 0;
-    for (int t = from; t < to; t += 64) {
-        bool sure, equal;
-        kind(t + lane, sure, equal);
-        nsure += __builtin_popcountll(__builtin_amdgcn_ballot_w64(sure));
-        nequal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(equal));
-    }
-    if (lane == 0) {
-        wave_sum[0][wave] = nsure;
-        wave_sum[1][wave] = nequal;
-    }
-    __syncthreads();
-    int s0 = 0, e0 = 0;
-    for (int i = 0; i < wave; ++i) {
-        s0 += wave_sum[0][i];
-        e0 += wave_sum[1][i];
-    }
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    for (int t = from; t < to; t += 64) {
-        bool sure, equal;
-        kind(t + lane, sure, equal);
-        const uint64_t sm = __builtin_amdgcn_ballot_w64(sure), em = __builtin_amdgcn_ballot_w64(equal);
-        const int s = s0 + __builtin_popcountll(sm & below), e = e0 + __builtin_popcountll(em & below);
-        const int at = s + (e < ties ? e : ties);
-        if ((sure || (equal && e < ties)) && at < p.budget) kept[at] = t + lane;
-        s0 += __builtin_popcountll(sm);
-        e0 += __builtin_popcountll(em);
     }
 }
 
+// Counts of a block in LDS, four of each so that lanes that meet in a bin (10 weights of 64 may be 0)
+// meet in an address four times as rarely.
+struct SelectCounts {
+    int bins[kSelectBins * 4];
+    int wave_sum[2][kSelectThreads / 64];
+    int found[2];
+};
+__device__ __forceinline__ void clear_counts(SelectCounts& c) {
+    int4* const b = reinterpret_cast<int4*>(c.bins);
+    b[threadIdx.x] = make_int4(0, 0, 0, 0);
+    b[threadIdx.x + kSelectThreads] = make_int4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void count_bin(SelectCounts& c, uint32_t bin) {
+    atomicAdd(&c.bins[bin * 4 + (threadIdx.x & 3)], 1);
+}
+// This thread's two bins, from the top: kSelectBins - 1 - 2 i and the one below.
+__device__ __forceinline__ int2 two_bins(const SelectCounts& c) {
+    const int top = kSelectBins - 1 - 2 * int(threadIdx.x);
+    const int4 a = reinterpret_cast<const int4*>(c.bins)[top], b = reinterpret_cast<const int4*>(c.bins)[top - 1];
+    return make_int2(a.x + a.y + a.z + a.w, b.x + b.y + b.z + b.w);
+}
+// The bin in which the want-th key from the top is, `above` keys being above all of them; `above` becomes
+// the number above that bin.  c2: two_bins of the counts.
+__device__ __forceinline__ uint32_t find_bin(SelectCounts& c, int2 c2, int want, int& above) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sum = c2.x + c2.y;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int o = __shfl_up(sum, s);
+        if (lane >= s) sum += o;
+    }
+    if (lane == 63) c.wave_sum[0][wave] = sum;
+    __syncthreads();
+    int prior = above;
+#pragma unroll
+    for (int i = 0; i < kSelectThreads / 64; ++i) prior += i < wave ? c.wave_sum[0][i] : 0;
+    const int end = prior + sum, mid = end - c2.y, start = mid - c2.x;
+    if (start < want && end >= want) {
+        const int top = kSelectBins - 1 - 2 * int(threadIdx.x);
+        c.found[0] = mid >= want ? top : top - 1;
+        c.found[1] = mid >= want ? start : mid;
+    }
+    __syncthreads();
+    above = c.found[1];
+    return uint32_t(c.found[0]);
+}
+
+// The indices of a slice's tokens that stay: those that do not compete, the keys above `least` and, while there
+// are `ties` of them, equal ones; `at` and `equal` of both kinds come before.
+__device__ __forceinline__ void write_kept(const SelectParams& p, const SelectRow& r, const SelectKeys& k, SelectCounts& c, int row,
+                                           uint32_t least, int ties, int at, int equal) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int sures = 0, equals = 0;
+    auto sure_of = [&](uint32_t key, int t, bool competes) { return competes ? key > least : t < r.n; };
+    each_key(r, k, [&](uint32_t key, int t, bool competes) {
+        sures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(sure_of(key, t, competes)));
+        equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(competes && key == least));
+    });
+    if (lane == 0) {
+        c.wave_sum[0][wave] = sures;
+        c.wave_sum[1][wave] = equals;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelectThreads / 64; ++i) {
+        at += i < wave ? c.wave_sum[0][i] : 0;
+        equal += i < wave ? c.wave_sum[1][i] : 0;
+    }
+    int32_t* const kept = p.kept + int64_t(row) * p.budget;
+    auto below = [](uint64_t m) { return int(__builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0u))); };
+    each_key(r, k, [&](uint32_t key, int t, bool competes) {
+        const bool sure = sure_of(key, t, competes), same = competes && key == least;
+        const uint64_t sm = __builtin_amdgcn_ballot_w64(sure), em = __builtin_amdgcn_ballot_w64(same);
+        const int e = em != 0 ? equal + below(em) : equal;
+        if (sure || (same && e < ties)) {
+            const int to = at + below(sm) + (e < ties ? e : ties);
+            if (to < p.budget) kept[to] = t;
+        }
+        at += __builtin_popcountll(sm);
+        equal += __builtin_popcountll(em);
+    });
+}
+
+// A row that stays whole; false: it does not.
+__device__ __forceinline__ bool keep_all(const SelectParams& p, const SelectRow& r, int row) {
+    if (row % p.heads == 0 && threadIdx.x == 0) p.kept_lens[row / p.heads] = r.n < p.budget ? r.n : p.budget;
+    if (r.n > p.budget) return false;
+    int32_t* const kept = p.kept + int64_t(row) * p.budget;
+    for (int i = threadIdx.x; i < p.budget; i += kSelectThreads) kept[i] = i < r.n ? i : -1;
+    return true;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_tokens_kernel(SelectParams p) {
+    __shared__ __attribute__((aligned(16))) SelectCounts c;
+    const int row = int(blockIdx.x);
+    const SelectRow r = select_row(p, row, 0);
+    if (keep_all(p, r, row)) return;
+    SelectKeys k;
+    load_keys(r, k);
+    uint32_t prefix = 0;    // the bits found
+    int above = 0;          // competing keys above every key that begins with them
+    // (want == 0: no key is above the largest one, and no equal one stays)
+    if (r.want > 0) {
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            clear_counts(c);
+            __syncthreads();
+            each_key(r, k, [&](uint32_t key, int, bool competes) {
+                if (pass == 0 ? competes : competes && key >> (pass == 1 ? 21 : 10) == prefix)
+                    count_bin(c, pass == 0 ? key >> 21 : pass == 1 ? key >> 10 & 2047u : key & 1023u);
+            });
+            __syncthreads();
+            const uint32_t bin = find_bin(c, two_bins(c), r.want, above);
+            prefix = pass == 0 ? bin : pass == 1 ? prefix << 11 | bin : prefix << 10 | bin;
+        }
+    }
+    write_kept(p, r, k, c, row, r.want > 0 ? prefix : 0xFFFFFFFFu, r.want > 0 ? r.want - above : 0, 0, 0);
+}
+
+// A slice's part of the workspace.
+struct SelectSlice {
+    int counts[kSelectBins];         // of the first 11 bits, from the top
+    uint32_t list[kSelectList];      // the keys that begin with the row's
+    int listed, sure, unused[2];     // how many there are (more than kSelectList: not listed), and tokens that stay for sure
+};
+static_assert(sizeof(SelectSlice) == kSelectSliceBytes, "its size in the workspace");
+__device__ __forceinline__ SelectSlice* slice_of(const SelectParams& p, int row, int slice) {
+    return reinterpret_cast<SelectSlice*>(p.workspace) + int64_t(row) * p.slices + slice;
+}
+// The first bits of a row, and the competing keys above them.
+__device__ __forceinline__ int2* first_bits_of(const SelectParams& p, int row) {
+    const int64_t rows = int64_t(p.batch) * p.heads;
+    return reinterpret_cast<int2*>(p.workspace + rows * p.slices * kSelectSliceBytes + int64_t(row) * 16);
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_count_kernel(SelectParams p) {
+    __shared__ __attribute__((aligned(16))) SelectCounts c;
+    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const SelectRow r = select_row(p, row, slice);
+    if (r.n <= p.budget) {
+        if (slice == 0) keep_all(p, r, row);
+        return;
+    }
+    if (slice == 0) keep_all(p, r, row);   // (its length)
+    if (slice * kSelectSlice >= r.n || r.want == 0) return;
+    SelectKeys k;
+    load_keys(r, k);
+    clear_counts(c);
+    __syncthreads();
+    each_key(r, k, [&](uint32_t key, int, bool competes) {
+        if (competes) count_bin(c, key >> 21);
+    });
+    __syncthreads();
+    reinterpret_cast<int2*>(slice_of(p, row, slice)->counts)[threadIdx.x] = two_bins(c);
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_list_kernel(SelectParams p) {
+    __shared__ SelectCounts c;
+    __shared__ int listed;
+    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const SelectRow r = select_row(p, row, slice);
+    if (r.n <= p.budget || slice * kSelectSlice >= r.n) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    SelectKeys k;
+    load_keys(r, k);
+    if (threadIdx.x == 0) listed = 0;
+    uint32_t bits = 0xFFFFFFFFu;     // (want == 0: above every key)
+    int above = 0;
+    if (r.want > 0) {
+        int2 sum = make_int2(0, 0);
+        const int slices = (r.n + kSelectSlice - 1) / kSelectSlice;
+#pragma unroll 8
+        for (int s = 0; s < slices; ++s) {
+            const int2 x = reinterpret_cast<const int2*>(slice_of(p, row, s)->counts)[threadIdx.x];
+            sum.x += x.x;
+            sum.y += x.y;
+        }
+        bits = find_bin(c, sum, r.want, above);
+        if (slice == 0 && threadIdx.x == 0) *first_bits_of(p, row) = make_int2(int(bits), above);
+    }
+    __syncthreads();
+    SelectSlice* const out = slice_of(p, row, slice);
+    int sures = 0;
+    each_key(r, k, [&](uint32_t key, int t, bool competes) {
+        const bool in = competes && key >> 21 == bits;
+        sures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(competes ? key >> 21 > bits : t < r.n));
+        const uint64_t who = __builtin_amdgcn_ballot_w64(in);
+        if (who == 0) return;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&listed, __builtin_popcountll(who));
+        at = __builtin_amdgcn_readfirstlane(at);
+        at += int(__builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0u)));
+        if (in && at < kSelectList) out->list[at] = key;
+    });
+    if (lane == 0) c.wave_sum[1][wave] = sures;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int sum = 0;
+        for (int i = 0; i < kSelectThreads / 64; ++i) sum += c.wave_sum[1][i];
+        out->sure = sum;
+        out->listed = listed;
+    }
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectParams p) {
+    __shared__ __attribute__((aligned(16))) SelectCounts c;
+    __shared__ int sums[2];
+    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const SelectRow r = select_row(p, row, slice);
+    if (r.n <= p.budget || slice * kSelectSlice >= r.n) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    SelectKeys k;
+    load_keys(r, k);
+    const int slices = (r.n + kSelectSlice - 1) / kSelectSlice;
+    uint32_t least = 0xFFFFFFFFu, bits = 0xFFFFFFFFu;
+    int ties = 0, above = 0;
+    if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+    // f(key, slice) for the row's keys that begin with its first bits: a quarter of a list per wave
+    auto each_listed = [&](auto f) {
+        constexpr int Q = kSelectList / 4 / 64;
+        for (int unit = wave; unit < 4 * slices; unit += kSelectThreads / 64) {
+            const int s = unit >> 2, q = unit & 3;
+            const SelectSlice* const x = slice_of(p, row, s);
+            const int listed = __builtin_amdgcn_readfirstlane(x->listed);
+            if (listed <= kSelectList) {
+                if (q * Q * 64 >= listed) continue;
+                uint32_t key[Q];
+#pragma unroll
+                for (int i = 0; i < Q; ++i) key[i] = x->list[(q * Q + i) * 64 + lane];
+#pragma unroll
+                for (int i = 0; i < Q; ++i)
+                    if ((q * Q + i) * 64 + lane < listed) f(key[i], s);
+            } else {
+                // (too many: the slice itself)
+                const int t0 = s * kSelectSlice + q * (kSelectSlice / 4);
+                for (int t = t0 + lane; t < t0 + kSelectSlice / 4 && t < r.hi; t += 64) {
+                    const uint32_t key = weight_key(r.w[t]);
+                    if (t >= r.lo && key >> 21 == bits) f(key, s);
+                }
+            }
+        }
+    };
+    if (r.want > 0) {
+        const int2 first = *first_bits_of(p, row);
+        bits = least = uint32_t(first.x);
+        above = first.y;
+#pragma unroll
+        for (int pass = 1; pass < 3; ++pass) {
+            clear_counts(c);
+            __syncthreads();
+            each_listed([&](uint32_t key, int) {
+                if (pass == 1 || key >> 10 == least) count_bin(c, pass == 1 ? key >> 10 & 2047u : key & 1023u);
+            });
+            __syncthreads();
+            const uint32_t bin = find_bin(c, two_bins(c), r.want, above);
+            least = pass == 1 ? least << 11 | bin : least << 10 | bin;
+        }
+        ties = r.want - above;
+    }
+    // of the slices before this one: the tokens that stay for sure, and the ties
+    __syncthreads();
+    int sures = 0, equals = 0;
+    for (int s = threadIdx.x; s < slice; s += kSelectThreads) sures += slice_of(p, row, s)->sure;
+    if (r.want > 0)
+        each_listed([&](uint32_t key, int s) {
+            sures += s < slice && key > least;
+            equals += s < slice && key == least;
+        });
+    if (sures != 0) atomicAdd(&sums[0], sures);
+    if (equals != 0) atomicAdd(&sums[1], equals);
+    __syncthreads();
+    write_kept(p, r, k, c, row, least, ties, sums[0], sums[1]);
+}
+
 hipError_t launch_select_tokens(const SelectParams& p, hipStream_t stream) {
-    hipLaunchKernelGGL(select_tokens_kernel, dim3(unsigned(p.batch * p.heads)), dim3(kSelectThreads), 0, stream, p);
+    const unsigned rows = unsigned(p.batch * p.heads);
+    const dim3 block{unsigned(kSelectThreads)};
+    if (p.slices == 1) {
+        hipLaunchKernelGGL(select_tokens_kernel, dim3(rows), block, 0, stream, p);
+        return hipGetLastError();
+    }
+    const dim3 grid{rows * unsigned(p.slices)};
+    hipLaunchKernelGGL(select_count_kernel, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(select_list_kernel, grid, block, 0, stream, p);
+    hipLaunchKernelGGL(select_write_kernel, grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
@@ -143,134 +381,344 @@ hipError_t launch_select_tokens(const SelectParams& p, hipStream_t stream) {
 
 constexpr int kCompactThreads = 256;
 
-template <int D>
-__global__ void __launch_bounds__(kCompactThreads) compact_kv_kernel(CompactParams p) {
-    constexpr int NT = kCompactThreads, G = D / 32;
-    constexpr int TOK = 64;                           // tokens of a chunk
-    constexpr int KU = TOK * G / NT, VU = TOK * (D / 8) / NT, SU = TOK * G * 2 / NT;   // units per thread
-    static_assert(KU * NT == TOK * G || KU == 0, "");
-    constexpr int KR = KU > 0 ? KU : 1, SR = SU > 0 ? SU : 1;
-    const int tid = threadIdx.x;
-    if (blockIdx.x == unsigned(p.batch * p.heads)) {
-        // page ids behind the kept tokens, in sequence order
-        __shared__ int sums[NT];
-        int base = 0;
-        for (int b0 = 0; b0 < p.batch; b0 += NT) {
-            const int b = b0 + tid;
-            int first = 0, count = 0;
-            if (b < p.batch) {
-                const int most = p.max_pages_per_seq * kPage;
-                int n = p.context_lens[b], k = p.kept_lens[b];
-                n = n < 0 ? 0 : n < most ? n : most;
-                k = k < 0 ? 0 : k < n ? k : n;
-                first = (k + kPage - 1) / kPage;
-                count = (n + kPage - 1) / kPage - first;
-            }
-            sums[tid] = count;
-            __syncthreads();
-            for (int s = 1; s < NT; s <<= 1) {
-                const int o = tid >= s ? sums[tid - s] : 0;
-                __syncthreads();
-                sums[tid] += o;
-                __syncthreads();
-            }
-            const int all = sums[NT - 1];
-            const int at = base + sums[tid] - count;
-            if (p.freed_pages != nullptr)
-                for (int i = 0; i < count; ++i) p.freed_pages[at + i] = p.page_table[int64_t(b) * p.max_pages_per_seq + first + i];
-            base += all;
-            __syncthreads();
+// Blocks that list the page ids behind the kept tokens: each finds every sequence's
+// place in the list, a thread each, and copies its share of the ids.  (One thread per
+// sequence took 130 us for the 1375 pages of one.)
+constexpr int kListBlocks = 8;
+
+template <int NT>
+__device__ __forceinline__ void list_freed_pages(const CompactParams& p, int block) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int start[NT + 1];        // of a sequence's ids in the list
+    __shared__ int first[NT];            // page-table entry of the first
+    __shared__ int wave_sum[NT / 64];
+    int base = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += NT) {
+        const int b = b0 + tid;
+        int count = 0;
+        if (b < p.batch) {
+            const int most = p.max_pages_per_seq * kPage;
+            int n = p.context_lens[b], k = p.kept_lens[b];
+            n = n < 0 ? 0 : n < most ? n : most;
+            k = k < 0 ? 0 : k < n ? k : n;
+            first[tid] = (k + kPage - 1) / kPage;
+            count = (n + kPage - 1) / kPage - first[tid];
         }
-        if (tid == 0) *p.freed_count = base;
-        return;
+        int sum = count;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int o = __shfl_up(sum, s);
+            if (lane >= s) sum += o;
+        }
+        if (lane == 63) wave_sum[wave] = sum;
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) sum += wave_sum[i];
+        start[tid + 1] = sum;
+        if (tid == 0) start[0] = 0;
+        __syncthreads();
+        const int all = start[NT], here = p.batch - b0 < NT ? p.batch - b0 : NT;
+        for (int i = block * NT + tid; i < all; i += kListBlocks * NT) {
+            int lo = 0, hi = here;       // the last sequence that starts at or before i
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (start[mid] <= i) lo = mid; else hi = mid;
+            }
+            p.freed_pages[base + i] = p.page_table[int64_t(b0 + lo) * p.max_pages_per_seq + first[lo] + (i - start[lo])];
+        }
+        base += all;
+        __syncthreads();
     }
-    const int b = int(blockIdx.x / unsigned(p.heads)), h = int(blockIdx.x % unsigned(p.heads));
+    if (block == 0 && tid == 0) *p.freed_count = base;
+}
+
+// Where token `to` of a (sequence, KV head) comes from.
+struct TokenMove {
+    int page, at;     // page id and place in it
+    bool moved;
+};
+__device__ __forceinline__ int kept_count(const CompactParams& p, int b) {
     const int most = p.max_pages_per_seq * kPage;
     int len = p.kept_lens[b];
     len = len < 0 ? 0 : len < p.budget ? len : p.budget;
-    len = len < most ? len : most;
-    const int32_t* kept = p.kept + int64_t(blockIdx.x) * p.budget;
-    const int32_t* table = p.page_table + int64_t(b) * p.max_pages_per_seq;
-    float* w = p.weights != nullptr ? p.weights + int64_t(blockIdx.x) * p.width : nullptr;
-    __shared__ int64_t src_tile[TOK], dst_tile[TOK];   // (page, head) index, -1: nothing to move
-    __shared__ int src_at[TOK];
-    for (int c0 = 0; c0 < len; c0 += TOK) {
-        float wv = 0.f;
-        int from = 0;
+    return len < most ? len : most;
+}
+// The page id that the tokens of page `page` of sequence b go to, or -1.
+__device__ __forceinline__ int target_page(const CompactParams& p, int b, int page) {
+    const int id = p.page_table[int64_t(b) * p.max_pages_per_seq + page];
+    return id >= 0 && int64_t(id) < p.num_pages ? id : -1;
+}
+__device__ __forceinline__ TokenMove token_move(const CompactParams& p, int row, int b, int to, int len) {
+    const int most = p.max_pages_per_seq * kPage;
+    int from = to < len ? p.kept[int64_t(row) * p.budget + to] : to;
+    from = from < to ? to : from < most ? from : most - 1;
+    TokenMove m;
+    m.moved = from != to;
+    m.at = from;
+    m.page = 0;
+    if (m.moved) {
+        const int id = p.page_table[int64_t(b) * p.max_pages_per_seq + from / kPage];
+        m.page = id >= 0 && int64_t(id) < p.num_pages ? id : 0;
+    }
+    return m;
+}
+
+// Few (sequence, KV head) pairs: a page of kept tokens per wave (two at head size 64), first
+// gathered into the workspace, then, in a launch of its own, put into place.  A lane holds a
+// 16-byte unit of the target's key tile (a token's 32 channels) and one of its value tile (4
+// tokens' 8 channels), and the scale bytes of its token; two at head size 256.
+template <int D, bool PLACE>
+__global__ void __launch_bounds__(kCompactThreads) compact_pages_kernel(CompactParams p) {
+    constexpr int LANES = D == 64 ? 32 : 64, U = D == 256 ? 2 : 1, TILES = 64 / LANES;
+    constexpr int E = D / 8;                         // value units of 4 tokens
+    const int pages = (p.budget + kPage - 1) / kPage;
+    if (!PLACE && p.freed_count != nullptr && blockIdx.x + kListBlocks >= gridDim.x) {
+        list_freed_pages<kCompactThreads>(p, int(blockIdx.x + kListBlocks - gridDim.x));
+        return;
+    }
+    const int lane = threadIdx.x & 63, l = lane & (LANES - 1), t = l & (kPage - 1);
+    const int64_t tile = (int64_t(blockIdx.x) * (kCompactThreads / 64) + (threadIdx.x >> 6)) * TILES + lane / LANES;
+    const int64_t rows = int64_t(p.batch) * p.heads;
+    if (tile >= rows * pages) return;                // whole tiles
+    const int row = int(tile / pages), j = int(tile - int64_t(row) * pages);
+    const int b = row / p.heads, h = row - b * p.heads;
+    const int len = kept_count(p, b), to = j * kPage + t;
+    uint8_t* const ws = p.workspace + tile * (17 * D);
+    float* const ws_weights = reinterpret_cast<float*>(p.workspace + rows * pages * (17 * D)) + int64_t(row) * p.budget;
+    float* const w = p.weights != nullptr ? p.weights + int64_t(row) * p.width : nullptr;
+    if constexpr (!PLACE) {
+        const TokenMove m = token_move(p, row, b, to, len);
+        if (w != nullptr && l < kPage && m.moved && m.at < p.width) ws_weights[to] = w[m.at];
+        const int64_t own = int64_t(m.page) * p.heads + h;
+        const int at = m.at & (kPage - 1);
+        u32x4 k[U], v[U];
+        uint8_t ks[U], vs[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = l + 64 * u, tq = q / E, e = q % E;
+            if (m.moved) {
+                k[u] = *reinterpret_cast<const u32x4*>(p.codes + own * (16 * D) + ((q >> 4) * kPage + at) * 16);
+                ks[u] = p.scales[own * D + (q >> 4) * kPage + at];
+                vs[u] = p.scales[own * D + D / 2 + (q >> 4) * kPage + at];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int src = (lane & ~(LANES - 1)) + 4 * tq + i;     // the lane of that token
+                const int page = __shfl(m.page, src), place = __shfl(m.moved ? at : -1, src);
+                v[u][i] = 0u;
+                if (place >= 0)
+                    v[u][i] = *reinterpret_cast<const uint32_t*>(p.codes + (int64_t(page) * p.heads + h) * (16 * D) + 8 * D +
+                                                                 ((place >> 2) * E + e) * 16 + (place & 3) * 4);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = l + 64 * u;
+            *reinterpret_cast<u32x4*>(ws + 8 * D + 16 * q) = v[u];
+            if (m.moved) {
+                *reinterpret_cast<u32x4*>(ws + 16 * q) = k[u];
+                ws[16 * D + q] = ks[u];
+                ws[16 * D + D / 2 + q] = vs[u];
+            }
+        }
+    } else {
+        const int from = to < len ? p.kept[int64_t(row) * p.budget + to] : to;
+        const int id = j * kPage < len ? target_page(p, b, j) : -1;
+        const bool moved = from > to && id >= 0;
+        const int64_t dst = int64_t(id) * p.heads + h;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int q = l + 64 * u, tq = q / E;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(ws + 8 * D + 16 * q);
+            if (moved) {
+                *reinterpret_cast<u32x4*>(p.codes + dst * (16 * D) + 16 * q) = *reinterpret_cast<const u32x4*>(ws + 16 * q);
+                p.scales[dst * D + q] = ws[16 * D + q];
+                p.scales[dst * D + D / 2 + q] = ws[16 * D + D / 2 + q];
+            }
+            int which = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) which |= __shfl(int(moved), (lane & ~(LANES - 1)) + 4 * tq + i) << i;
+            uint32_t* const out = reinterpret_cast<uint32_t*>(p.codes + dst * (16 * D) + 8 * D + 16 * q);
+            if (which == 15) {
+                *reinterpret_cast<u32x4*>(out) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (which >> i & 1) out[i] = v[i];
+            }
+        }
+        if (w != nullptr) {
+            if (l < kPage && from > to && from < p.width) w[to] = ws_weights[to];
+            // the entries behind the kept ones, spread over the row's pages
+            int n = p.context_lens[b];
+            const int most = p.max_pages_per_seq * kPage;
+            n = n < most ? n : most;
+            n = n < p.width ? n : int(p.width);
+            for (int i = len + j * LANES + l; i < n; i += pages * LANES) w[i] = 0.f;
+        }
+    }
+}
+
+// Many pairs: a block for the keys and one for the values of each, in place and in one
+// pass.  It takes kMoveTokens tokens at a time: those of the next chunk are read before this
+// one's are written, which is after all threads have read theirs.
+constexpr int kMoveThreads = 1024, kMoveTokens = 512;
+
+template <int D, bool KEYS>
+__device__ __forceinline__ void move_tokens(const CompactParams& p, int row) {
+    constexpr int NT = kMoveThreads, TOK = kMoveTokens, G = D / 32, E = D / 8;
+    constexpr int U = TOK * G / NT;                  // 16-byte units per thread, of keys or of values
+    static_assert(U * NT == TOK * G && TOK <= NT, "a thread per token, whole units per thread");
+    const int tid = threadIdx.x;
+    const int b = row / p.heads, h = row - b * p.heads;
+    const int len = kept_count(p, b);
+    float* const w = KEYS && p.weights != nullptr ? p.weights + int64_t(row) * p.width : nullptr;
+    // of the tokens of three chunks (one is found while one is read and one written): where
+    // they are, or a negative number for those that stay, and where their pages go
+    __shared__ int src_page[3][TOK], src_at[3][TOK], dst_page[3][TOK / kPage];
+    const int chunks = (len + TOK - 1) / TOK;
+    float wv = 0.f, next_wv = 0.f;
+    bool w_moved = false, next_w_moved = false;
+    auto find = [&](int chunk) {
+        next_w_moved = false;
         if (tid < TOK) {
-            const int to = c0 + tid;
-            int64_t d = -1, s = -1;
-            if (to < len) {
-                from = kept[to];
-                from = from < to ? to : from < most ? from : most - 1;
-                if (from != to) {
-                    const int sp = table[from / kPage], dp = table[to / kPage];
-                    s = (sp >= 0 && sp < p.num_pages ? int64_t(sp) : 0) * p.heads + h;
-                    d = dp >= 0 && dp < p.num_pages ? int64_t(dp) * p.heads + h : -1;
-                    if (w != nullptr && from < p.width) wv = w[from];
+            const int to = chunk * TOK + tid;
+            const TokenMove m = token_move(p, row, b, to, len);
+            src_page[chunk % 3][tid] = m.page;
+            src_at[chunk % 3][tid] = m.moved ? m.at & (kPage - 1) : -1;
+            if (w != nullptr && m.moved && m.at < p.width) {
+                next_wv = w[m.at];
+                next_w_moved = true;
+            }
+        }
+        if (tid >= NT - TOK / kPage) {   // (the last threads, which may be of those above too)
+            const int i = tid - (NT - TOK / kPage), page = chunk * (TOK / kPage) + i;
+            dst_page[chunk % 3][i] = page * kPage < len ? target_page(p, b, page) : -1;
+        }
+    };
+    u32x4 cur[U], nxt[U];
+    uint8_t cur_sc[U], nxt_sc[U];
+    // unit i of a chunk: a token's 32 channels of the keys, or 4 tokens' 8 channels of the values; and the
+    // scale byte of a token and group
+    auto load = [&](int chunk) {
+        const int* const pages = src_page[chunk % 3];
+        const int* const places = src_at[chunk % 3];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = tid + u * NT, t = i % TOK, g = i / TOK;
+            const int at = places[t];
+            const int64_t tile = int64_t(pages[t]) * p.heads + h;
+            nxt_sc[u] = 0;
+            if (at >= 0) nxt_sc[u] = p.scales[tile * D + (KEYS ? 0 : D / 2) + g * kPage + at];
+            if constexpr (KEYS) {
+                nxt[u] = u32x4{0u, 0u, 0u, 0u};
+                if (at >= 0) nxt[u] = *reinterpret_cast<const u32x4*>(p.codes + tile * (16 * D) + (g * kPage + at) * 16);
+            } else {
+                const int t4 = i / E, e = i % E;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int place = places[4 * t4 + k];
+                    nxt[u][k] = 0u;
+                    if (place >= 0)
+                        nxt[u][k] = *reinterpret_cast<const uint32_t*>(p.codes + (int64_t(pages[4 * t4 + k]) * p.heads + h) * (16 * D) +
+                                                                       8 * D + ((place >> 2) * E + e) * 16 + (place & 3) * 4);
                 }
             }
-            src_tile[tid] = s;
-            dst_tile[tid] = d;
-            src_at[tid] = from % kPage;
         }
+    };
+    auto store = [&](int chunk) {
+        const int* const places = src_at[chunk % 3];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = tid + u * NT, t = i % TOK, g = i / TOK;
+            const int id = dst_page[chunk % 3][t / kPage];
+            const int64_t tile = int64_t(id) * p.heads + h;
+            const bool moved = id >= 0 && places[t] >= 0;
+            if (moved) p.scales[tile * D + (KEYS ? 0 : D / 2) + g * kPage + t % kPage] = cur_sc[u];
+            if constexpr (KEYS) {
+                if (moved) *reinterpret_cast<u32x4*>(p.codes + tile * (16 * D) + (g * kPage + t % kPage) * 16) = cur[u];
+            } else {
+                const int t4 = i / E, e = i % E, to = dst_page[chunk % 3][t4 / 4];
+                uint32_t* const out = reinterpret_cast<uint32_t*>(p.codes + (int64_t(to) * p.heads + h) * (16 * D) + 8 * D +
+                                                                  ((t4 % 4) * E + e) * 16);
+                int which = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) which |= int(places[4 * t4 + k] >= 0) << k;
+                if (to < 0) which = 0;
+                if (which == 15) {
+                    *reinterpret_cast<u32x4*>(out) = cur[u];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (which >> k & 1) out[k] = cur[u][k];
+                }
+            }
+        }
+        if (w_moved && chunk * TOK + tid < p.width) w[chunk * TOK + tid] = wv;
+    };
+    if (chunks > 0) {
+        find(0);
         __syncthreads();
-        u32x4 kc[KR];
-        uint32_t vc[VU];
-        uint8_t sc[SR];
+        load(0);
+    }
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        wv = next_wv;
+        w_moved = next_w_moved;
 #pragma unroll
-        for (int u = 0; u < KR; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), g = i / TOK;
-            if (g < G && dst_tile[t] >= 0)
-                kc[u] = *reinterpret_cast<const u32x4*>(p.codes + src_tile[t] * (16 * D) + (g * kPage + src_at[t]) * 16);
+        for (int u = 0; u < U; ++u) {
+            cur[u] = nxt[u];
+            cur_sc[u] = nxt_sc[u];
         }
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), e = i / TOK;
-            if (dst_tile[t] >= 0)
-                vc[u] = *reinterpret_cast<const uint32_t*>(p.codes + src_tile[t] * (16 * D) + 8 * D +
-                                                           ((src_at[t] >> 2) * (D / 8) + e) * 16 + (src_at[t] & 3) * 4);
-        }
-#pragma unroll
-        for (int u = 0; u < SR; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), g = i / TOK;
-            if (g < 2 * G && dst_tile[t] >= 0) sc[u] = p.scales[src_tile[t] * D + g * kPage + src_at[t]];
-        }
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the chunk is read
+        if (chunk + 1 < chunks) find(chunk + 1);
         __syncthreads();
+        if (chunk + 1 < chunks) load(chunk + 1);
+        // what was read for this chunk has arrived, in every thread
 #pragma unroll
-        for (int u = 0; u < KR; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), g = i / TOK, a = (c0 + t) & (kPage - 1);
-            if (g < G && dst_tile[t] >= 0)
-                *reinterpret_cast<u32x4*>(p.codes + dst_tile[t] * (16 * D) + (g * kPage + a) * 16) = kc[u];
-        }
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), e = i / TOK, a = (c0 + t) & (kPage - 1);
-            if (dst_tile[t] >= 0)
-                *reinterpret_cast<uint32_t*>(p.codes + dst_tile[t] * (16 * D) + 8 * D + ((a >> 2) * (D / 8) + e) * 16 + (a & 3) * 4) = vc[u];
-        }
-#pragma unroll
-        for (int u = 0; u < SR; ++u) {
-            const int i = tid + u * NT, t = i & (TOK - 1), g = i / TOK, a = (c0 + t) & (kPage - 1);
-            if (g < 2 * G && dst_tile[t] >= 0) p.scales[dst_tile[t] * D + g * kPage + a] = sc[u];
-        }
-        if (w != nullptr && tid < TOK && c0 + tid < len && from != c0 + tid && c0 + tid < p.width) w[c0 + tid] = wv;
+        for (int u = 0; u < U; ++u) asm volatile("" ::"v"(cur[u][0]), "v"(cur[u][1]), "v"(cur[u][2]), "v"(cur[u][3]), "v"(uint32_t(cur_sc[u])));
+        asm volatile("" ::"v"(wv));
         __syncthreads();
+        store(chunk);
     }
     if (w != nullptr) {
+        // every weight has been read
+        __syncthreads();
+        const int most = p.max_pages_per_seq * kPage;
         int n = p.context_lens[b];
         n = n < most ? n : most;
-        n = n < p.width ? n : p.width;
+        n = n < p.width ? n : int(p.width);
         for (int t = len + tid; t < n; t += NT) w[t] = 0.f;
     }
 }
 
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) compact_rows_kernel(CompactParams p) {
+    const unsigned blocks = 2u * unsigned(p.batch * p.heads);
+    if (blockIdx.x >= blocks) {
+        list_freed_pages<kMoveThreads>(p, int(blockIdx.x - blocks));
+        return;
+    }
+    if (blockIdx.x & 1u) move_tokens<D, false>(p, int(blockIdx.x >> 1));
+    else move_tokens<D, true>(p, int(blockIdx.x >> 1));
+}
+
+template <int D>
+static void launch_compact_kv_d(const CompactParams& p, hipStream_t stream) {
+    const dim3 block{unsigned(kCompactThreads)};
+    const unsigned list = p.freed_count != nullptr ? kListBlocks : 0u;
+    if (p.workspace == nullptr) {
+        hipLaunchKernelGGL(compact_rows_kernel<D>, dim3(2u * unsigned(p.batch * p.heads) + list), dim3(unsigned(kMoveThreads)), 0, stream, p);
+        return;
+    }
+    constexpr int TILES = (D == 64 ? 2 : 1) * kCompactThreads / 64;
+    const int64_t tiles = int64_t(p.batch) * p.heads * ((p.budget + kPage - 1) / kPage);
+    const unsigned blocks = unsigned((tiles + TILES - 1) / TILES);
+    hipLaunchKernelGGL((compact_pages_kernel<D, false>), dim3(blocks + list), block, 0, stream, p);
+    if (blocks > 0) hipLaunchKernelGGL((compact_pages_kernel<D, true>), dim3(blocks), block, 0, stream, p);
+}
+
 hipError_t launch_compact_kv(const CompactParams& p, hipStream_t stream) {
-    const dim3 grid{unsigned(p.batch * p.heads) + (p.freed_count != nullptr ? 1u : 0u)}, block{unsigned(kCompactThreads)};
-    if (p.head_dim == 64) hipLaunchKernelGGL(compact_kv_kernel<64>, grid, block, 0, stream, p);
-    else if (p.head_dim == 128) hipLaunchKernelGGL(compact_kv_kernel<128>, grid, block, 0, stream, p);
-    else hipLaunchKernelGGL(compact_kv_kernel<256>, grid, block, 0, stream, p);
+    if (p.head_dim == 64) launch_compact_kv_d<64>(p, stream);
+    else if (p.head_dim == 128) launch_compact_kv_d<128>(p, stream);
+    else launch_compact_kv_d<256>(p, stream);
     return hipGetLastError();
 }
 

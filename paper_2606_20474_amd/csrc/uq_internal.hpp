@@ -235,11 +235,11 @@ struct WeightsParams {
     int64_t width;
     int32_t by_seq;            // rows are numbered by sequence, `last` queries each (else by token row)
     int64_t rows_per_head;     // of that numbering
-    int32_t row_units;         // 16-row units a wave of the norms holds
-    int32_t chunk;             // tokens a wave of the norms walks
+    int32_t few;               // few_rows_kernel for both, else token_norms_kernel and token_sums_kernel
+    int32_t row_units;         // 16-row units a wave holds
+    int32_t chunk;             // tokens a wave walks
     int32_t chunks;            // of the longest context
-    int32_t key_units;         // key units a wave of the sums holds
-    int32_t row_split;         // rows a wave of the sums walks, a multiple of 16
+    int32_t row_split;         // many rows: rows a wave of the sums walks, a multiple of 16
     int32_t splits;            // of a sequence with the most rows
     int32_t norm_blocks;
     int32_t sum_blocks;
@@ -261,7 +261,12 @@ struct SelectParams {
     int32_t recent;
     int32_t* kept;             // [batch][heads][budget]
     int32_t* kept_lens;        // [batch]
+    int32_t slices;            // of the longest row; 1: a block per row does it all
+    uint8_t* workspace;        // slices > 1: kSelectSliceBytes for each slice of each row, then 16 for each row
 };
+constexpr int kSelectSlice = 16384;      // tokens of a slice, 16 per thread
+constexpr int kSelectList = 4096;        // candidates of a slice that are listed
+constexpr int kSelectSliceBytes = (2048 + kSelectList + 4) * 4;   // its first counts, its candidates, their number and that of the sure ones
 hipError_t launch_select_tokens(const SelectParams& p, hipStream_t stream);
 
 struct CompactParams {
@@ -281,6 +286,8 @@ struct CompactParams {
     int64_t width;
     int32_t* freed_pages;      // nullptr: not wanted
     int32_t* freed_count;
+    uint8_t* workspace;        // [batch][heads][pages of the budget][17 d], then weights [batch][heads][budget]; nullptr: in
+                               // one pass
 };
 hipError_t launch_compact_kv(const CompactParams& p, hipStream_t stream);
 

@@ -5,21 +5,10 @@
 // r / G, head r % G.  Its scores s_t over the visible tokens give the softmax
 // weights p_t = 2^(c s_t - m) / l, c = scale log2 e, and token t gets the sum of
 // its weights over all rows.  Weights of different rows add up only when they are
-// normalised, so the keys are read twice:
-//
-//   token_norms   m and l of every row.  A wave holds 16 NB rows as operand B and
-//                 walks the tokens of a chunk; keys are operand A, so a lane sees
-//                 4 tokens of one row and needs no exchange until the end.
-//   token_sums    the sums.  A wave holds P units of keys as operand B and walks
-//                 the rows, which are operand A: a lane sees 4 rows of one token
-//                 and adds in its register.
-//
-// A page's key tile is [channels / 32][token][16 bytes], which is operand order of
-// v_mfma_scale_f32_16x16x128_f8f6f4 (lane: token l % 16, 32 channels l / 16), and so
-// are its scale bytes: keys go from memory to the matrix instruction with one
-// 16-byte load per lane and no LDS.  FP8 query rows are two such loads.  Head size
-// 64 takes two pages into one operand and half of the query operand is zero; head
-// size 256 takes two instructions per page.
+// normalised, so the keys are read twice: first for m and l of every row, then for
+// the sums.  m is no maximum but the largest score of the first tokens a lane sees: in
+// fp32 any reference serves that keeps 2^(c s - m) in range, so it is moved only
+// when a sum has passed 2^96.
 //
 // Every sum has a fixed order: results do not depend on what else runs.
 #pragma once
@@ -31,49 +20,34 @@ namespace uq {
 
 constexpr float kNoRow = -1e30f;      // reference of a row that has seen no token
 constexpr float kMaskedRow = 3e38f;   // reference that makes every weight 0
-constexpr float kRefSlack = 8.0f;     // powers of two a score may pass the reference
+constexpr float kMostSum = 0x1p96f;   // sum at which the reference moves
 constexpr float kBigRef = 0x1p20f;    // from here on c s is rounded before the reference is taken off
 
-// Keys of 16 tokens (32 at head size 64) as operand bytes.
+// Keys of a page as operand bytes.
 template <int D> struct KeyUnit {
     static constexpr int kSteps = D == 256 ? 2 : 1;
-    static constexpr int kPages = D == 64 ? 2 : 1;
-    static constexpr int kTiles = kPages;            // 16x16 results per 16 rows
-    static constexpr int kTokens = kPage * kPages;
     u32x4 code[kSteps];
     int scale[kSteps];
 };
 
 // 16 rows of FP8 queries as operand bytes.
 template <int D> struct RowUnit {
-    u32x4 lo[D == 256 ? 2 : 1], hi[D == 64 ? 1 : D == 256 ? 2 : 1];
+    u32x4 lo[D == 256 ? 2 : 1], hi[D == 256 ? 2 : 1];
 };
 
 __device__ __forceinline__ v8i join_halves(const u32x4& a, const u32x4& b) {
     return v8i{int(a[0]), int(a[1]), int(a[2]), int(a[3]), int(b[0]), int(b[1]), int(b[2]), int(b[3])};
 }
 
-// The row operand of result tile `tile` and step `s`.
-template <int D>
-__device__ __forceinline__ v8i row_operand(const RowUnit<D>& q, int tile, int s) {
-    const u32x4 none = {0u, 0u, 0u, 0u};
-    if constexpr (D == 64) return tile == 0 ? join_halves(q.lo[0], none) : join_halves(none, q.lo[0]);
-    else return join_halves(q.lo[s], q.hi[s]);
-}
-template <int D>
-__device__ __forceinline__ v8i key_operand(const KeyUnit<D>& k, int s) {
-    const u32x4 none = {0u, 0u, 0u, 0u};
-    return join_halves(k.code[s], none);
-}
-
-// Scores of 16 tokens (tile of the unit) against 16 rows: result row = token,
-// column = row (TOKEN_ROWS), or the other way round.
+// Scores of 16 tokens against 16 rows: result row = token, column = row (TOKEN_ROWS),
+// or the other way round.
 template <int D, bool TOKEN_ROWS>
-__device__ __forceinline__ v4f unit_scores(const KeyUnit<D>& k, const RowUnit<D>& q, int tile) {
+__device__ __forceinline__ v4f unit_scores(const KeyUnit<D>& k, const RowUnit<D>& q) {
+    const u32x4 none = {0u, 0u, 0u, 0u};
     v4f s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < KeyUnit<D>::kSteps; ++i) {
-        const v8i ko = key_operand<D>(k, i), qo = row_operand<D>(q, tile, i);
+        const v8i ko = join_halves(k.code[i], none), qo = join_halves(q.lo[i], q.hi[i]);
         if constexpr (TOKEN_ROWS)
             s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ko, qo, s, 4, 0, 0, k.scale[i], 0, 127);
         else
@@ -144,32 +118,46 @@ struct ItemFinder {
     }
 };
 
-// Page ids of a sequence, 64 at a time.
+// Page ids of a walk over ascending pages, 64 at a time, the next 64 on their way.
 struct PageIds {
-    int ids = 0, from = -1;
-    __device__ __forceinline__ void load(const WeightsParams& p, int b, int page, int pages) {
+    const int32_t* row;
+    int64_t num_pages;
+    int pages, from, ids, next;
+    __device__ __forceinline__ int fetch(int page) const {
         const int i = page + int(threadIdx.x & 63);
-        from = page;
-        ids = p.page_table[int64_t(b) * p.max_pages_per_seq + (i < pages ? i : pages - 1)];
-        ids = ids >= 0 && int64_t(ids) < p.num_pages ? ids : 0;
+        return row[i < pages ? i : pages - 1];
     }
-    __device__ __forceinline__ int at(int page) const { return __builtin_amdgcn_readlane(ids, page - from); }
+    __device__ __forceinline__ PageIds(const WeightsParams& p, int b, int page, int n)
+        : row(p.page_table + int64_t(b) * p.max_pages_per_seq), num_pages(p.num_pages), pages((n + kPage - 1) / kPage), from(page) {
+        ids = fetch(page);
+        next = fetch(page + 64);
+    }
+    // (a page id outside the pool reads page 0)
+    __device__ __forceinline__ int at(int page) {
+        if (page >= from + 64) {
+            from += 64;
+            ids = next;
+            next = fetch(from + 64);
+        }
+        const int id = __builtin_amdgcn_readlane(ids, page - from);
+        return id >= 0 && int64_t(id) < num_pages ? id : 0;
+    }
 };
 
-// Unit `u` of a sequence (its pages among the loaded ids): tokens at n and behind
-// may never have been written, and their scale bytes become 0.
+// The keys of page `id`.  At head size 64 they fill half of an operand, and the other
+// half is 0.
 template <int D>
-__device__ __forceinline__ void load_keys(const WeightsParams& p, const PageIds& ids, int hk, int u, int pages, KeyUnit<D>& k) {
-    const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void load_keys(const WeightsParams& p, int id, int hk, KeyUnit<D>& k) {
+    const unsigned lane = threadIdx.x & 63u;
+    const int64_t ph = int64_t(id) * p.num_kv_heads + hk;
+    const uint8_t* codes = p.codes + ph * (16 * D);
+    const uint8_t* scales = p.scales + ph * D;
     if constexpr (D == 64) {
-        const int a = ids.at(2 * u), c = ids.at(2 * u + 1 < pages ? 2 * u + 1 : 2 * u);
-        const int64_t ph = int64_t(lane < 32 ? a : c) * p.num_kv_heads + hk;
-        k.code[0] = *reinterpret_cast<const u32x4*>(p.codes + ph * (16 * D) + 16 * (lane & 31));
-        k.scale[0] = p.scales[ph * D + (lane & 31)];
+        const u32x4 none = {0u, 0u, 0u, 0u};
+        const u32x4 x = *reinterpret_cast<const u32x4*>(codes + 16 * (lane & 31));
+        k.code[0] = lane < 32 ? x : none;
+        k.scale[0] = scales[lane & 31];
     } else {
-        const int64_t ph = int64_t(ids.at(u)) * p.num_kv_heads + hk;
-        const uint8_t* codes = p.codes + ph * (16 * D);
-        const uint8_t* scales = p.scales + ph * D;
 #pragma unroll
         for (int i = 0; i < KeyUnit<D>::kSteps; ++i) {
             k.code[i] = *reinterpret_cast<const u32x4*>(codes + 1024 * i + 16 * lane);
@@ -177,12 +165,12 @@ __device__ __forceinline__ void load_keys(const WeightsParams& p, const PageIds&
         }
     }
 }
+// Tokens at n and behind may never have been written: their scale bytes become 0.
 template <int D>
-__device__ __forceinline__ void hide_unwritten(KeyUnit<D>& k, int u, int n) {
-    const int lane = threadIdx.x & 63;
-    const int t = u * KeyUnit<D>::kTokens + (D == 64 ? (lane >> 5) * kPage : 0) + (lane & 15);
+__device__ __forceinline__ void hide_unwritten(KeyUnit<D>& k, int page, int n) {
+    const bool written = page * kPage + int(threadIdx.x & 15) < n;
 #pragma unroll
-    for (int i = 0; i < KeyUnit<D>::kSteps; ++i) k.scale[i] = t < n ? k.scale[i] : 0;
+    for (int i = 0; i < KeyUnit<D>::kSteps; ++i) k.scale[i] = written ? k.scale[i] : 0;
 }
 
 // The row that this lane holds of the 16 from r0 on, clamped to the last.
@@ -193,11 +181,11 @@ __device__ __forceinline__ void load_rows(const WeightsParams& p, const WeightsS
     r = r < rows ? r : rows - 1;
     const int i = weights_div(p, r);
     const uint8_t* at = p.q + int64_t(s.first + i) * p.q_stride + int64_t(hk * p.group + r - i * p.group) * D + 16 * (lane >> 4);
-    q.lo[0] = *reinterpret_cast<const u32x4*>(at);
-    if constexpr (D >= 128) q.hi[0] = *reinterpret_cast<const u32x4*>(at + 64);
-    if constexpr (D == 256) {
-        q.lo[1] = *reinterpret_cast<const u32x4*>(at + 128);
-        q.hi[1] = *reinterpret_cast<const u32x4*>(at + 192);
+#pragma unroll
+    for (int st = 0; st < KeyUnit<D>::kSteps; ++st) {
+        q.lo[st] = *reinterpret_cast<const u32x4*>(at + 128 * st);
+        if constexpr (D >= 128) q.hi[st] = *reinterpret_cast<const u32x4*>(at + 128 * st + 64);
+        else q.hi[st] = q.lo[st];   // (against keys of 0)
     }
 }
 
@@ -207,15 +195,338 @@ __device__ __forceinline__ float above_ref(float s, float c, float m, bool big) 
     return big ? s * c - m : __builtin_fmaf(s, c, -m);
 }
 
-// Row blocks of 16 NB rows times chunks of p.chunk tokens, a wave each: the row's
-// reference and sum over the chunk, or (one chunk) the reference and 1 / sum.
+// 4 scores of a row, added to its sum relative to a reference that moves up to them.
+__device__ __forceinline__ void add_moving(const v4f& x, float c, float& m, float& l) {
+    const float mx = __builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])) * c;
+    if (mx > m) {
+        l *= __builtin_amdgcn_exp2f(m - mx);
+        m = mx;
+    }
+    // (nothing seen yet: -inf - -1e30 is -inf still)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l += __builtin_amdgcn_exp2f(above_ref(x[i], c, m, true));
+}
+
+// A row's parts in the four lane groups into one, and where it goes: the chunk's
+// reference and sum, or (one chunk) the reference and 1 / sum.
+__device__ __forceinline__ void store_norm(const WeightsParams& p, float m, float l, int chunk, int64_t row, bool real) {
+#pragma unroll
+    for (int x = 16; x < 64; x <<= 1) {
+        const float mo = __shfl_xor(m, x), lo = __shfl_xor(l, x);
+        const float top = __builtin_fmaxf(m, mo);
+        l = l * __builtin_amdgcn_exp2f(m - top) + lo * __builtin_amdgcn_exp2f(mo - top);
+        m = top;
+    }
+    if (!real) return;
+    if (p.chunks > 1) {
+        *reinterpret_cast<float2*>(p.parts + 2 * (int64_t(chunk) * p.rows_per_head * p.num_kv_heads + row)) = make_float2(m, l);
+    } else {
+        p.ref[row] = l > 0.f ? m : kMaskedRow;
+        p.inv[row] = l > 0.f ? 1.0f / l : 0.f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows (a decode step, the last queries of a prompt): bound by the keys'
+// bytes.  A wave holds 16 NB rows and streams the keys of a chunk past them, four
+// pages computed while the next four are on their way, for the norms (keys as operand
+// A: a lane sees 4 tokens of one row) and again for the sums (rows as operand A: 4 rows
+// of one token).  There is time to multiply in BF16, which holds FP8 queries and FP4 keys
+// with their scales exactly, and whose products are summed to 2^-21 of the largest
+// where the scaled FP4 x FP8 instruction keeps 2^-12.5: few rows do not average that
+// out.  The k index of a step is free: lane group g takes the channels that it loads
+// in one piece of the page's tile.
+
+// A lane's piece of 16 keys: D / 32 dwords of 8 codes, and their scales.
+template <int D> struct FewKeys {
+    uint32_t code[D / 32];
+    int scale[D == 256 ? 2 : 1];
+};
+
+template <int D>
+__device__ __forceinline__ void load_few(const WeightsParams& p, int id, int hk, FewKeys<D>& k) {
+    const int lane = threadIdx.x & 63;
+    const int64_t ph = int64_t(id) * p.num_kv_heads + hk;
+    const uint8_t* codes = p.codes + ph * (16 * D);
+    const uint8_t* scales = p.scales + ph * D;
+    if constexpr (D == 64) {
+        // 16 channels: half of a group's 16 bytes
+        const int at = (lane >> 5) * kPage + (lane & 15);
+        const uint2 c = *reinterpret_cast<const uint2*>(codes + 16 * at + 8 * ((lane >> 4) & 1));
+        k.code[0] = c.x;
+        k.code[1] = c.y;
+        k.scale[0] = scales[at];
+    } else {
+#pragma unroll
+        for (int i = 0; i < D / 128; ++i) {
+            const u32x4 c = *reinterpret_cast<const u32x4*>(codes + 1024 * i + 16 * lane);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) k.code[4 * i + w] = c[w];
+            k.scale[i] = scales[64 * i + lane];
+        }
+    }
+}
+
+// Rows in operand order: the 8 channels of step s are those of dword s of the keys.
+template <int D> struct FewRows {
+    v8bf q[D / 32];
+};
+template <int D>
+__device__ __forceinline__ void load_few_rows(const WeightsParams& p, const WeightsSeq& s, int hk, int r0, int rows, FewRows<D>& q) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    int r = r0 + (lane & 15);
+    r = r < rows ? r : rows - 1;
+    const int i = weights_div(p, r);
+    const uint8_t* at = p.q + int64_t(s.first + i) * p.q_stride + int64_t(hk * p.group + r - i * p.group) * D;
+    auto convert = [&](int step, const uint2& w) {
+        const uint32_t d[2] = {w.x, w.y};
+        v8bf o;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(int(d[h]), false), b = __builtin_amdgcn_cvt_pk_f32_fp8(int(d[h]), true);
+            o[4 * h] = __bf16(a[0]);
+            o[4 * h + 1] = __bf16(a[1]);
+            o[4 * h + 2] = __bf16(b[0]);
+            o[4 * h + 3] = __bf16(b[1]);
+        }
+        q.q[step] = o;
+    };
+#pragma unroll
+    for (int st = 0; st < D / 32; ++st) {
+        const int c = D == 64 ? 16 * g + 8 * st : 128 * (st / 4) + 32 * g + 8 * (st % 4);
+        convert(st, *reinterpret_cast<const uint2*>(at + c));
+    }
+}
+
+// The keys as BF16 operands; `t`: the lane's token, at n and behind never written.
+template <int D>
+__device__ __forceinline__ void decode_few(const FewKeys<D>& k, bool written, v8bf (&o)[D / 32]) {
+#pragma unroll
+    for (int st = 0; st < D / 32; ++st) {
+        const float sc = bits_f32(uint32_t(written ? k.scale[st / 4] : 0) << 23);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            v2bf x;
+            if (h == 0) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k.code[st], sc, 0);
+            else if (h == 1) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k.code[st], sc, 1);
+            else if (h == 2) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k.code[st], sc, 2);
+            else x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(k.code[st], sc, 3);
+            o[st][2 * h] = x[0];
+            o[st][2 * h + 1] = x[1];
+        }
+    }
+}
+
+template <int D, bool TOKEN_ROWS>
+__device__ __forceinline__ v4f few_scores(const v8bf (&k)[D / 32], const FewRows<D>& q) {
+    v4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < D / 32; ++st)
+        s = TOKEN_ROWS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st], q.q[st], s, 0, 0, 0)
+                       : __builtin_amdgcn_mfma_f32_16x16x32_bf16(q.q[st], k[st], s, 0, 0, 0);
+    return s;
+}
+
+// Four values per lane, one for each of four results whose columns are the lanes' low
+// four bits: the sum of the i-th over the lane groups, in lane group i.
+__device__ __forceinline__ float sum_groups(float a, float b, float c, float d) {
+    auto add32 = [](float x, float y) {
+        const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(x), f32_bits(y), false, false);
+        return bits_f32(r[0]) + bits_f32(r[1]);
+    };
+    const float x = add32(a, c), y = add32(b, d);
+    const auto r = __builtin_amdgcn_permlane16_swap(f32_bits(x), f32_bits(y), false, false);
+    return bits_f32(r[0]) + bits_f32(r[1]);
+}
+
+template <int D, int NB, bool SUMS>
+__global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
+    constexpr int PF = 4;
+    const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
+    const int waves = int(gridDim.x) * 4;
+    const float c = p.scale_log2;
+    auto blocks_of = [&](const WeightsSeq& s) { return (s.use * p.group + 16 * NB - 1) / (16 * NB); };
+    // a chunk's wave takes one row block for the norms, all of them for the sums
+    auto count = [&](const WeightsSeq& s) {
+        const int blocks = blocks_of(s);
+        return p.num_kv_heads * (SUMS && blocks > 1 ? 1 : blocks) * ((s.n + p.chunk - 1) / p.chunk);
+    };
+    ItemFinder items;
+    int b, idx;
+    WeightsSeq s;
+    for (int at = int(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); items.find(p, at, count, b, idx, s);
+         at += waves) {
+        const int rows = s.use * p.group, blocks = blocks_of(s), chunks = (s.n + p.chunk - 1) / p.chunk;
+        const int rest = SUMS ? idx : idx / blocks;
+        const int hk = rest / chunks, chunk = rest - hk * chunks;
+        const int pos0 = first_position(p, s);
+        for (int rb = SUMS ? 0 : idx - rest * blocks, last = SUMS ? blocks : rb + 1; rb < last; ++rb) {
+            const int r0 = rb * (16 * NB);
+            const int r1 = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;     // the block's last row
+            const int lo = p.causal ? pos0 + weights_div(p, r0) : pos0, hi = p.causal ? pos0 + weights_div(p, r1) : pos0;
+            FewRows<D> q[NB];
+            float m[SUMS ? 1 : NB], l[SUMS ? 1 : NB], ref[SUMS ? NB : 1][4], inv[SUMS ? NB : 1][4];
+            int pos[SUMS ? 1 : NB];
+            bool big = false;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                load_few_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
+                if constexpr (SUMS) {
+                    const int64_t at_row = first_row(p, b, s, hk) + r0 + 16 * j + 4 * grp;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool real = r0 + 16 * j + 4 * grp + i < rows;
+                        ref[j][i] = real ? p.ref[at_row + i] : kMaskedRow;
+                        inv[j][i] = real ? p.inv[at_row + i] : 0.f;
+                        big = big | (real & (__builtin_fabsf(ref[j][i]) >= kBigRef));
+                    }
+                } else {
+                    const int r = r0 + 16 * j + col < rows ? r0 + 16 * j + col : rows - 1;
+                    pos[j] = p.causal ? pos0 + weights_div(p, r) : pos0;
+                    m[j] = kNoRow;
+                    l[j] = 0.f;
+                }
+            }
+            big = __builtin_amdgcn_ballot_w64(big) != 0;
+            // pages of the chunk up to the last that a row of the block sees
+            const int u0 = chunk * (p.chunk / kPage);
+            int u1 = hi >= 0 ? hi / kPage + 1 : 0;
+            u1 = u1 < u0 + p.chunk / kPage ? u1 : u0 + p.chunk / kPage;
+            // the norms of one page: `moving`, the reference follows
+            auto norms_of = [&](const FewKeys<D>& k, int u, bool moving) {
+                v8bf ko[D / 32];
+                decode_few<D>(k, u * kPage + col < s.n, ko);
+                const bool edge = u * kPage + kPage - 1 > lo;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    v4f x = few_scores<D, true>(ko, q[j]);
+                    if (edge) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = u * kPage + 4 * grp + i <= pos[j] ? x[i] : -__builtin_inff();
+                    }
+                    if (moving) {
+                        add_moving(x, c, m[j], l[j]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) l[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m[j]));
+                    }
+                }
+            };
+            auto find_big = [&]() {
+                bool any = false;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) any = any | ((__builtin_fabsf(m[j]) >= kBigRef) & (m[j] != kNoRow));
+                big = __builtin_amdgcn_ballot_w64(any) != 0;
+            };
+            // the weights of one page's tokens, summed over this lane's rows
+            auto sums_of = [&](const FewKeys<D>& k, int u) {
+                v8bf ko[D / 32];
+                const int t = u * kPage + col;
+                decode_few<D>(k, t < s.n, ko);
+                float sum = 0.f;
+                if (u * kPage + kPage - 1 > lo || big) {
+                    const int i0 = t - pos0;
+                    const int seen = !p.causal || i0 <= 0 ? 0 : (i0 < s.use ? i0 : s.use) * p.group;   // the first row that sees it
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const v4f x = few_scores<D, false>(ko, q[j]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float e = __builtin_amdgcn_exp2f(above_ref(x[i], c, ref[j][i], big));
+                            sum = __builtin_fmaf(r0 + 16 * j + 4 * grp + i >= seen ? e : 0.f, inv[j][i], sum);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const v4f x = few_scores<D, false>(ko, q[j]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            sum = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -ref[j][i])), inv[j][i], sum);
+                    }
+                }
+                return sum;
+            };
+            float* const out = p.weights + (int64_t(b) * p.num_kv_heads + hk) * p.width;
+            if (u0 < u1) {
+                PageIds ids(p, b, u0, s.n);
+                FewKeys<D> cur[PF], nxt[PF];
+#pragma unroll
+                for (int i = 0; i < PF; ++i) load_few<D>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
+                if constexpr (!SUMS) {
+                    // a lane that sees a token of the chunk sees one in its first page, or no later one
+                    norms_of(cur[0], u0, true);
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) l[j] = 0.f;
+                    find_big();
+                }
+                for (int u = u0; u < u1; u += PF) {
+                    float before = 0.f;
+                    const int t = u * kPage + lane;
+                    if (SUMS && t < s.n) before = out[t];
+#pragma unroll
+                    for (int i = 0; i < PF; ++i) load_few<D>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
+                    if constexpr (SUMS) {
+                        float sum[PF];
+#pragma unroll
+                        for (int i = 0; i < PF; ++i) sum[i] = sums_of(cur[i], u + i);
+                        before += sum_groups(sum[0], sum[1], sum[2], sum[3]);
+                        if (t < s.n) out[t] = before;
+                    } else {
+                        float l0[NB];
+                        bool past = big;
+#pragma unroll
+                        for (int j = 0; j < NB; ++j) l0[j] = l[j];
+                        if (!big) {
+#pragma unroll
+                            for (int i = 0; i < PF; ++i) norms_of(cur[i], u + i, false);
+                            bool over = false;
+#pragma unroll
+                            for (int j = 0; j < NB; ++j) over = over | !(l[j] <= kMostSum);
+                            past = __builtin_amdgcn_ballot_w64(over) != 0;
+                        }
+                        if (__builtin_expect(past, 0)) {
+#pragma unroll
+                            for (int j = 0; j < NB; ++j) l[j] = l0[j];
+#pragma unroll
+                            for (int i = 0; i < PF; ++i) norms_of(cur[i], u + i, true);
+                            find_big();
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < PF; ++i) cur[i] = nxt[i];
+                }
+            }
+            if constexpr (!SUMS) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const int r = r0 + 16 * j + lane;
+                    store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (a prompt's): bound by the exponentials.  For the norms a wave holds 16 NB
+// rows as operand B and walks the tokens of a chunk; for the sums it holds P units of keys
+// as operand B and walks the rows.  A page's key tile is [channels / 32][token][16
+// bytes], which is operand order of v_mfma_scale_f32_16x16x128_f8f6f4 (lane: token l
+// % 16, 32 channels l / 16), and so are its scale bytes: keys go from memory to the
+// matrix instruction with one 16-byte load per lane and no LDS.  FP8 query rows are
+// two such loads.  At head size 64 half of the operands is 0, head size 256 takes two
+// instructions per page.
+
+// Row blocks of 16 NB rows times chunks of p.chunk tokens, a wave each.
 template <int D, int NB>
-__global__ void __launch_bounds__(256) token_norms_kernel(WeightsParams p) {
+__global__ void __launch_bounds__(256, 2) token_norms_kernel(WeightsParams p) {
     using Unit = KeyUnit<D>;
-    constexpr int TOK = Unit::kTokens, PF = 4;
+    constexpr int PF = 2;   // pages computed while as many are on their way (the slow path counts on 2)
     const int lane = threadIdx.x & 63, grp = lane >> 4;
     const int waves = int(gridDim.x) * 4;
-    const int units_per_chunk = p.chunk / TOK;
+    const int pages_per_chunk = p.chunk / kPage;
+    const float c = p.scale_log2;
     auto count = [&](const WeightsSeq& s) {
         const int rows = s.use * p.group;
         return p.num_kv_heads * ((rows + 16 * NB - 1) / (16 * NB)) * ((s.n + p.chunk - 1) / p.chunk);
@@ -231,104 +542,92 @@ __global__ void __launch_bounds__(256) token_norms_kernel(WeightsParams p) {
         const int pos0 = first_position(p, s);
         const int r1 = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;     // the block's last row
         const int lo = p.causal ? pos0 + weights_div(p, r0) : pos0, hi = p.causal ? pos0 + weights_div(p, r1) : pos0;
+        // pages of the chunk up to the last that a row of the block sees
+        const int u0 = chunk * pages_per_chunk;
+        int u1 = hi >= 0 ? hi / kPage + 1 : 0;
+        u1 = u1 < u0 + pages_per_chunk ? u1 : u0 + pages_per_chunk;
         RowUnit<D> q[NB];
         float m[NB], l[NB];
-        int pos[NB];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            load_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
-            const int r = r0 + 16 * j + (lane & 15) < rows ? r0 + 16 * j + (lane & 15) : rows - 1;
-            pos[j] = p.causal ? pos0 + weights_div(p, r) : pos0;
+            if (u0 < u1) load_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
             m[j] = kNoRow;
             l[j] = 0.f;
         }
-        // units of the chunk up to the last that a row of the block sees
-        const int u0 = chunk * units_per_chunk;
-        int u1 = hi >= 0 ? hi / TOK + 1 : 0;
-        u1 = u1 < u0 + units_per_chunk ? u1 : u0 + units_per_chunk;
-        const int pages = (s.n + kPage - 1) / kPage;
         bool big = false;
-        auto use_unit = [&](const Unit& k, int u) {
+        // a page whose tokens need not all be seen, or whose scores may be far from the reference
+        auto use_moving = [&](const Unit& k, int u) {
 #pragma unroll
-            for (int t = 0; t < Unit::kTiles; ++t) {
-                const int t0 = u * TOK + kPage * t;
-                v4f x[NB];
-                bool up = false;
+            for (int j = 0; j < NB; ++j) {
+                v4f x = unit_scores<D, true>(k, q[j]);
+                const int r = r0 + 16 * j + (lane & 15) < rows ? r0 + 16 * j + (lane & 15) : rows - 1;
+                const int pos = p.causal ? pos0 + weights_div(p, r) : pos0;
 #pragma unroll
-                for (int j = 0; j < NB; ++j) x[j] = unit_scores<D, true>(k, q[j], t);
-                if (t0 + kPage - 1 > lo) {
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[j][i] = t0 + 4 * grp + i <= pos[j] ? x[j][i] : -__builtin_inff();
-                }
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const float mx = __builtin_fmaxf(__builtin_fmaxf(x[j][0], x[j][1]), __builtin_fmaxf(x[j][2], x[j][3]));
-                    up = up || mx * p.scale_log2 > m[j] + kRefSlack;
-                }
-                if (__builtin_amdgcn_ballot_w64(up) != 0) {
-                    big = false;
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) {
-                        const float mx = __builtin_fmaxf(__builtin_fmaxf(x[j][0], x[j][1]), __builtin_fmaxf(x[j][2], x[j][3])) * p.scale_log2;
-                        if (mx > m[j] + kRefSlack) {
-                            l[j] *= __builtin_amdgcn_exp2f(m[j] - mx);
-                            m[j] = mx;
-                        }
-                        big = big || __builtin_amdgcn_ballot_w64(__builtin_fabsf(m[j]) >= kBigRef && m[j] != kNoRow) != 0;
-                    }
-                }
-                // (a row that has seen nothing yet: -inf - -1e30 is -inf still)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) l[j] += __builtin_amdgcn_exp2f(above_ref(x[j][i], p.scale_log2, m[j], big));
+                for (int i = 0; i < 4; ++i) x[i] = u * kPage + 4 * grp + i <= pos ? x[i] : -__builtin_inff();
+                add_moving(x, c, m[j], l[j]);
             }
         };
-        for (int u = u0; u < u1;) {
-            // up to 64 pages' ids at once
-            PageIds ids;
-            ids.load(p, b, u * Unit::kPages, pages);
-            const int end = u + 64 / Unit::kPages < u1 ? u + 64 / Unit::kPages : u1;
+        auto find_big = [&]() {
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) any = any | ((__builtin_fabsf(m[j]) >= kBigRef) & (m[j] != kNoRow));
+            big = __builtin_amdgcn_ballot_w64(any) != 0;
+        };
+        if (u0 < u1) {
+            PageIds ids(p, b, u0, s.n);
             Unit cur[PF], nxt[PF];
 #pragma unroll
-            for (int i = 0; i < PF; ++i) load_keys<D>(p, ids, hk, u + i < end ? u + i : end - 1, pages, cur[i]);
-            for (; u < end; u += PF) {
+            for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
+            // a lane that sees a token of the chunk sees one in its first page, or no later one
+            hide_unwritten<D>(cur[0], u0, s.n);
+            use_moving(cur[0], u0);
 #pragma unroll
-                for (int i = 0; i < PF; ++i) load_keys<D>(p, ids, hk, u + PF + i < end ? u + PF + i : end - 1, pages, nxt[i]);
+            for (int j = 0; j < NB; ++j) l[j] = 0.f;
+            find_big();
+            for (int u = u0; u < u1; u += PF) {
 #pragma unroll
-                for (int i = 0; i < PF; ++i) {
-                    if (u + i < end) {
-                        hide_unwritten<D>(cur[i], u + i, s.n);
-                        use_unit(cur[i], u + i);
+                for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
+                // (pages behind the last are hidden from every row)
+                bool slow = big | (u * kPage + PF * kPage - 1 > lo);
+                float l0[NB];
+#pragma unroll
+                for (int j = 0; j < NB; ++j) l0[j] = l[j];
+                if (__builtin_expect(!slow, 1)) {
+                    // one block, in which the products of a page run beside the exponentials of another
+#pragma unroll
+                    for (int i = 0; i < PF; ++i) {
+                        v4f x[NB];
+#pragma unroll
+                        for (int j = 0; j < NB; ++j) x[j] = unit_scores<D, true>(cur[i], q[j]);
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) l[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], c, -m[j]));
                     }
+                    float most = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) most = __builtin_fmaxf(most, l[j]);
+                    slow = __builtin_amdgcn_ballot_w64(!(most <= kMostSum)) != 0;
+                }
+                if (__builtin_expect(slow, 0)) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) l[j] = l0[j];
+#pragma unroll 1
+                    for (int i = 0; i < PF; ++i) {
+                        Unit k = i == 0 ? cur[0] : cur[PF - 1];
+                        hide_unwritten<D>(k, u + i, s.n);
+                        use_moving(k, u + i);
+                    }
+                    find_big();
                 }
 #pragma unroll
                 for (int i = 0; i < PF; ++i) cur[i] = nxt[i];
             }
-            u = end;
         }
-        // the four lane groups' parts of a row
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-#pragma unroll
-            for (int x = 16; x < 64; x <<= 1) {
-                const float mo = __shfl_xor(m[j], x), lo2 = __shfl_xor(l[j], x);
-                const float top = __builtin_fmaxf(m[j], mo);
-                l[j] = l[j] * __builtin_amdgcn_exp2f(m[j] - top) + lo2 * __builtin_amdgcn_exp2f(mo - top);
-                m[j] = top;
-            }
             const int r = r0 + 16 * j + lane;
-            if (lane < 16 && r < rows) {
-                const int64_t row = first_row(p, b, s, hk) + r;
-                if (p.chunks > 1) {
-                    *reinterpret_cast<float2*>(p.parts + 2 * (int64_t(chunk) * p.rows_per_head * p.num_kv_heads + row)) = make_float2(m[j], l[j]);
-                } else {
-                    p.ref[row] = l[j] > 0.f ? m[j] : kMaskedRow;
-                    p.inv[row] = l[j] > 0.f ? 1.0f / l[j] : 0.f;
-                }
-            }
+            store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows);
         }
     }
 }
@@ -386,13 +685,15 @@ struct __attribute__((packed, aligned(4))) Float4At4 {
     float v[4];
 };
 
-// Groups of P units of keys times splits of p.row_split rows, a wave each.
+// Groups of P pages times splits of p.row_split rows, a wave each.
 template <int D, int P>
-__global__ void __launch_bounds__(256) token_sums_kernel(WeightsParams p) {
+__global__ void __launch_bounds__(256, 3) token_sums_kernel(WeightsParams p) {
     using Unit = KeyUnit<D>;
-    constexpr int TOK = Unit::kTokens, N = P * Unit::kTiles;
+    constexpr int TOK = kPage;
+    static_assert(P % 4 == 0, "whole sets of lane groups");
     const int lane = threadIdx.x & 63, grp = lane >> 4;
     const int waves = int(gridDim.x) * 4;
+    const float c = p.scale_log2;
     auto splits_of = [&](const WeightsSeq& s) {
         const int rows = s.use * p.group;
         return rows > 0 ? (rows - 1) / p.row_split + 1 : 0;
@@ -406,13 +707,11 @@ __global__ void __launch_bounds__(256) token_sums_kernel(WeightsParams p) {
         const int groups = (s.n + P * TOK - 1) / (P * TOK), splits = splits_of(s), rows = s.use * p.group;
         const int rest = idx / groups, u0 = (idx - rest * groups) * P;
         const int hk = rest / splits, split = rest - hk * splits;
-        const int pages = (s.n + kPage - 1) / kPage, last_unit = (s.n - 1) / TOK;
-        PageIds ids;
-        ids.load(p, b, u0 * Unit::kPages, pages);
+        const int pages = (s.n + kPage - 1) / kPage;
+        PageIds ids(p, b, u0, s.n);
         Unit k[P];
 #pragma unroll
-        for (int u = 0; u < P; ++u) load_keys<D>(p, ids, hk, u0 + u < last_unit ? u0 + u : last_unit, pages, k[u]);
-        // this lane's tokens of the result: 4 lane groups write a quarter of the tiles each
+        for (int u = 0; u < P; ++u) load_keys<D>(p, ids.at(u0 + u < pages ? u0 + u : pages - 1), hk, k[u]);
         float* const out = p.splits > 1 ? p.parts + ((int64_t(split) * p.batch + b) * p.num_kv_heads + hk) * p.max_context
                                         : p.weights + (int64_t(b) * p.num_kv_heads + hk) * p.width;
         const int pos0 = first_position(p, s);
@@ -427,71 +726,93 @@ __global__ void __launch_bounds__(256) token_sums_kernel(WeightsParams p) {
         const int end = (split + 1) * p.row_split < rows ? (split + 1) * p.row_split : rows;
         const int clear = rows_to(tok1);
         const int64_t base = first_row(p, b, s, hk);
-        float acc[N];
+        float acc[P];
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = 0.f;
+        for (int i = 0; i < P; ++i) acc[i] = 0.f;
 #pragma unroll
         for (int u = 0; u < P; ++u) hide_unwritten<D>(k[u], u0 + u, s.n);
-        RowUnit<D> q;
-        Float4At4 ref, inv;
-        auto load = [&](int r, RowUnit<D>& qq, Float4At4& a, Float4At4& c) {
-            load_rows<D>(p, s, hk, r, rows, qq);
-            a = *reinterpret_cast<const Float4At4*>(p.ref + base + r + 4 * grp);
-            c = *reinterpret_cast<const Float4At4*>(p.inv + base + r + 4 * grp);
+        // 16 rows, while the next 16 are on their way to the other of two buffers
+        struct Rows {
+            RowUnit<D> q;
+            Float4At4 ref, inv;
         };
-        if (r0 < end) load(r0, q, ref, inv);
-        for (; r0 < end; r0 += 16) {
-            RowUnit<D> qn;
-            Float4At4 refn, invn;
-            load(r0 + 16 < end ? r0 + 16 : r0, qn, refn, invn);
-            bool big = false;
+        // this lane's row and its query's place in the group, 16 rows on at every load
+        const uint8_t* row_at = p.q;
+        int member = 0;
+        auto place = [&](int r) {
+            r = r + (lane & 15) < rows ? r + (lane & 15) : rows - 1;
+            const int i = weights_div(p, r);
+            member = r - i * p.group;
+            row_at = p.q + int64_t(s.first + i) * p.q_stride + int64_t(hk * p.group + member) * D + 16 * grp;
+        };
+        const int members = 16 % p.group, step = 16 / p.group * int(p.q_stride) + members * D, wrap = int(p.q_stride) - p.group * D;
+        const float *const refs = p.ref + base, *const invs = p.inv + base;
+        auto load = [&](int r, Rows& x) {
+            // (no branch around the loads: a wait for one buffer would become a wait for both.
+            // Behind the last row: it again, not used)
+            if (__builtin_expect(r + 16 > rows, 0)) place(r);
+            r = r < end ? r : end - 1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // (rows behind the last: memory that no row owns)
-                const bool real = r0 + 4 * grp + i < rows;
-                ref.v[i] = real ? ref.v[i] : kMaskedRow;
-                inv.v[i] = real ? inv.v[i] : 0.f;
-                big = big || (real && __builtin_fabsf(ref.v[i]) >= kBigRef);
+            for (int st = 0; st < Unit::kSteps; ++st) {
+                x.q.lo[st] = *reinterpret_cast<const u32x4*>(row_at + 128 * st);
+                if constexpr (D >= 128) x.q.hi[st] = *reinterpret_cast<const u32x4*>(row_at + 128 * st + 64);
+                else x.q.hi[st] = x.q.lo[st];   // (against keys of 0)
             }
-            big = __builtin_amdgcn_ballot_w64(big) != 0;
-            const bool masked = r0 < clear;
+            x.ref = *reinterpret_cast<const Float4At4*>(refs + r + 4u * unsigned(grp));
+            x.inv = *reinterpret_cast<const Float4At4*>(invs + r + 4u * unsigned(grp));
+            member += members;
+            const bool past = member >= p.group;
+            member -= past ? p.group : 0;
+            row_at += past ? step + wrap : step;
+        };
+        auto use = [&](int r, const Rows& x) {
+            const float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(x.ref.v[0]), __builtin_fabsf(x.ref.v[1])),
+                                              __builtin_fmaxf(__builtin_fabsf(x.ref.v[2]), __builtin_fabsf(x.ref.v[3])));
+            const bool big = __builtin_amdgcn_ballot_w64(top >= kBigRef) != 0;
+            if (__builtin_expect((r < clear) | (r + 16 > rows) | big, 0)) {
 #pragma unroll
-            for (int u = 0; u < P; ++u)
+                for (int u = 0; u < P; ++u) {
+                    const v4f y = unit_scores<D, false>(k[u], x.q);
+                    const int seen = rows_to((u0 + u) * TOK + (lane & 15));
 #pragma unroll
-                for (int t = 0; t < Unit::kTiles; ++t) {
-                    const v4f x = unit_scores<D, false>(k[u], q, t);
-                    float e[4];
-                    if (__builtin_expect(masked || big, 0)) {
-                        const int seen = rows_to((u0 + u) * TOK + kPage * t + (lane & 15));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            e[i] = __builtin_amdgcn_exp2f(above_ref(x[i], p.scale_log2, ref.v[i], big));
-                            e[i] = r0 + 4 * grp + i >= seen ? e[i] : 0.f;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], p.scale_log2, -ref.v[i]));
+                    for (int i = 0; i < 4; ++i) {
+                        const float e = __builtin_amdgcn_exp2f(above_ref(y[i], c, x.ref.v[i], big));
+                        // (rows behind the last: memory that no row owns)
+                        const int row = r + 4 * grp + i;
+                        acc[u] = __builtin_fmaf((row >= seen) & (row < rows) ? e : 0.f, row < rows ? x.inv.v[i] : 0.f, acc[u]);
                     }
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < P; ++u) {
+                    const v4f y = unit_scores<D, false>(k[u], x.q);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        acc[u * Unit::kTiles + t] = __builtin_fmaf(e[i], inv.v[i], acc[u * Unit::kTiles + t]);
+                        acc[u] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(y[i], c, -x.ref.v[i])), x.inv.v[i], acc[u]);
                 }
-            q = qn;
-            ref = refn;
-            inv = invn;
+            }
+        };
+        if (r0 < end) {
+            Rows a, z;
+            place(r0);
+            load(r0, a);
+            while (true) {
+                load(r0 + 16, z);
+                use(r0, a);
+                r0 += 16;
+                if (r0 >= end) break;
+                load(r0 + 16, a);
+                use(r0, z);
+                r0 += 16;
+                if (r0 >= end) break;
+            }
         }
-        // the four lane groups' rows of a token; group g writes tiles g, g + 4 ..
-        float mine[(N + 3) / 4];
+        // the four lane groups' rows of a token; group g writes pages g, g + 4 ..
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            acc[i] += __shfl_xor(acc[i], 16);
-            acc[i] += __shfl_xor(acc[i], 32);
-            mine[i / 4] = (i & 3) == 0 || grp == (i & 3) ? acc[i] : mine[i / 4];
-        }
-#pragma unroll
-        for (int i = 0; i < (N + 3) / 4; ++i) {
-            const int t = tok0 + kPage * (4 * i + grp) + (lane & 15);
-            if (4 * i + grp < N && t < s.n) out[t] = p.splits > 1 ? mine[i] : out[t] + mine[i];
+        for (int i = 0; i < P; i += 4) {
+            const float sum = sum_groups(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+            const int t = tok0 + kPage * i + lane;
+            if (t < s.n) out[t] = p.splits > 1 ? sum : out[t] + sum;
         }
     }
 }
@@ -504,24 +825,32 @@ __global__ void __launch_bounds__(256) token_sums_join_kernel(WeightsParams p) {
     const int rows = s.use * p.group, splits = rows > 0 ? (rows - 1) / p.row_split + 1 : 0;
     if (t >= s.n || splits == 0) return;
     float sum = 0.f;
+#pragma unroll 8
     for (int i = 0; i < splits; ++i) sum += p.parts[(int64_t(i) * gridDim.y + bh) * p.max_context + t];
     p.weights[int64_t(bh) * p.width + t] += sum;
 }
 
 template <int D>
 static void launch_token_weights_d(const WeightsParams& p, hipStream_t stream) {
-    const dim3 block{256u};
-    const dim3 norms{unsigned(p.norm_blocks)}, sums{unsigned(p.sum_blocks)};
-    if (p.row_units == 1) hipLaunchKernelGGL((token_norms_kernel<D, 1>), norms, block, 0, stream, p);
-    else if (p.row_units == 2) hipLaunchKernelGGL((token_norms_kernel<D, 2>), norms, block, 0, stream, p);
-    else if (p.row_units == 4 || D == 256) hipLaunchKernelGGL((token_norms_kernel<D, 4>), norms, block, 0, stream, p);
-    else hipLaunchKernelGGL((token_norms_kernel<D, (D == 256 ? 4 : 8)>), norms, block, 0, stream, p);
+    const dim3 block{256u}, norms{unsigned(p.norm_blocks)}, sums{unsigned(p.sum_blocks)};
+    if (p.few) {
+        if (p.row_units == 1) hipLaunchKernelGGL((few_rows_kernel<D, 1, false>), norms, block, 0, stream, p);
+        else if (p.row_units == 2 || D == 256) hipLaunchKernelGGL((few_rows_kernel<D, 2, false>), norms, block, 0, stream, p);
+        else hipLaunchKernelGGL((few_rows_kernel<D, (D == 256 ? 2 : 4), false>), norms, block, 0, stream, p);
+    } else {
+        hipLaunchKernelGGL((token_norms_kernel<D, (D == 256 ? 4 : 8)>), norms, block, 0, stream, p);
+    }
     if (p.chunks > 1) {
         const int64_t rows = p.rows_per_head * p.num_kv_heads;
         hipLaunchKernelGGL(token_norms_join_kernel, dim3(unsigned((rows + 63) / 64)), block, 0, stream, p);
     }
-    if (p.key_units == 2) hipLaunchKernelGGL((token_sums_kernel<D, 2>), sums, block, 0, stream, p);
-    else hipLaunchKernelGGL((token_sums_kernel<D, (D == 128 ? 8 : 4)>), sums, block, 0, stream, p);
+    if (p.few) {
+        if (p.row_units == 1) hipLaunchKernelGGL((few_rows_kernel<D, 1, true>), sums, block, 0, stream, p);
+        else if (p.row_units == 2 || D == 256) hipLaunchKernelGGL((few_rows_kernel<D, 2, true>), sums, block, 0, stream, p);
+        else hipLaunchKernelGGL((few_rows_kernel<D, (D == 256 ? 2 : 4), true>), sums, block, 0, stream, p);
+        return;
+    }
+    hipLaunchKernelGGL((token_sums_kernel<D, (D == 256 ? 4 : 8)>), sums, block, 0, stream, p);
     if (p.splits > 1)
         hipLaunchKernelGGL(token_sums_join_kernel, dim3(unsigned((p.max_context + 255) / 256), unsigned(p.batch * p.num_kv_heads)), block,
                            0, stream, p);

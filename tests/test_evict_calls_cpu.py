@@ -152,8 +152,13 @@ def test_select_tokens():
                dict(kept=at(3) - 8), dict(kl=at(0) + 400)):
         assert select(**kw) == INVALID, kw
     for kw in (dict(B=65536), dict(H=65536), dict(B=2000, H=5000), dict(bound=(1 << 30) + 1, width=1 << 31),
-               dict(budget=(1 << 30) + 1)):
+               dict(budget=(1 << 30) + 1), dict(B=1000, H=8, bound=1 << 26, width=1 << 26)):
         assert select(**kw) == UNSUPPORTED, kw
+    assert uq.select_workspace_bytes(2, 3, 16384, 10) == 0 and uq.select_workspace_bytes(2, 3, 1 << 20, 1 << 20) == 0
+    n = uq.select_workspace_bytes(2, 3, 40000, 10)
+    assert n > 0 and select(bound=40000, width=40000, wsb=n - 1) == SMALL
+    for kw in (dict(ws=None), dict(ws=at(4) + 4), dict(ws=at(0)), dict(ws=at(2) + 16)):
+        assert select(bound=40000, width=40000, **kw) == INVALID, kw
 
 
 def compact(D=None, kept=at(0), budget=10, kl=at(1), lens=at(2), B=2, codes=at(3), scales=at(4), table=at(5), mpps=4, w=at(6),
@@ -174,6 +179,12 @@ def test_compact_kv():
     for kw in (dict(B=65536), dict(mpps=1 << 27), dict(budget=(1 << 30) + 1), dict(D=desc(head_dim=96))):
         assert compact(**kw) == UNSUPPORTED, kw
     assert compact(B=0, freed=None, count=None) == OK
+    D = desc()
+    n = uq.lib.uq_compact_kv_workspace_bytes(ctypes.byref(D), 2, 10)
+    assert n > 0 and compact(wsb=n - 1) == SMALL
+    for kw in (dict(ws=None), dict(ws=at(9) + 8), dict(ws=at(3)), dict(ws=at(0))):
+        assert compact(**kw) == INVALID, kw
+    assert uq.lib.uq_compact_kv_workspace_bytes(ctypes.byref(D), 32, 10) == 0   # 64 pairs: in place
 
 
 def test_binding_wants_gpu_tensors():

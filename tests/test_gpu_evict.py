@@ -92,6 +92,40 @@ def test_long_row_and_wide_array(uq):
     check_select(uq, w, [33000], 1000)
 
 
+@pytest.mark.parametrize("n", [16384, 16385, 17000, 32768, 40001])
+def test_rows_of_several_slices(uq, n):
+    g = torch.Generator(device=DEV).manual_seed(n)
+    w = torch.exp(2.5 * torch.randn((2, 2, n + 3), generator=g, device=DEV))
+    w[torch.rand(w.shape, generator=g, device=DEV) < 0.1] = 0.0
+    for budget, sinks, recent in ((1, 0, 0), (1000, 4, 64), (16390, 0, 16390), (n - 1, 5, n // 2), (12000, 12000, 0)):
+        check_select(uq, w, [n, 16383], budget, sinks=min(sinks, budget), recent=min(recent, budget), bound=n)
+
+
+def test_slices_of_equal_and_close_weights(uq):
+    """More keys with the same first bits than a list holds, and ties over slices."""
+    g = torch.Generator(device=DEV).manual_seed(6)
+    n = 50000
+    w = torch.randint(0, 3, (1, 2, n), generator=g, device=DEV).float()
+    for budget in (1, 100, 16000, 33000, 49999):
+        check_select(uq, w, [n], budget, sinks=min(7, budget), recent=min(20, budget) // 2)
+    check_select(uq, torch.zeros_like(w), [n], 20000, sinks=4, recent=100)
+    base = torch.tensor([1.0], device=DEV).view(torch.int32)
+    w = (base + torch.randint(0, 30000, (1, 1, n), generator=g, device=DEV).int()).view(torch.float32)
+    for budget in (5, 25000):
+        check_select(uq, w, [n], budget)
+    # one slice with nothing but ties, the others mixed
+    w = torch.rand((1, 1, n), generator=g, device=DEV)
+    w[:, :, 16384:32768] = 0.5
+    for budget in (20000, 26000, 40000):
+        check_select(uq, w, [n], budget)
+
+
+def test_short_rows_beside_long_ones(uq):
+    g = torch.Generator(device=DEV).manual_seed(7)
+    w = torch.rand((6, 1, 60000), generator=g, device=DEV)
+    check_select(uq, w, [60000, 0, 5, 16384, 900, 33000], 900, sinks=1, recent=30)
+
+
 def test_lengths_of_zero_and_negative(uq):
     w = torch.rand((3, 2, 40), device=DEV)
     kept, kl = uq.select_tokens(w, torch.tensor([0, -3, 40], dtype=torch.int32, device=DEV), 40, 8)

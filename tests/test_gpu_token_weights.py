@@ -246,7 +246,9 @@ def test_accumulates(uq):
     w = torch.zeros_like(c.before)
     for _ in range(2):
         c.call(weights=w)
-    assert torch.equal(w, one + one)
+    # a call adds the sums of at most two blocks of rows one after another, so a weight has been
+    # rounded to half a step, 2^-24, at most four times, `one` twice
+    assert ((w - (one + one)).abs() <= 6 * 2 ** -24 * (one + one)).all()
 
 
 def test_tables_wider_than_the_bound(uq):
