@@ -1012,7 +1012,7 @@ struct WeightsShape {
     size_t query, rows;    // bytes of the prepared queries and of the rows' references and sums
     size_t workspace;
 };
-// Partial results of split rows or contexts: the splits below keep to it.
+// Partial results of split rows or contexts: the splits below keep to it (or to one part of every row).
 constexpr size_t kWeightsParts = size_t(16) << 20;
 constexpr int64_t kFewWaves = 8192, kManyWaves = 16384, kSumWaves = 16384;
 
@@ -1045,6 +1045,8 @@ static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int6
     e.chunk = 1 << 30;
     while (e.chunk > least && row_blocks * ((bound + e.chunk - 1) / e.chunk) < (e.few ? kFewWaves : kManyWaves)) e.chunk /= 2;
     while (e.chunk < (1 << 30) && bound > e.chunk && size_t(rows) * size_t((bound + e.chunk - 1) / e.chunk) * 8 > kWeightsParts) e.chunk *= 2;
+    // (few rows: a wave of the sums joins its rows' chunks itself)
+    while (e.few && (bound + e.chunk - 1) / e.chunk > 256) e.chunk *= 2;
     e.chunks = int32_t((bound + e.chunk - 1) / e.chunk);
     const int64_t norm_waves = row_blocks * e.chunks;
     int64_t sum_waves = norm_waves;
@@ -1070,7 +1072,8 @@ static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int6
     e.sum_blocks = int32_t(sum_waves / 4 + 1 < at_once ? sum_waves / 4 + 1 : at_once);
     e.query = q_dtype == UQ_FP8_E4M3 ? 0 : align16(size_t(num_tokens) * size_t(num_q_heads) * size_t(desc->head_dim));
     e.rows = align16((size_t(rows) + 16) * sizeof(float));
-    e.workspace = e.query + 2 * e.rows + kWeightsParts;
+    const size_t one = align16(size_t(rows) * 2 * sizeof(float));
+    e.workspace = e.query + 2 * e.rows + (one > kWeightsParts ? one : kWeightsParts);
     return UQ_OK;
 }
 

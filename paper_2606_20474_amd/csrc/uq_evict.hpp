@@ -266,17 +266,20 @@ __global__ void __launch_bounds__(kSelectThreads) select_list_kernel(SelectParam
     }
     __syncthreads();
     SelectSlice* const out = slice_of(p, row, slice);
-    int sures = 0;
+    int sures = 0, mine = 0;
     each_key(r, k, [&](uint32_t key, int t, bool competes) {
-        const bool in = competes && key >> 21 == bits;
         sures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(competes ? key >> 21 > bits : t < r.n));
+        mine += __builtin_popcountll(__builtin_amdgcn_ballot_w64(competes && key >> 21 == bits));
+    });
+    int at = 0;
+    if (lane == 0 && mine > 0) at = atomicAdd(&listed, mine);
+    at = __builtin_amdgcn_readfirstlane(at);
+    each_key(r, k, [&](uint32_t key, int, bool competes) {
+        const bool in = competes && key >> 21 == bits;
         const uint64_t who = __builtin_amdgcn_ballot_w64(in);
-        if (who == 0) return;
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&listed, __builtin_popcountll(who));
-        at = __builtin_amdgcn_readfirstlane(at);
-        at += int(__builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0u)));
-        if (in && at < kSelectList) out->list[at] = key;
+        const int to = at + int(__builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0u)));
+        if (in && to < kSelectList) out->list[to] = key;
+        at += __builtin_popcountll(who);
     });
     if (lane == 0) c.wave_sum[1][wave] = sures;
     __syncthreads();
@@ -294,28 +297,58 @@ __global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectPara
     const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
     const SelectRow r = select_row(p, row, slice);
     if (r.n <= p.budget || slice * kSelectSlice >= r.n) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    SelectKeys k;
-    load_keys(r, k);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int slices = (r.n + kSelectSlice - 1) / kSelectSlice;
     uint32_t least = 0xFFFFFFFFu, bits = 0xFFFFFFFFu;
     int ties = 0, above = 0;
     if (threadIdx.x < 2) sums[threadIdx.x] = 0;
-    // f(key, slice) for the row's keys that begin with its first bits: a quarter of a list per wave
+    // Up to 8 slices whose keys are all listed: a wave holds every fourth 64 of a list, twice; a place
+    // without a key has other first bits.
+    constexpr int Q = kSelectList / 4 / 64, kUnits = 2;
+    uint32_t held[kUnits][Q];
+    int sets[kUnits] = {0, 0};       // of 64 places with a key
+    bool hold = 4 * slices <= kUnits * (kSelectThreads / 64);
+    if (r.want > 0) {
+        const int2 first = *first_bits_of(p, row);
+        bits = least = uint32_t(first.x);
+        above = first.y;
+        if (hold) {
+            const int listed = slice_of(p, row, lane < slices ? lane : 0)->listed;
+            hold = __builtin_amdgcn_ballot_w64(listed > kSelectList) == 0;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int unit = wave + u * (kSelectThreads / 64), q = unit & 3;
+                const int s = unit >> 2 < slices ? unit >> 2 : 0;
+                const int here = unit >> 2 < slices ? __builtin_amdgcn_readlane(listed, s) : 0;
+                const SelectSlice* const x = slice_of(p, row, s);
+                sets[u] = (here + 64 * (3 - q) + 63) / 256;
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    const int at = (4 * i + q) * 64 + lane;
+                    held[u][i] = (bits ^ 1u) << 21;
+                    if (i < sets[u] && at < here) held[u][i] = x->list[at];
+                }
+            }
+        }
+    }
+    // f(key, slice) for the row's keys that begin with its first bits
     auto each_listed = [&](auto f) {
-        constexpr int Q = kSelectList / 4 / 64;
+        if (hold) {
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    if (i >= sets[u]) break;
+                    if (held[u][i] >> 21 == bits) f(held[u][i], (wave + u * (kSelectThreads / 64)) >> 2);
+                }
+            return;
+        }
         for (int unit = wave; unit < 4 * slices; unit += kSelectThreads / 64) {
             const int s = unit >> 2, q = unit & 3;
             const SelectSlice* const x = slice_of(p, row, s);
             const int listed = __builtin_amdgcn_readfirstlane(x->listed);
             if (listed <= kSelectList) {
-                if (q * Q * 64 >= listed) continue;
-                uint32_t key[Q];
-#pragma unroll
-                for (int i = 0; i < Q; ++i) key[i] = x->list[(q * Q + i) * 64 + lane];
-#pragma unroll
-                for (int i = 0; i < Q; ++i)
-                    if ((q * Q + i) * 64 + lane < listed) f(key[i], s);
+                for (int i = 64 * q + lane; i < listed; i += 256) f(x->list[i], s);
             } else {
                 // (too many: the slice itself)
                 const int t0 = s * kSelectSlice + q * (kSelectSlice / 4);
@@ -327,9 +360,6 @@ __global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectPara
         }
     };
     if (r.want > 0) {
-        const int2 first = *first_bits_of(p, row);
-        bits = least = uint32_t(first.x);
-        above = first.y;
 #pragma unroll
         for (int pass = 1; pass < 3; ++pass) {
             clear_counts(c);
@@ -352,8 +382,17 @@ __global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectPara
             sures += s < slice && key > least;
             equals += s < slice && key == least;
         });
-    if (sures != 0) atomicAdd(&sums[0], sures);
-    if (equals != 0) atomicAdd(&sums[1], equals);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        sures += __shfl_xor(sures, x);
+        equals += __shfl_xor(equals, x);
+    }
+    if (lane == 0) {
+        atomicAdd(&sums[0], sures);
+        atomicAdd(&sums[1], equals);
+    }
+    SelectKeys k;
+    load_keys(r, k);
     __syncthreads();
     write_kept(p, r, k, c, row, least, ties, sums[0], sums[1]);
 }

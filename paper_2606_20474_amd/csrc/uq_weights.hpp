@@ -189,10 +189,11 @@ __device__ __forceinline__ void load_rows(const WeightsParams& p, const WeightsS
     }
 }
 
-// c s - m: fused, or where m is large from the rounded product, as m is one.
-__device__ __forceinline__ float above_ref(float s, float c, float m, bool big) {
+// c s - m: fused, or where m is large from the rounded product, as m is one (what the
+// fused form leaves of its rounding may then be out of range itself).
+__device__ __forceinline__ float above_ref(float s, float c, float m) {
 #pragma clang fp contract(off)
-    return big ? s * c - m : __builtin_fmaf(s, c, -m);
+    return __builtin_fabsf(m) >= kBigRef ? s * c - m : __builtin_fmaf(s, c, -m);
 }
 
 // 4 scores of a row, added to its sum relative to a reference that moves up to them.
@@ -202,14 +203,14 @@ __device__ __forceinline__ void add_moving(const v4f& x, float c, float& m, floa
         l *= __builtin_amdgcn_exp2f(m - mx);
         m = mx;
     }
-    // (nothing seen yet: -inf - -1e30 is -inf still)
+    // (nothing seen yet: -inf - -1e30 and -inf c are -inf still)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) l += __builtin_amdgcn_exp2f(above_ref(x[i], c, m, true));
+    for (int i = 0; i < 4; ++i) l += __builtin_amdgcn_exp2f(above_ref(x[i], c, m));
 }
 
 // A row's parts in the four lane groups into one, and where it goes: the chunk's
-// reference and sum, or (one chunk) the reference and 1 / sum.
-__device__ __forceinline__ void store_norm(const WeightsParams& p, float m, float l, int chunk, int64_t row, bool real) {
+// reference and sum, or (not `part`) the reference and 1 / sum.
+__device__ __forceinline__ void store_norm(const WeightsParams& p, float m, float l, int chunk, int64_t row, bool real, bool part) {
 #pragma unroll
     for (int x = 16; x < 64; x <<= 1) {
         const float mo = __shfl_xor(m, x), lo = __shfl_xor(l, x);
@@ -218,7 +219,7 @@ __device__ __forceinline__ void store_norm(const WeightsParams& p, float m, floa
         m = top;
     }
     if (!real) return;
-    if (p.chunks > 1) {
+    if (part) {
         *reinterpret_cast<float2*>(p.parts + 2 * (int64_t(chunk) * p.rows_per_head * p.num_kv_heads + row)) = make_float2(m, l);
     } else {
         p.ref[row] = l > 0.f ? m : kMaskedRow;
@@ -243,8 +244,10 @@ template <int D> struct FewKeys {
     int scale[D == 256 ? 2 : 1];
 };
 
-template <int D>
+// (NT: past the caches, for the sums, which read them last)
+template <int D, bool NT>
 __device__ __forceinline__ void load_few(const WeightsParams& p, int id, int hk, FewKeys<D>& k) {
+    auto get = [](const auto* x) { return NT ? __builtin_nontemporal_load(x) : *x; };
     const int lane = threadIdx.x & 63;
     const int64_t ph = int64_t(id) * p.num_kv_heads + hk;
     const uint8_t* codes = p.codes + ph * (16 * D);
@@ -252,17 +255,17 @@ __device__ __forceinline__ void load_few(const WeightsParams& p, int id, int hk,
     if constexpr (D == 64) {
         // 16 channels: half of a group's 16 bytes
         const int at = (lane >> 5) * kPage + (lane & 15);
-        const uint2 c = *reinterpret_cast<const uint2*>(codes + 16 * at + 8 * ((lane >> 4) & 1));
-        k.code[0] = c.x;
-        k.code[1] = c.y;
-        k.scale[0] = scales[at];
+        const u32x2 c = get(reinterpret_cast<const u32x2*>(codes + 16 * at + 8 * ((lane >> 4) & 1)));
+        k.code[0] = c[0];
+        k.code[1] = c[1];
+        k.scale[0] = get(scales + at);
     } else {
 #pragma unroll
         for (int i = 0; i < D / 128; ++i) {
-            const u32x4 c = *reinterpret_cast<const u32x4*>(codes + 1024 * i + 16 * lane);
+            const u32x4 c = get(reinterpret_cast<const u32x4*>(codes + 1024 * i + 16 * lane));
 #pragma unroll
             for (int w = 0; w < 4; ++w) k.code[4 * i + w] = c[w];
-            k.scale[i] = scales[64 * i + lane];
+            k.scale[i] = get(scales + 64 * i + lane);
         }
     }
 }
@@ -339,8 +342,27 @@ __device__ __forceinline__ float sum_groups(float a, float b, float c, float d) 
     return bits_f32(r[0]) + bits_f32(r[1]);
 }
 
+// The reference and sum of a row over its chunks: this lane group's share of them, then all four groups.
+__device__ __forceinline__ float2 join_chunks(const WeightsParams& p, int64_t row, int grp, int chunks) {
+    const int64_t all = p.rows_per_head * p.num_kv_heads;
+    float m = kNoRow, l = 0.f;
+    auto add = [&](float mo, float lo) {
+        const float top = __builtin_fmaxf(m, mo);
+        l = l * __builtin_amdgcn_exp2f(m - top) + lo * __builtin_amdgcn_exp2f(mo - top);
+        m = top;
+    };
+#pragma unroll 4
+    for (int c = grp; c < chunks; c += 4) {
+        const float2 x = *reinterpret_cast<const float2*>(p.parts + 2 * (c * all + row));
+        add(x.x, x.y);
+    }
+    add(__shfl_xor(m, 16), __shfl_xor(l, 16));
+    add(__shfl_xor(m, 32), __shfl_xor(l, 32));
+    return make_float2(m, l);
+}
+
 template <int D, int NB, bool SUMS>
-__global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
+__global__ void __launch_bounds__(256, NB == 1 && D <= 128 ? 4 : 2) few_rows_kernel(WeightsParams p) {
     constexpr int PF = 4;
     const int lane = threadIdx.x & 63, grp = lane >> 4, col = lane & 15;
     const int waves = int(gridDim.x) * 4;
@@ -364,6 +386,26 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
             const int r0 = rb * (16 * NB);
             const int r1 = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;     // the block's last row
             const int lo = p.causal ? pos0 + weights_div(p, r0) : pos0, hi = p.causal ? pos0 + weights_div(p, r1) : pos0;
+            // pages of the chunk up to the last that a row of the block sees
+            const int u0 = chunk * (p.chunk / kPage);
+            int u1 = hi >= 0 ? hi / kPage + 1 : 0;
+            u1 = u1 < u0 + p.chunk / kPage ? u1 : u0 + p.chunk / kPage;
+            if (u0 >= u1) {
+                // no token is seen
+                if constexpr (!SUMS) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const int r = r0 + 16 * j + lane;
+                        store_norm(p, kNoRow, 0.f, chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows, true);
+                    }
+                }
+                continue;
+            }
+            // the first keys, on their way while the rows are made ready
+            PageIds ids(p, b, u0, s.n);
+            FewKeys<D> cur[PF], nxt[PF];
+#pragma unroll
+            for (int i = 0; i < PF; ++i) load_few<D, SUMS>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
             FewRows<D> q[NB];
             float m[SUMS ? 1 : NB], l[SUMS ? 1 : NB], ref[SUMS ? NB : 1][4], inv[SUMS ? NB : 1][4];
             int pos[SUMS ? 1 : NB];
@@ -372,12 +414,15 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
             for (int j = 0; j < NB; ++j) {
                 load_few_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
                 if constexpr (SUMS) {
-                    const int64_t at_row = first_row(p, b, s, hk) + r0 + 16 * j + 4 * grp;
+                    // this lane's row of 16, from a quarter of its chunks; then rows 4 grp .. 4 grp + 3
+                    const float2 x = join_chunks(p, first_row(p, b, s, hk) + (r0 + 16 * j + col < rows ? r0 + 16 * j + col : rows - 1), grp,
+                                                 chunks);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const bool real = r0 + 16 * j + 4 * grp + i < rows;
-                        ref[j][i] = real ? p.ref[at_row + i] : kMaskedRow;
-                        inv[j][i] = real ? p.inv[at_row + i] : 0.f;
+                        const float m = __shfl(x.x, 4 * grp + i), l = __shfl(x.y, 4 * grp + i);
+                        ref[j][i] = real && l > 0.f ? m : kMaskedRow;
+                        inv[j][i] = real && l > 0.f ? 1.0f / l : 0.f;
                         big = big | (real & (__builtin_fabsf(ref[j][i]) >= kBigRef));
                     }
                 } else {
@@ -388,10 +433,6 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
                 }
             }
             big = __builtin_amdgcn_ballot_w64(big) != 0;
-            // pages of the chunk up to the last that a row of the block sees
-            const int u0 = chunk * (p.chunk / kPage);
-            int u1 = hi >= 0 ? hi / kPage + 1 : 0;
-            u1 = u1 < u0 + p.chunk / kPage ? u1 : u0 + p.chunk / kPage;
             // the norms of one page: `moving`, the reference follows
             auto norms_of = [&](const FewKeys<D>& k, int u, bool moving) {
                 v8bf ko[D / 32];
@@ -432,7 +473,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
                         const v4f x = few_scores<D, false>(ko, q[j]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float e = __builtin_amdgcn_exp2f(above_ref(x[i], c, ref[j][i], big));
+                            const float e = __builtin_amdgcn_exp2f(above_ref(x[i], c, ref[j][i]));
                             sum = __builtin_fmaf(r0 + 16 * j + 4 * grp + i >= seen ? e : 0.f, inv[j][i], sum);
                         }
                     }
@@ -448,11 +489,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
                 return sum;
             };
             float* const out = p.weights + (int64_t(b) * p.num_kv_heads + hk) * p.width;
-            if (u0 < u1) {
-                PageIds ids(p, b, u0, s.n);
-                FewKeys<D> cur[PF], nxt[PF];
-#pragma unroll
-                for (int i = 0; i < PF; ++i) load_few<D>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
+            {
                 if constexpr (!SUMS) {
                     // a lane that sees a token of the chunk sees one in its first page, or no later one
                     norms_of(cur[0], u0, true);
@@ -465,7 +502,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
                     const int t = u * kPage + lane;
                     if (SUMS && t < s.n) before = out[t];
 #pragma unroll
-                    for (int i = 0; i < PF; ++i) load_few<D>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
+                    for (int i = 0; i < PF; ++i) load_few<D, SUMS>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
                     if constexpr (SUMS) {
                         float sum[PF];
 #pragma unroll
@@ -501,7 +538,7 @@ __global__ void __launch_bounds__(256, 2) few_rows_kernel(WeightsParams p) {
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     const int r = r0 + 16 * j + lane;
-                    store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows);
+                    store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows, true);
                 }
             }
         }
@@ -627,7 +664,7 @@ __global__ void __launch_bounds__(256, 2) token_norms_kernel(WeightsParams p) {
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int r = r0 + 16 * j + lane;
-            store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows);
+            store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows, p.chunks > 1);
         }
     }
 }
@@ -776,7 +813,7 @@ __global__ void __launch_bounds__(256, 3) token_sums_kernel(WeightsParams p) {
                     const int seen = rows_to((u0 + u) * TOK + (lane & 15));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(above_ref(y[i], c, x.ref.v[i], big));
+                        const float e = __builtin_amdgcn_exp2f(above_ref(y[i], c, x.ref.v[i]));
                         // (rows behind the last: memory that no row owns)
                         const int row = r + 4 * grp + i;
                         acc[u] = __builtin_fmaf((row >= seen) & (row < rows) ? e : 0.f, row < rows ? x.inv.v[i] : 0.f, acc[u]);
@@ -840,7 +877,7 @@ static void launch_token_weights_d(const WeightsParams& p, hipStream_t stream) {
     } else {
         hipLaunchKernelGGL((token_norms_kernel<D, (D == 256 ? 4 : 8)>), norms, block, 0, stream, p);
     }
-    if (p.chunks > 1) {
+    if (p.chunks > 1 && !p.few) {
         const int64_t rows = p.rows_per_head * p.num_kv_heads;
         hipLaunchKernelGGL(token_norms_join_kernel, dim3(unsigned((rows + 63) / 64)), block, 0, stream, p);
     }
