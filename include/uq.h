@@ -701,8 +701,7 @@ typedef struct uq_rope_axes {
  * uq_norm_rope_write where pair j of token t turns by row
  * positions[pair_axes[j]][t] of cos_sin, its columns j and rot_dim / 2 + j.
  * Axes that are equal give the bits of those calls.  Each axis's positions
- * are clamped to [0, max_position).  Any map of pairs to axes is taken;
- * one that is constant over aligned 8 pairs, or 4, loads angles in wide words.
+ * are clamped to [0, max_position).  Any map of pairs to axes is taken.
  * Errors: those of the calls, plus INVALID_ARGUMENT for a NULL axes or
  * pair_axes, num_axes outside 1 .. 4, an axis out of range, a
  * position_stride below num_tokens, or rot_dim == 0.

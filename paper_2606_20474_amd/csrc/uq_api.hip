@@ -568,7 +568,6 @@ static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, const uq_rope_ax
     if (num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
     p.num_axes = 0;
     p.axis_stride = 0;
-    p.axis_unit = 8;
     for (uint32_t& w : p.axis_of) w = 0;
     if (axes != nullptr) {
         if (rot == 0 || axes->num_axes < 1 || axes->num_axes > 4 || axes->pair_axes == nullptr ||
@@ -580,7 +579,6 @@ static uq_status norm_rope_setup(const uq_norm_rope_desc* spec, const uq_rope_ax
             const uint32_t a = axes->pair_axes[i];
             if (a >= uint32_t(axes->num_axes)) return UQ_ERR_INVALID_ARGUMENT;
             p.axis_of[i / 16] |= a << (2 * (i % 16));
-            while (a != axes->pair_axes[i & ~(p.axis_unit - 1)]) p.axis_unit = p.axis_unit == 8 ? 4 : 1;
         }
     }
     p.q = q;

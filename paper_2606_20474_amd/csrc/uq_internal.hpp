@@ -332,7 +332,6 @@ struct NormRopeParams {
     // positions[a * axis_stride + t], and 2 bits per pair that name its axis
     int32_t num_axes;
     int64_t axis_stride;
-    int32_t axis_unit;         // aligned pairs that share an axis: 8, 4, or 1 (no rule)
     uint32_t axis_of[8];
 };
 

@@ -43,13 +43,12 @@ __device__ __forceinline__ void rotate_pair(float& a, float& b, float c, float s
     a = ya;
 }
 
-// The angles of a token: N consecutive pairs from `pair` on.  A token with one
-// position: one row of the table, rot / 2 cosines, then the sines.
-struct RowAngles {
+// The angles of a token: N consecutive pairs from `pair` on, from a row of rot / 2
+// cosines, then the sines of the same angles: the table's for a token with one position ...
+struct TableAngles {
     const float* cs;
     int half;
-    __device__ __forceinline__ uint32_t map(int, bool, int) const { return 0; }
-    template <int N> __device__ __forceinline__ void load(int pair, uint32_t, float (&c)[N], float (&s)[N]) const {
+    template <int N> __device__ __forceinline__ void load(int pair, float (&c)[N], float (&s)[N]) const {
         if constexpr (N == 8) {
             load_x8<0>(cs, pair, c);
             load_x8<0>(cs, half + pair, s);
@@ -60,59 +59,46 @@ struct RowAngles {
     }
 };
 
-// A token with a position on every axis: a row of the table for each, and 2 bits per
-// pair that say which.  Where 8 or 4 aligned pairs share an axis (p.axis_unit) they are
-// loaded together.
-struct AxisAngles {
-    const NormRopeParams& p;
-    int64_t at[4];   // the axes' rows
-    __device__ __forceinline__ AxisAngles(const NormRopeParams& q, int64_t t) : p(q) {
+// ... or a row in LDS that the block has put together (stage_angles).
+extern __shared__ __attribute__((aligned(16))) float staged_angles[];
+struct StagedAngles {
+    int at, half;
+    template <int N> __device__ __forceinline__ void load(int pair, float (&c)[N], float (&s)[N]) const {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            int pos = q.positions[(a < q.num_axes ? a : 0) * q.axis_stride + t];
-            pos = pos < 0 ? 0 : pos < q.max_position ? pos : q.max_position - 1;
-            at[a] = int64_t(pos) * q.rot;
-        }
-    }
-    // the axes of 16 pairs from 16 w (or, with `next`, 16 w + 16) on, shifted
-    __device__ __forceinline__ uint32_t map(int w, bool next, int shift) const {
-        return (next ? p.axis_of[w + 1] : p.axis_of[w]) >> shift;
-    }
-    __device__ __forceinline__ const float* row(uint32_t axis) const {
-        const int64_t lo = axis & 1u ? at[1] : at[0], hi = axis & 1u ? at[3] : at[2];
-        return p.cos_sin + (axis & 2u ? hi : lo);
-    }
-    template <int N> __device__ __forceinline__ void load(int pair, uint32_t axes, float (&c)[N], float (&s)[N]) const {
-        const int half = p.rot / 2;
-        if (N == 8 && p.axis_unit == 8) {
-            const float* r = row(axes);
-            if constexpr (N == 8) {
-                load_x8<0>(r, pair, c);
-                load_x8<0>(r, half + pair, s);
-            }
-        } else if (p.axis_unit >= 4) {
-#pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const float* r = row(axes >> (2 * k));
-                float x[4], y[4];
-                load_x4<0>(r, pair + k, x);
-                load_x4<0>(r, half + pair + k, y);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c[k + i] = x[i];
-                    s[k + i] = y[i];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float* r = row(axes >> (2 * i));
-                c[i] = r[pair + i];
-                s[i] = r[half + pair + i];
-            }
+        for (int k = 0; k < N; k += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(staged_angles + at + pair + k);
+            const float4 y = *reinterpret_cast<const float4*>(staged_angles + at + half + pair + k);
+            c[k] = x.x; c[k + 1] = x.y; c[k + 2] = x.z; c[k + 3] = x.w;
+            s[k] = y.x; s[k + 1] = y.y; s[k + 2] = y.z; s[k + 3] = y.w;
         }
     }
 };
+
+// The angle rows of `count` tokens from t0 on whose positions have several axes, one after
+// another in LDS; the whole block calls it.  A row costs the same whatever the map of pairs to
+// axes, and a token's heads share it (each lane of each head loading its own pairs: 70 us where
+// the axes are runs of 8 pairs, 89 where they take turns, for the 8191 tokens below).
+__device__ __forceinline__ void stage_angles(const NormRopeParams& p, int64_t t0, int count) {
+    const int half = p.rot / 2;
+    const int wide = half <= 8 ? 8 : half <= 16 ? 16 : half <= 32 ? 32 : half <= 64 ? 64 : 128;   // threads per row
+    const int j = int(threadIdx.x) & (wide - 1);
+    if (j < half) {
+        // the pair's axis: 2 bits of 16 in a word
+        uint32_t word = p.axis_of[0];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) word = (j >> 4) == w ? p.axis_of[w] : word;
+        const int32_t* const positions = p.positions + int64_t(word >> (2 * (j & 15)) & 3u) * p.axis_stride;
+        for (int i = int(threadIdx.x) / wide; i < count; i += 256 / wide) {
+            const int64_t t = t0 + i < p.num_tokens ? t0 + i : p.num_tokens - 1;
+            int pos = positions[t];
+            pos = pos < 0 ? 0 : pos < p.max_position ? pos : p.max_position - 1;
+            const float* const row = p.cos_sin + int64_t(pos) * p.rot + j;
+            staged_angles[i * p.rot + j] = row[0];
+            staged_angles[i * p.rot + half + j] = row[half];
+        }
+    }
+    __syncthreads();
+}
 
 // Pairs (c, c + 32 H), c < 32 H: both in this lane.
 template <int NG, int H, class ANGLES>
@@ -121,7 +107,7 @@ __device__ __forceinline__ void rope_in_lane(float (&x)[NG][8], const ANGLES& an
 #pragma unroll
         for (int j = 0; j < H; ++j) {
             float c[8], s[8];
-            ang.load(32 * j + 8 * L, ang.map(2 * j, (L & 2) != 0, 16 * (L & 1)), c, s);
+            ang.load(32 * j + 8 * L, c, s);
 #pragma unroll
             for (int i = 0; i < 8; ++i) rotate_pair(x[j][i], x[j + H][i], c[i], s[i]);
         }
@@ -133,7 +119,7 @@ __device__ __forceinline__ void rope_in_lane(float (&x)[NG][8], const ANGLES& an
 template <int S, int NG, class ANGLES>
 __device__ __forceinline__ void rope_across(float (&x)[NG][8], const ANGLES& ang, int L) {
     float c[8], s[8];
-    ang.load(8 * (L & (S - 1)), ang.map(0, false, 16 * (L & (S - 1))), c, s);
+    ang.load(8 * (L & (S - 1)), c, s);
     const bool upper = (L & S) != 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -152,7 +138,7 @@ __device__ __forceinline__ void rope_quad(float (&x)[NG][8], const ANGLES& ang, 
             const int c0 = 32 * j + 8 * L;   // this lane's 8 channels, 4 pairs (rot is a multiple of 8)
             if (c0 < rot) {
                 float c[4], s[4];
-                ang.load(c0 / 2, ang.map(j, false, 8 * L), c, s);
+                ang.load(c0 / 2, c, s);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) rotate_pair(x[j][2 * i], x[j][2 * i + 1], c[i], s[i]);
             }
@@ -191,17 +177,18 @@ __device__ __forceinline__ void store_x8(void* base, int64_t elem, int dt, const
     }
 }
 
-// Norm and rotation of the vector a quad holds (token t, weight w or nullptr).
+// Norm and rotation of the vector a quad holds (token t, weight w or nullptr).  AXES: the angles of
+// the tokens from t0 on are staged.
 template <int NG, bool AXES>
-__device__ __forceinline__ void norm_rope_quad(float (&x)[NG][8], const NormRopeParams& p, int64_t t, const float* w,
+__device__ __forceinline__ void norm_rope_quad(float (&x)[NG][8], const NormRopeParams& p, int64_t t, int64_t t0, const float* w,
                                                int L) {
     if (w != nullptr) norm_quad<NG>(x, w, p.eps, L);
     if constexpr (AXES) {
-        rope_quad<NG>(x, AxisAngles(p, t), p.rot, p.interleaved != 0, L);
+        rope_quad<NG>(x, StagedAngles{int(t - t0) * p.rot, p.rot / 2}, p.rot, p.interleaved != 0, L);
     } else if (p.rot > 0) {
         int pos = p.positions[t];
         pos = pos < 0 ? 0 : pos < p.max_position ? pos : p.max_position - 1;
-        rope_quad<NG>(x, RowAngles{p.cos_sin + int64_t(pos) * p.rot, p.rot / 2}, p.rot, p.interleaved != 0, L);
+        rope_quad<NG>(x, TableAngles{p.cos_sin + int64_t(pos) * p.rot, p.rot / 2}, p.rot, p.interleaved != 0, L);
     }
 }
 
@@ -228,14 +215,15 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
     if (blockIdx.x < p.q_blocks || !WRITE) {
         const bool isk = blockIdx.x >= p.q_blocks;
         const int heads = isk ? p.num_kv_heads : p.num_q_heads;
-        const unsigned vec = (blockIdx.x - (isk ? p.q_blocks : 0u)) * 64u + (threadIdx.x >> 2);
-        const unsigned t = vec / unsigned(heads);
+        const unsigned vec0 = (blockIdx.x - (isk ? p.q_blocks : 0u)) * 64u, vec = vec0 + (threadIdx.x >> 2);
+        const unsigned t = vec / unsigned(heads), t0 = vec0 / unsigned(heads);
+        if constexpr (AXES) stage_angles(p, t0, int((vec0 + 63u) / unsigned(heads) - t0) + 1);
         if (t >= p.num_tokens) return;   // whole quads
         const int h = int(vec - t * unsigned(heads));
         const int64_t row = int64_t(t) * (isk ? p.k_stride : p.q_stride) + int64_t(h) * D + 8 * L;
 #pragma unroll
         for (int j = 0; j < NG; ++j) load_x8<DT>(isk ? p.k : p.q, row + 32 * j, x[j]);
-        norm_rope_quad<NG, AXES>(x, p, t, isk ? p.k_weight : p.q_weight, L);
+        norm_rope_quad<NG, AXES>(x, p, t, t0, isk ? p.k_weight : p.q_weight, L);
         const int64_t out = int64_t(vec) * D + 8 * L;
         if (p.out_dtype == 3) {
             wht_quad<NG>(x, L);
@@ -253,6 +241,9 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         const unsigned wi = (blockIdx.x - p.q_blocks) * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int h = int(wi % unsigned(c.num_kv_heads));
         const int64_t t = int64_t(wi / unsigned(c.num_kv_heads)) * 16 + ((threadIdx.x & 63) >> 2);
+        const unsigned w0 = (blockIdx.x - p.q_blocks) * 4u;
+        const int64_t t0 = int64_t(w0 / unsigned(c.num_kv_heads)) * 16;
+        if constexpr (AXES) stage_angles(p, t0, int((w0 + 3u) / unsigned(c.num_kv_heads) - w0 / unsigned(c.num_kv_heads) + 1u) * 16);
         if (t >= c.num_tokens) return;
         const int64_t row = t * c.token_stride + int64_t(h) * D + 8 * L;
         const int64_t slot = c.slot_mapping[t];
@@ -263,7 +254,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         int off;
         const bool valid = page_of_slot(c, slot, page, off);
         if (!valid) return;
-        norm_rope_quad<NG, AXES>(x, p, t, p.k_weight, L);
+        norm_rope_quad<NG, AXES>(x, p, t, t0, p.k_weight, L);
         const int64_t ph = page * c.num_kv_heads + h;
         uint8_t* kc = c.codes + ph * (16 * D);
         uint8_t* ks = c.scales + ph * D;
@@ -271,7 +262,7 @@ __global__ void __launch_bounds__(256, NG <= 4 ? 5 : 2) norm_rope_kernel(NormRop
         quantize_xq<NG>(x, L, c.c, true, w, b, [&](float (&y)[NG][8]) {
 #pragma unroll
             for (int j = 0; j < NG; ++j) load_x8<DT>(c.k, row + 32 * j, y[j]);
-            norm_rope_quad<NG, AXES>(y, p, t, p.k_weight, L);
+            norm_rope_quad<NG, AXES>(y, p, t, t0, p.k_weight, L);
         });
         store_k_quad<NG>(kc, ks, off, L, w, b);
 #pragma unroll
@@ -340,9 +331,21 @@ template <int NG, bool WRITE, bool AXES>
 static void launch_norm_rope_ng(const NormRopeParams& p, const QuantizeParams& c, int dtype, unsigned blocks,
                                 hipStream_t stream) {
     const dim3 grid{blocks}, block{256u};
-    if (dtype == 0) hipLaunchKernelGGL((norm_rope_kernel<0, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
-    else if (dtype == 1) hipLaunchKernelGGL((norm_rope_kernel<1, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
-    else hipLaunchKernelGGL((norm_rope_kernel<2, NG, WRITE, AXES>), grid, block, 0, stream, p, c);
+    unsigned lds = 0;
+    if (AXES) {
+        // the tokens that 64 vectors reach over, or 4 units of the writer (at most 64: 64 KiB at rot 256)
+        auto tokens = [](int heads) { return heads > 0 ? (64 + heads - 2) / heads + 1 : 0; };
+        int most = tokens(p.num_q_heads);
+        if (!WRITE && tokens(p.num_kv_heads) > most) most = tokens(p.num_kv_heads);
+        if (WRITE) {
+            const int units = (4 + c.num_kv_heads - 2) / c.num_kv_heads + 1;
+            most = most > 16 * units ? most : 16 * units;
+        }
+        lds = unsigned(most * p.rot) * sizeof(float);
+    }
+    if (dtype == 0) hipLaunchKernelGGL((norm_rope_kernel<0, NG, WRITE, AXES>), grid, block, lds, stream, p, c);
+    else if (dtype == 1) hipLaunchKernelGGL((norm_rope_kernel<1, NG, WRITE, AXES>), grid, block, lds, stream, p, c);
+    else hipLaunchKernelGGL((norm_rope_kernel<2, NG, WRITE, AXES>), grid, block, lds, stream, p, c);
 }
 template <bool WRITE, bool AXES>
 static void launch_norm_rope_as(const NormRopeParams& p, const QuantizeParams& c, int head_dim, int dtype, unsigned blocks,
