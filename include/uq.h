@@ -863,8 +863,13 @@ uq_status uq_cross_attention(const uq_cache_desc *desc, const void *q, uq_dtype 
  * Errors: those of uq_extend_attention, plus INVALID_ARGUMENT for a NULL
  * weights or workspace, a weights_width below max_context, a negative last, or
  * weights or a workspace that overlap an input or each other;
- * UNSUPPORTED for 2^30 pieces of work or more (a wave's, of 512 tokens or 128
- * rows), or 2^30 query vectors that are not FP8.
+ * UNSUPPORTED for 2^30 query vectors (a token's head) or pieces of work (a wave's: 128
+ * tokens and 16 to 128 rows) or more, or a q_stride of 2^26 or more.
+ * Calls whose sequences have 64 rows (queries times query heads of a KV head; 32 at
+ * head_dim 256) or fewer on average multiply in BF16, whose products are summed to 2^-21
+ * of the largest; the others on the instruction of the attention calls, off by up to
+ * 2^-12.5 of the largest product in a score, which many rows average out.  A few single
+ * tokens beside long chunks are computed like the chunks and take longer than alone.
  */
 size_t uq_token_weights_workspace_bytes(const uq_cache_desc *desc, uq_dtype q_dtype, int64_t num_tokens, int32_t batch,
                                         int32_t num_q_heads, int32_t max_context, int32_t last);
@@ -892,8 +897,9 @@ uq_status uq_token_weights(const uq_cache_desc *desc, const void *q, uq_dtype q_
  * Errors: INVALID_ARGUMENT for null pointers, negative sizes, num_kv_heads or
  * budget < 1, sinks + recent > budget, weights_width < max_context, outputs that
  * overlap an input or each other (kept_lens is not the context_lens of the call);
- * UNSUPPORTED for batch or num_kv_heads > 65535, 2^22 (sequence, KV head)
- * pairs, or sizes above 2^30; WORKSPACE_TOO_SMALL.
+ * UNSUPPORTED for batch or num_kv_heads > 65535, 2^21 - 16 (sequence, KV head) pairs or
+ * more, sizes above 2^30, or 2^22 slices (16384 tokens of max_context for every pair) or
+ * more where max_context is above 16384; WORKSPACE_TOO_SMALL.
  */
 size_t uq_select_tokens_workspace_bytes(int32_t batch, int32_t num_kv_heads, int32_t max_context, int32_t budget);
 uq_status uq_select_tokens(const float *weights, int64_t weights_width, int32_t batch, int32_t num_kv_heads,
@@ -924,7 +930,7 @@ uq_status uq_select_tokens(const float *weights, int64_t weights_width, int32_t 
  * freed_pages and freed_count, negative sizes, num_kv_heads, budget or
  * max_pages_per_seq < 1, pools, weights or freed arrays that overlap an input or
  * each other; UNSUPPORTED as in uq_select_tokens, and for
- * max_pages_per_seq >= 2^27; WORKSPACE_TOO_SMALL.
+ * max_pages_per_seq >= 2^27 or (below 64 pairs) 2^26 - 64 pages of kept tokens; WORKSPACE_TOO_SMALL.
  */
 size_t uq_compact_kv_workspace_bytes(const uq_cache_desc *desc, int32_t batch, int32_t budget);
 uq_status uq_compact_kv(const uq_cache_desc *desc, const int32_t *kept, int32_t budget, const int32_t *kept_lens,

@@ -1025,7 +1025,7 @@ static uq_status weights_shape(const uq_cache_desc* desc, uq_dtype q_dtype, int6
     if (group > kMaxGroup || batch > 65535 || heads > 65535) return UQ_ERR_UNSUPPORTED;
     if (num_tokens >= (int64_t(1) << 24)) return UQ_ERR_UNSUPPORTED;   // rows of a KV head are numbered in 28 bits
     if (max_context > (1 << 30)) return UQ_ERR_UNSUPPORTED;
-    if (q_dtype != UQ_FP8_E4M3 && num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
+    if (num_tokens >= kMaxVectors / num_q_heads) return UQ_ERR_UNSUPPORTED;
     const int64_t seqs = num_tokens < batch ? num_tokens : batch;
     e.by_seq = last > 0 && int64_t(batch) * last < num_tokens;
     const int64_t queries = e.by_seq ? int64_t(batch) * last : num_tokens;
@@ -1161,7 +1161,8 @@ uq_status uq_token_weights(const uq_cache_desc* desc, const void* q, uq_dtype q_
 // Sizes that uq_select_tokens and uq_compact_kv share.
 static uq_status check_kept(int32_t batch, int32_t num_kv_heads, int32_t budget) {
     if (batch < 0 || num_kv_heads < 1 || budget < 1) return UQ_ERR_INVALID_ARGUMENT;
-    if (batch > 65535 || num_kv_heads > 65535 || int64_t(batch) * num_kv_heads >= kMaxBlocks / 4 || budget > (1 << 30))
+    // (two blocks of 1024 threads each, and a few more)
+    if (batch > 65535 || num_kv_heads > 65535 || int64_t(batch) * num_kv_heads >= kMaxBlocks / 8 - 16 || budget > (1 << 30))
         return UQ_ERR_UNSUPPORTED;
     return UQ_OK;
 }
@@ -1225,7 +1226,8 @@ uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t 
     uq_status s = check_desc(desc);
     if (s == UQ_OK) s = check_kept(batch, desc->num_kv_heads, budget);
     if (s != UQ_OK) return s;
-    if (max_pages_per_seq < 1 || weights_width < 0 || (freed_pages == nullptr) != (freed_count == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
+    if (max_pages_per_seq < 1 || weights_width < 0) return UQ_ERR_INVALID_ARGUMENT;
+    if (batch > 0 && (freed_pages == nullptr) != (freed_count == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
     if (max_pages_per_seq >= (1 << 27)) return UQ_ERR_UNSUPPORTED;
     if (batch > 0 && (kept == nullptr || kept_lens == nullptr || context_lens == nullptr || kv_codes == nullptr ||
                       kv_scales == nullptr || page_table == nullptr))
@@ -1234,7 +1236,7 @@ uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t 
     const size_t need = uq_compact_kv_workspace_bytes(desc, batch, budget);
     if (need > 0 && (workspace == nullptr || !aligned16(workspace))) return UQ_ERR_INVALID_ARGUMENT;
     if (workspace_bytes < need) return UQ_ERR_WORKSPACE_TOO_SMALL;
-    if (need > 0 && int64_t(batch) * desc->num_kv_heads * ((budget + kPageSize - 1) / kPageSize) >= 4 * kMaxBlocks - 8) return UQ_ERR_UNSUPPORTED;
+    if (need > 0 && int64_t(batch) * desc->num_kv_heads * ((budget + kPageSize - 1) / kPageSize) >= 4 * kMaxBlocks - 64) return UQ_ERR_UNSUPPORTED;
     const size_t word = sizeof(int32_t), rows = size_t(batch) * size_t(desc->num_kv_heads), seqs = size_t(batch);
     const std::initializer_list<Span> outs = {codes_span(desc, kv_codes), scales_span(desc, kv_scales), {weights, rows * size_t(weights_width) * word},
                          {freed_pages, seqs * size_t(max_pages_per_seq) * word}, {freed_count, word}, {workspace, need}},

@@ -555,15 +555,111 @@ __global__ void __launch_bounds__(256, NB == 1 && D <= 128 ? 4 : 2) few_rows_ker
 // two such loads.  At head size 64 half of the operands is 0, head size 256 takes two
 // instructions per page.
 
-// Row blocks of 16 NB rows times chunks of p.chunk tokens, a wave each.
+// The norms of rows r0 .. r0 + 16 NB - 1 (below `rows`) of a sequence over a chunk.
 template <int D, int NB>
-__global__ void __launch_bounds__(256, 2) token_norms_kernel(WeightsParams p) {
+__device__ __forceinline__ void norms_of_block(const WeightsParams& p, const WeightsSeq& s, int b, int hk, int chunk, int r0, int rows) {
     using Unit = KeyUnit<D>;
     constexpr int PF = 2;   // pages computed while as many are on their way (the slow path counts on 2)
     const int lane = threadIdx.x & 63, grp = lane >> 4;
-    const int waves = int(gridDim.x) * 4;
     const int pages_per_chunk = p.chunk / kPage;
     const float c = p.scale_log2;
+    const int pos0 = first_position(p, s);
+    const int r1 = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;     // the block's last row
+    const int lo = p.causal ? pos0 + weights_div(p, r0) : pos0, hi = p.causal ? pos0 + weights_div(p, r1) : pos0;
+    // pages of the chunk up to the last that a row of the block sees
+    const int u0 = chunk * pages_per_chunk;
+    int u1 = hi >= 0 ? hi / kPage + 1 : 0;
+    u1 = u1 < u0 + pages_per_chunk ? u1 : u0 + pages_per_chunk;
+    RowUnit<D> q[NB];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        if (u0 < u1) load_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
+        m[j] = kNoRow;
+        l[j] = 0.f;
+    }
+    bool big = false;
+    // a page whose tokens need not all be seen, or whose scores may be far from the reference
+    auto use_moving = [&](const Unit& k, int u) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            v4f x = unit_scores<D, true>(k, q[j]);
+            const int r = r0 + 16 * j + (lane & 15) < rows ? r0 + 16 * j + (lane & 15) : rows - 1;
+            const int pos = p.causal ? pos0 + weights_div(p, r) : pos0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = u * kPage + 4 * grp + i <= pos ? x[i] : -__builtin_inff();
+            add_moving(x, c, m[j], l[j]);
+        }
+    };
+    auto find_big = [&]() {
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) any = any | ((__builtin_fabsf(m[j]) >= kBigRef) & (m[j] != kNoRow));
+        big = __builtin_amdgcn_ballot_w64(any) != 0;
+    };
+    if (u0 < u1) {
+        PageIds ids(p, b, u0, s.n);
+        Unit cur[PF], nxt[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
+        // a lane that sees a token of the chunk sees one in its first page, or no later one
+        hide_unwritten<D>(cur[0], u0, s.n);
+        use_moving(cur[0], u0);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) l[j] = 0.f;
+        find_big();
+        for (int u = u0; u < u1; u += PF) {
+#pragma unroll
+            for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
+            // (pages behind the last are hidden from every row)
+            bool slow = big | (u * kPage + PF * kPage - 1 > lo);
+            float l0[NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) l0[j] = l[j];
+            if (__builtin_expect(!slow, 1)) {
+                // one block, in which the products of a page run beside the exponentials of another
+#pragma unroll
+                for (int i = 0; i < PF; ++i) {
+                    v4f x[NB];
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) x[j] = unit_scores<D, true>(cur[i], q[j]);
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) l[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], c, -m[j]));
+                }
+                float most = 0.f;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) most = __builtin_fmaxf(most, l[j]);
+                slow = __builtin_amdgcn_ballot_w64(!(most <= kMostSum)) != 0;
+            }
+            if (__builtin_expect(slow, 0)) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) l[j] = l0[j];
+#pragma unroll 1
+                for (int i = 0; i < PF; ++i) {
+                    Unit k = i == 0 ? cur[0] : cur[PF - 1];
+                    hide_unwritten<D>(k, u + i, s.n);
+                    use_moving(k, u + i);
+                }
+                find_big();
+            }
+#pragma unroll
+            for (int i = 0; i < PF; ++i) cur[i] = nxt[i];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int r = r0 + 16 * j + lane;
+        store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows, p.chunks > 1);
+    }
+}
+
+// Row blocks of 16 NB rows times chunks of p.chunk tokens, a wave each.  (A block of up to 16 rows, as of
+// single tokens beside prompts, does not pay for the others.)
+template <int D, int NB>
+__global__ void __launch_bounds__(256, 3) token_norms_kernel(WeightsParams p) {
+    const int waves = int(gridDim.x) * 4;
     auto count = [&](const WeightsSeq& s) {
         const int rows = s.use * p.group;
         return p.num_kv_heads * ((rows + 16 * NB - 1) / (16 * NB)) * ((s.n + p.chunk - 1) / p.chunk);
@@ -576,96 +672,8 @@ __global__ void __launch_bounds__(256, 2) token_norms_kernel(WeightsParams p) {
         const int rows = s.use * p.group, blocks = (rows + 16 * NB - 1) / (16 * NB), chunks = (s.n + p.chunk - 1) / p.chunk;
         const int rest = idx / blocks, r0 = (idx - rest * blocks) * (16 * NB);
         const int hk = rest / chunks, chunk = rest - hk * chunks;
-        const int pos0 = first_position(p, s);
-        const int r1 = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;     // the block's last row
-        const int lo = p.causal ? pos0 + weights_div(p, r0) : pos0, hi = p.causal ? pos0 + weights_div(p, r1) : pos0;
-        // pages of the chunk up to the last that a row of the block sees
-        const int u0 = chunk * pages_per_chunk;
-        int u1 = hi >= 0 ? hi / kPage + 1 : 0;
-        u1 = u1 < u0 + pages_per_chunk ? u1 : u0 + pages_per_chunk;
-        RowUnit<D> q[NB];
-        float m[NB], l[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            if (u0 < u1) load_rows<D>(p, s, hk, r0 + 16 * j, rows, q[j]);
-            m[j] = kNoRow;
-            l[j] = 0.f;
-        }
-        bool big = false;
-        // a page whose tokens need not all be seen, or whose scores may be far from the reference
-        auto use_moving = [&](const Unit& k, int u) {
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                v4f x = unit_scores<D, true>(k, q[j]);
-                const int r = r0 + 16 * j + (lane & 15) < rows ? r0 + 16 * j + (lane & 15) : rows - 1;
-                const int pos = p.causal ? pos0 + weights_div(p, r) : pos0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = u * kPage + 4 * grp + i <= pos ? x[i] : -__builtin_inff();
-                add_moving(x, c, m[j], l[j]);
-            }
-        };
-        auto find_big = [&]() {
-            bool any = false;
-#pragma unroll
-            for (int j = 0; j < NB; ++j) any = any | ((__builtin_fabsf(m[j]) >= kBigRef) & (m[j] != kNoRow));
-            big = __builtin_amdgcn_ballot_w64(any) != 0;
-        };
-        if (u0 < u1) {
-            PageIds ids(p, b, u0, s.n);
-            Unit cur[PF], nxt[PF];
-#pragma unroll
-            for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u0 + i < u1 ? u0 + i : u1 - 1), hk, cur[i]);
-            // a lane that sees a token of the chunk sees one in its first page, or no later one
-            hide_unwritten<D>(cur[0], u0, s.n);
-            use_moving(cur[0], u0);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) l[j] = 0.f;
-            find_big();
-            for (int u = u0; u < u1; u += PF) {
-#pragma unroll
-                for (int i = 0; i < PF; ++i) load_keys<D>(p, ids.at(u + PF + i < u1 ? u + PF + i : u1 - 1), hk, nxt[i]);
-                // (pages behind the last are hidden from every row)
-                bool slow = big | (u * kPage + PF * kPage - 1 > lo);
-                float l0[NB];
-#pragma unroll
-                for (int j = 0; j < NB; ++j) l0[j] = l[j];
-                if (__builtin_expect(!slow, 1)) {
-                    // one block, in which the products of a page run beside the exponentials of another
-#pragma unroll
-                    for (int i = 0; i < PF; ++i) {
-                        v4f x[NB];
-#pragma unroll
-                        for (int j = 0; j < NB; ++j) x[j] = unit_scores<D, true>(cur[i], q[j]);
-#pragma unroll
-                        for (int j = 0; j < NB; ++j)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) l[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], c, -m[j]));
-                    }
-                    float most = 0.f;
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) most = __builtin_fmaxf(most, l[j]);
-                    slow = __builtin_amdgcn_ballot_w64(!(most <= kMostSum)) != 0;
-                }
-                if (__builtin_expect(slow, 0)) {
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) l[j] = l0[j];
-#pragma unroll 1
-                    for (int i = 0; i < PF; ++i) {
-                        Unit k = i == 0 ? cur[0] : cur[PF - 1];
-                        hide_unwritten<D>(k, u + i, s.n);
-                        use_moving(k, u + i);
-                    }
-                    find_big();
-                }
-#pragma unroll
-                for (int i = 0; i < PF; ++i) cur[i] = nxt[i];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int r = r0 + 16 * j + lane;
-            store_norm(p, m[j], l[j], chunk, first_row(p, b, s, hk) + r, lane < 16 && r < rows, p.chunks > 1);
-        }
+        if (rows - r0 <= 16) norms_of_block<D, 1>(p, s, b, hk, chunk, r0, rows);
+        else norms_of_block<D, NB>(p, s, b, hk, chunk, r0, rows);
     }
 }
 

@@ -116,7 +116,8 @@ def test_token_weights():
                dict(ws=at(4) - 256), dict(ws=at(0))):
         assert weights(**kw) == INVALID, kw
     for kw in (dict(dt=4), dict(hq=34), dict(T=1 << 24), dict(B=65536), dict(D=desc(head_dim=96)),
-               dict(bound=(1 << 30) + 1), dict(D=desc(group_size=16))):
+               dict(bound=(1 << 30) + 1), dict(D=desc(group_size=16)), dict(stride=1 << 26),
+               dict(T=1 << 23, hq=128, D=desc(num_kv_heads=128), stride=128 * 128)):
         assert weights(**kw) == UNSUPPORTED, kw
     assert weights(wsb=1 << 20) == SMALL
 
@@ -151,7 +152,7 @@ def test_select_tokens():
                dict(sinks=1 << 30, recent=1 << 30), dict(width=99), dict(kl=at(1)), dict(kl=at(1) + 4), dict(kept=at(0)),
                dict(kept=at(3) - 8), dict(kl=at(0) + 400)):
         assert select(**kw) == INVALID, kw
-    for kw in (dict(B=65536), dict(H=65536), dict(B=2000, H=5000), dict(bound=(1 << 30) + 1, width=1 << 31),
+    for kw in (dict(B=65536), dict(H=65536), dict(B=2000, H=5000), dict(B=(1 << 15) - 1, H=64 + 1), dict(bound=(1 << 30) + 1, width=1 << 31),
                dict(budget=(1 << 30) + 1), dict(B=1000, H=8, bound=1 << 26, width=1 << 26)):
         assert select(**kw) == UNSUPPORTED, kw
     assert uq.select_workspace_bytes(2, 3, 16384, 10) == 0 and uq.select_workspace_bytes(2, 3, 1 << 20, 1 << 20) == 0

@@ -222,6 +222,24 @@ def test_compact_without_weights_and_freed(uq):
     assert torch.equal(codes, c2) and torch.equal(scales, s2)
 
 
+def test_compact_in_place_and_through_the_workspace(uq):
+    """64 and more (sequence, KV head) pairs are moved in place, fewer through the workspace."""
+    for d in (64, 128, 256):
+        check_compact(uq, [700 + 37 * i for i in range(16)], 500, 4, d, seed=d, sinks=16, recent=100)
+        check_compact(uq, [(97 * i) % 1200 for i in range(70)], 513, 1, d, seed=d + 1)
+        check_compact(uq, [3000, 1100], 1030, 32, d, seed=d + 2, sinks=0, recent=0)
+
+
+def test_compact_nothing(uq):
+    desc = uq.CacheDesc(num_kv_heads=2, num_pages=4)
+    codes, scales = desc.alloc_pools(DEV, fill=1)
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    count = torch.full((1,), 9, dtype=torch.int32, device=DEV)
+    uq.compact_kv(desc, torch.empty((0, 2, 8), dtype=torch.int32, device=DEV), none, none,
+                  codes, scales, torch.empty((0, 4), dtype=torch.int32, device=DEV), freed_pages=none, freed_count=count)
+    assert count.item() == 0 and (codes == 1).all()
+
+
 def test_compact_leaves_shared_front_pages(uq):
     """Pages that keep all their tokens are not written: two sequences share one."""
     desc = uq.CacheDesc(num_kv_heads=2, num_pages=12)

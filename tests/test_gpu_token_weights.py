@@ -149,6 +149,11 @@ def test_many_sequences(uq):
     Case(uq, lens, news, 6, 2, 128, seed=6, pad=9, bound=400, width_pad=13).check()
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_single_tokens_beside_a_prompt(uq, d):
+    Case(uq, [700, 3000, 45, 16, 900], [700, 1, 1, 1, 2], 8, 2, d, seed=20 + d).check()
+
+
 def test_empty_sequences_and_rows_that_see_nothing(uq):
     # no context, no queries, more queries than context: the ones before its start see nothing
     Case(uq, [0, 30, 5, 0, 20], [3, 0, 12, 0, 2], 8, 2, 128, seed=7, pad=4, bound=64).check()
@@ -199,6 +204,32 @@ def test_large_scores(uq, d):
     for b, n in enumerate(c.lens):
         for h in range(2):
             assert torch.equal(got[b, h, :n].double(), want[b][h])
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("m", [1, 60])
+def test_scores_that_climb(uq, d, m):
+    """Later tokens' scores are up to hundreds of powers of two above the first ones', in fp32's
+    range: products and sums are exact, so the weights are those of the formula to the rounding of
+    the exponential and the sums."""
+    n = 900
+    c = Case(uq, [n], [m], 16, 2, d, seed=19, scale=1.0, poison=False)
+    c.codes.fill_(0x22)                                   # every channel 1
+    exps = torch.sort(torch.randint(-12, 1, (n,), generator=torch.Generator().manual_seed(d)))[0]
+    exps[100:140] = -12                                    # (and back once)
+    page, off = c.table[0].long().cpu()[torch.arange(n) // 16], torch.arange(n) % 16
+    c.scales.view(c.desc.num_pages, 2, 2, d // 32, 16)[page.to(DEV), :, :, :, off.to(DEV)] = (
+        (exps + 127).to(torch.uint8).to(DEV)[:, None, None, None])
+    c.q = torch.ones_like(c.q.float()).to(torch.float8_e4m3fn)
+    s = d * torch.exp2(exps.double()).to(DEV)
+    want = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for i in range(m):
+        want[:n - m + i + 1] += 8 * torch.softmax(s[:n - m + i + 1], 0)
+    got = c.call(weights=torch.zeros_like(c.before))[0].double()
+    # |c s| <= 2^9: the product with c = fp32(log2 e) and the exponential's argument are off by 2^-15 each
+    tol = 2 ** -13 + (n / 4 + 8 * m / 4 + 16) * 2 ** -24
+    for h in range(2):
+        assert ((got[h, :n] - want).abs() <= tol * want + 2 ** -60).all()
 
 
 def test_equal_scores(uq):
