@@ -573,8 +573,10 @@ uq_status uq_decode_attention_noalloc(const uq_cache_desc *desc, const void *q, 
  * slots and positions; uq_norm_rope(_write) takes the rows of the QKV
  * projection to prepared queries and cache entries; uq_read_kv gives stored
  * tokens back as rows; uq_extend_attention is attention for several new
- * queries per sequence (prompt chunks, drafted tokens), uq_decode_window for
- * one query per sequence under a sliding window.
+ * queries per sequence (prompt chunks, drafted tokens), uq_cross_attention for
+ * queries over tokens without order, uq_decode_window for one query per
+ * sequence under a sliding window.  uq_token_weights, uq_select_tokens and
+ * uq_compact_kv keep a sequence's cache within a budget.
  * ---------------------------------------------------------------------- */
 
 /*
@@ -930,7 +932,8 @@ uq_status uq_select_tokens(const float *weights, int64_t weights_width, int32_t 
  * freed_pages and freed_count, negative sizes, num_kv_heads, budget or
  * max_pages_per_seq < 1, pools, weights or freed arrays that overlap an input or
  * each other; UNSUPPORTED as in uq_select_tokens, and for
- * max_pages_per_seq >= 2^27 or (below 64 pairs) 2^26 - 64 pages of kept tokens; WORKSPACE_TOO_SMALL.
+ * max_pages_per_seq >= 2^27, 2^31 entries of freed_pages or (below 64 pairs) 2^26 - 64 pages of kept
+ * tokens; WORKSPACE_TOO_SMALL.
  */
 size_t uq_compact_kv_workspace_bytes(const uq_cache_desc *desc, int32_t batch, int32_t budget);
 uq_status uq_compact_kv(const uq_cache_desc *desc, const int32_t *kept, int32_t budget, const int32_t *kept_lens,
@@ -1050,7 +1053,7 @@ uq_status uq_probe_mfma(int32_t kind, const void *a, const void *b, const uint8_
  * uq_time_next_launch(start, stop), the next launch of the decode partition
  * kernel (by uq_decode_attention, uq_decode_partials,
  * uq_decode_step(_partials), uq_decode_window, the cascade calls or their
- * comparison-cache forms), of uq_extend_attention's first kernel, of the quantize-on-write kernel (uq_quantize_kv) or of a bandwidth
+ * comparison-cache forms), of uq_extend_attention's or uq_cross_attention's first kernel, of the quantize-on-write kernel (uq_quantize_kv) or of a bandwidth
  * probe (uq_probe_stream_read, uq_probe_page_gather(_cascade)) made from the calling
  * host thread is dispatched with hipExtLaunchKernel, which sets
  * `start` and `stop` (hipEvent_t, created by the caller, not owned by the

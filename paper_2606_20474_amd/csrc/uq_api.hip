@@ -1229,6 +1229,8 @@ uq_status uq_compact_kv(const uq_cache_desc* desc, const int32_t* kept, int32_t 
     if (max_pages_per_seq < 1 || weights_width < 0) return UQ_ERR_INVALID_ARGUMENT;
     if (batch > 0 && (freed_pages == nullptr) != (freed_count == nullptr)) return UQ_ERR_INVALID_ARGUMENT;
     if (max_pages_per_seq >= (1 << 27)) return UQ_ERR_UNSUPPORTED;
+    // the list is numbered in 31 bits
+    if (freed_count != nullptr && int64_t(batch) * max_pages_per_seq > INT32_MAX) return UQ_ERR_UNSUPPORTED;
     if (batch > 0 && (kept == nullptr || kept_lens == nullptr || context_lens == nullptr || kv_codes == nullptr ||
                       kv_scales == nullptr || page_table == nullptr))
         return UQ_ERR_INVALID_ARGUMENT;

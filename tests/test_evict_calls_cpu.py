@@ -177,7 +177,8 @@ def test_compact_kv():
                dict(w=at(0)), dict(w=at(3) + 128), dict(freed=at(5)), dict(freed=at(2)), dict(count=at(1)),
                dict(count=at(7) + 8), dict(scales=at(3) + 64)):
         assert compact(**kw) == INVALID, kw
-    for kw in (dict(B=65536), dict(mpps=1 << 27), dict(budget=(1 << 30) + 1), dict(D=desc(head_dim=96))):
+    for kw in (dict(B=65536), dict(mpps=1 << 27), dict(budget=(1 << 30) + 1), dict(D=desc(head_dim=96)),
+               dict(B=32, mpps=1 << 26)):
         assert compact(**kw) == UNSUPPORTED, kw
     assert compact(B=0, freed=None, count=None) == OK
     D = desc()
