@@ -23,10 +23,12 @@ namespace uq {
 // bits from the lists (from the slice itself where there are more than a list holds) and
 // the indices.  Every block of a row finds the same; none waits for another.
 //
-// Bound by latency: 32 sequences of about 32k tokens and 4 heads (21 MB) take 8, 11 and 25 us,
+// Bound by latency: 32 sequences of about 32k tokens and 4 heads (21 MB) take 7, 11 and 18 us,
 // 8 rows of 131000 tokens 5, 9 and 13, with five waits for all threads of a block in each.  One block
 // per row whatever its length took 79 and 168 us: it reads the row four times, and 8 rows fill 8
-// CUs.  The lists held in registers rather than read in each pass: 33 -> 25 us of the last launch.
+// CUs.  Lists held in registers rather than read in each pass, 33 -> 25 us of the last launch; two blocks per
+// CU, and the first slices of all rows before the second ones (rows end at different slices, which
+// left half of the XCDs idle), 25 -> 18.
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectBins = 2048;
@@ -226,7 +228,7 @@ __device__ __forceinline__ int2* first_bits_of(const SelectParams& p, int row) {
 
 __global__ void __launch_bounds__(kSelectThreads) select_count_kernel(SelectParams p) {
     __shared__ __attribute__((aligned(16))) SelectCounts c;
-    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const int row = int(blockIdx.x % unsigned(p.batch * p.heads)), slice = int(blockIdx.x / unsigned(p.batch * p.heads));
     const SelectRow r = select_row(p, row, slice);
     if (r.n <= p.budget) {
         if (slice == 0) keep_all(p, r, row);
@@ -248,7 +250,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_count_kernel(SelectPara
 __global__ void __launch_bounds__(kSelectThreads) select_list_kernel(SelectParams p) {
     __shared__ SelectCounts c;
     __shared__ int listed;
-    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const int row = int(blockIdx.x % unsigned(p.batch * p.heads)), slice = int(blockIdx.x / unsigned(p.batch * p.heads));
     const SelectRow r = select_row(p, row, slice);
     if (r.n <= p.budget || slice * kSelectSlice >= r.n) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -296,10 +298,10 @@ __global__ void __launch_bounds__(kSelectThreads) select_list_kernel(SelectParam
     }
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectParams p) {
+__global__ void __launch_bounds__(kSelectThreads, 8) select_write_kernel(SelectParams p) {
     __shared__ __attribute__((aligned(16))) SelectCounts c;
     __shared__ int sums[2];
-    const int row = int(blockIdx.x / unsigned(p.slices)), slice = int(blockIdx.x % unsigned(p.slices));
+    const int row = int(blockIdx.x % unsigned(p.batch * p.heads)), slice = int(blockIdx.x / unsigned(p.batch * p.heads));
     const SelectRow r = select_row(p, row, slice);
     if (r.n <= p.budget || slice * kSelectSlice >= r.n) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -307,9 +309,10 @@ __global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectPara
     uint32_t least = 0xFFFFFFFFu, bits = 0xFFFFFFFFu;
     int ties = 0, above = 0;
     if (threadIdx.x < 2) sums[threadIdx.x] = 0;
-    // Up to 8 slices whose keys are all listed: a wave holds every fourth 64 of a list, twice; a place
-    // without a key has other first bits.
-    constexpr int Q = kSelectList / 4 / 64, kUnits = 2;
+    // Up to 8 slices of up to 1024 listed keys: a wave holds every fourth 64 of a list, twice; a place
+    // without a key has other first bits.  (All 4096 in registers leave room for one block per CU, not two:
+    // 23 us instead of 18.)
+    constexpr int Q = 4, kUnits = 2;
     uint32_t held[kUnits][Q];
     int sets[kUnits] = {0, 0};       // of 64 places with a key
     bool hold = 4 * slices <= kUnits * (kSelectThreads / 64);
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_write_kernel(SelectPara
         above = first.y;
         if (hold) {
             const int listed = slice_of(p, row, lane < slices ? lane : 0)->listed;
-            hold = __builtin_amdgcn_ballot_w64(listed > kSelectList) == 0;
+            hold = __builtin_amdgcn_ballot_w64(listed > 256 * Q) == 0;
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
                 const int unit = wave + u * (kSelectThreads / 64), q = unit & 3;
