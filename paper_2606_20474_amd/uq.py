@@ -703,7 +703,7 @@ class NormRope:
         """The ``uq_rope_axes`` of the spec, or None."""
         if self.pair_axes is None:
             return None
-        axes = bytes(self.pair_axes)
+        axes = bytes(list(self.pair_axes))   # (a number is no sequence of axes)
         if len(axes) != self.cos_sin.shape[1] // 2:
             raise ValueError(f"pair_axes: {len(axes)} axes, expected {self.cos_sin.shape[1] // 2}, one per rotated pair")
         return uq_rope_axes(self.positions.shape[0], self.positions.shape[1], axes)

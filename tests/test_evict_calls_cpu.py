@@ -201,3 +201,16 @@ def test_binding_wants_gpu_tensors():
                  lambda: uq.norm_rope(uq.NormRope(i(3, 3), torch.zeros((4, 128)), pair_axes=[0] * 64), q)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_pair_axes_from_sequences():
+    sp = uq.NormRope(torch.zeros((3, 5), dtype=torch.int32), torch.zeros(8, 16), pair_axes=(0, 0, 1, 1, 2, 2, 0, 1))
+    want = sp.axes_struct().pair_axes
+    for axes in (list(sp.pair_axes), bytes(sp.pair_axes), torch.tensor(sp.pair_axes), torch.tensor(sp.pair_axes).numpy()):
+        sp.pair_axes = axes
+        a = sp.axes_struct()
+        assert (a.num_axes, a.position_stride, a.pair_axes) == (3, 5, want)
+    for axes in (8, (0,) * 7, (0,) * 7 + (256,), (0,) * 7 + (-1,), (0,) * 7 + (0.5,)):
+        sp.pair_axes = axes
+        with pytest.raises((TypeError, ValueError)):
+            sp.axes_struct()
